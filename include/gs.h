@@ -11,6 +11,8 @@
  * figure).  Because the update is element-wise it may be applied to any contiguous range:
  * in full, split into an immediate part and a deferred part (delay ratio alpha, Sec. 4.4),
  * or chunk by chunk over states that live in host memory (Sec. 2.2 chunk loop; Sec. 4.3).
+ *   Beside the step: the losses that post-training takes its gradients from, and the norm and clip of
+ * gradients that are many tensors (their own conventions on shapes and alignment stand with them).
  *
  * Conventions for every entry point
  *   - Plain C types only.  "device" pointers are HIP device addresses, "host" pointers are
@@ -480,6 +482,151 @@ const char *gs_tier_ctx_error(gs_tier_ctx *ctx);
  * states of tens of GB cannot afford that).  Returns NULL on failure. */
 void *gs_pinned_alloc(size_t bytes);
 void gs_pinned_free(void *ptr);
+
+/* ------------------------------------------------------------------------------------------
+ * Where the gradients come from: the losses of post-training, on rows of logits.  Row r belongs
+ * to one token whose id is targets[r]; with z the row, it = 1/temperature,
+ *     M = max_i z_i,   S = sum_i exp(it (z_i - M)),   logp = it (z_t - M) - ln S,
+ *     dlogp/dz_i = it ([i = t] - exp(it (z_i - M)) / S).
+ * A target outside [0, vocab) (-1, -100: padding, a prompt) marks a row without a token: its logits are not
+ * read, its logp is 0 and its gradient +0.  Logits may hold -inf (excluded tokens); a row of nothing
+ * else, or one with a NaN or +inf, gives NaN, as the formula does.  Maxima, sums and
+ * log-probabilities are held in 32 bits, sums over tokens in 64; gradients are rounded once, to the logits' type.
+ * All results are the same from call to call.
+ * ------------------------------------------------------------------------------------------ */
+
+typedef enum {
+    GS_BF16 = 0,
+    GS_F32 = 1
+} gs_dtype;
+
+/* rows x vocab logits; row r starts at element r * row_stride.  data: device, aligned to its type; row_stride >= vocab
+ * (any value with one row), vocab in [1, 2^30].  rows == 0 is an empty batch (pointers are then not looked at). */
+typedef struct {
+    const void *data;
+    int64_t rows;
+    int64_t vocab;
+    int64_t row_stride;
+    int32_t dtype;          /* gs_dtype */
+} gs_logits;
+
+/*
+ * Log-probability of one given token per row: scoring of sequences, or of the token just drawn (rows == 1).
+ *   targets      device int64, `rows` ids
+ *   temperature  in [1e-4, 1e4]
+ *   logp         device fp32, `rows` values
+ *   row_stats    NULL, or device fp32, 2 x `rows`: (M, S) of every row, for gs_token_logp_grad ((0, 1) in rows without a token)
+ *   workspace    as for gs_grad_sqnorm; long rows are split over several workgroups while there are few of them
+ */
+gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float temperature, float *logp, float *row_stats,
+                        void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of a loss in the logits, from its gradient in the token log-probabilities:
+ *     dlogits[r][i] = dlogp[r] dlogp/dz_i
+ * with (M, S) as gs_token_logp left them for the same logits, targets and temperature.  A row with dlogp[r] == 0, or without a token,
+ * gets +0 and is not read.
+ *   dlogits      device, the logits' type and shape, row r at element r * dlogits_stride (>= vocab); may be the logits
+ *                themselves (same address and stride), else must not overlap them
+ */
+gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, float temperature, const float *row_stats,
+                             const float *dlogp, void *dlogits, int64_t dlogits_stride, void *stream);
+
+/* Clipped policy loss: ratios are held within [1 - clip_low, 1 + clip_high] (0 <= clip_low <= 1, clip_high >= 0), the
+ * KL term's factor is kl_coef >= 0; all finite. */
+typedef struct {
+    float temperature;
+    float clip_low;
+    float clip_high;
+    float kl_coef;
+} gs_policy_hparams;
+
+/*
+ * Clipped policy loss with a KL term over the tokens drawn, forward and backward in one pass over the logits:
+ *     ratio = exp(logp - old_logp)
+ *     pg    = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A)      A = advantages[r]
+ *     kl    = exp(d) - d - 1,  d = ref_logp - logp                             (0 without ref_logp)
+ *     loss  = sum_r weights[r] (pg + kl_coef kl)
+ *     dloss/dlogp = weights[r] (-(ratio A, 0 where the clamped product is the smaller) + kl_coef (1 - exp(d)))
+ * and dlogits = dloss/dlogp dlogp/dz.  With kl_coef == 0 kl is reported but takes no part.
+ *   old_logp, advantages  device fp32, `rows`
+ *   ref_logp     device fp32, `rows`, or NULL
+ *   weights      device fp32, `rows`, or NULL for ones: a mask times whatever the loss is divided by.  Where it is 0 the row is as one
+ *                without a token: nothing else of it is read
+ *   logp         device fp32, `rows`, written
+ *   dlogits      as for gs_token_logp_grad, or NULL: no gradient
+ *   d_stats      device fp32, 4 values: sums of weights times (pg + kl_coef kl), pg, kl, [clamped product smaller];
+ *                added to what is there with accumulate != 0 (micro-batches)
+ *   workspace    as for gs_grad_sqnorm
+ */
+gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const gs_policy_hparams *hp, const float *old_logp,
+                         const float *ref_logp, const float *advantages, const float *weights, float *logp, void *dlogits,
+                         int64_t dlogits_stride, float *d_stats, int accumulate, void *d_workspace, size_t workspace_bytes,
+                         void *stream);
+
+/* Preference loss: beta > 0, 0 <= label_smoothing < 1, scale (1 / pairs for a mean); all finite. */
+typedef struct {
+    float beta;
+    float label_smoothing;
+    float scale;
+} gs_preference_hparams;
+
+/*
+ * Preference loss over pairs of sequences, forward and backward on the log-probabilities of their tokens.  Sequence s
+ * holds the tokens [offsets[s], offsets[s+1]); sequences 0 .. pairs-1 are the chosen ones, pairs .. 2 pairs - 1 the rejected
+ * ones of the same pairs.
+ *     D_s  = sum over the tokens of s of weights (logp - ref_logp)
+ *     h    = beta (D_p - D_{pairs+p})                                          -> margins[p]
+ *     loss = scale sum_p -(1 - e) ln sigmoid(h) - e ln sigmoid(-h)             e = label_smoothing
+ *     dlogp = +-scale beta weights (e sigmoid(h) - (1 - e) sigmoid(-h))        (minus in rejected sequences)
+ *   logp       device fp32, `tokens`
+ *   ref_logp   device fp32, `tokens`, or NULL for zeros
+ *   weights    device fp32, `tokens`, or NULL for ones.  Where it is 0 nothing else of the token is read, and its dlogp is +0
+ *   offsets    device int64, 2 pairs + 1, not decreasing, within [0, tokens] (each is taken into that range).  Tokens before the first
+ *              and from the last on belong to no sequence; their dlogp is +0
+ *   margins    device fp32, `pairs`;  dlogp: device fp32, `tokens`
+ *   d_loss     device fp32, one value; added to what is there with accumulate != 0
+ *   workspace  as for gs_grad_sqnorm
+ * dlogp may not overlap an input.  An empty sequence has D = 0; pairs == 0 leaves a loss of 0 and dlogp +0.
+ */
+gs_status gs_preference_loss(const float *logp, const float *ref_logp, const float *weights, int64_t tokens,
+                             const int64_t *offsets, int64_t pairs, const gs_preference_hparams *hp, float *margins, float *dlogp,
+                             float *d_loss, int accumulate, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Norm and clip of gradients that are many tensors and not one flat layer (Sec. 2.1: clipping needs the global norm).
+ * ------------------------------------------------------------------------------------------ */
+
+/* One contiguous tensor of `numel` elements, aligned to its type.  out: where its clipped gradient goes, NULL for in place. */
+typedef struct {
+    const void *data;
+    void *out;
+    int64_t numel;
+    int32_t dtype;          /* gs_dtype */
+} gs_tensor;
+
+#define GS_MAX_TENSORS 65536
+
+/*
+ * S = sum over all elements of all tensors of g^2, squares and sum in fp64, in a fixed order.  *d_sqnorm, accumulate, the
+ * workspace as for gs_grad_sqnorm; the step reads *d_sqnorm as it does that call's.
+ *   tensors   host array of `count` (0 .. GS_MAX_TENSORS) tensors, copied by value; empty tensors may be among them, of which no
+ *             address is looked at; `out` is not looked at
+ */
+gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqnorm, int accumulate, void *d_workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * Scales every tensor by c = min(1, max_norm / (sqrt(*d_sqnorm) + 1e-6)), rounding each product once to fp32 and, in bf16
+ * tensors, once more to bf16.  *d_sqnorm is read on the device; a NaN norm gives c = 1 and an infinite one c = 0, as in the
+ * step.  Where c is 1, tensors that are scaled in place are not touched.
+ *   max_norm   > 0
+ *   d_norm     NULL, or device fp32 that receives sqrt(*d_sqnorm)
+ * An output may be exactly its own input; any other overlap of an output with an input or an output is GS_ERR_INVALID_ARG,
+ * a tensor that is listed twice among them (gs_grads_sqnorm counts one as often as it is listed).
+ */
+gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, float max_norm, float *d_norm,
+                        void *stream);
 
 /* ------------------------------------------------------------------------------------------ */
 const char *gs_strerror(gs_status s);

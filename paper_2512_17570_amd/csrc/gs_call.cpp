@@ -10,7 +10,7 @@
 // then reads the same arguments in its general way, which decides what is accepted and raises what it raises.
 // So this file only has to recognise the usual form, never to refuse: plain CUDA tensors (torch.Tensor or
 // Parameter, no subclass and no torch function mode), gradients in a list or tuple, whole numbers as int,
-// HParams as gs.py defines it, the stream as None, an int or an object with an int `cuda_stream`.
+// HParams (and the losses' hyper-parameters) as gs.py defines them, the stream as None, an int or an object with an int `cuda_stream`.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
@@ -19,6 +19,7 @@
 #include <pthread.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "gs.h"
 
@@ -34,7 +35,14 @@ decltype(&::gs_accum_adamw) f_accum_adamw;
 decltype(&::gs_adamw_from_acc) f_adamw_from_acc;
 decltype(&::gs_accum_adamw_oop) f_accum_adamw_oop;
 decltype(&::gs_accum_adamw_spec) f_accum_adamw_spec;
-PyTypeObject *hparams_type;
+decltype(&::gs_token_logp) f_token_logp;
+decltype(&::gs_token_logp_grad) f_token_logp_grad;
+decltype(&::gs_policy_loss) f_policy_loss;
+decltype(&::gs_preference_loss) f_preference_loss;
+decltype(&::gs_grads_sqnorm) f_grads_sqnorm;
+decltype(&::gs_grads_clip) f_grads_clip;
+PyTypeObject *hparams_type, *policy_type, *preference_type;
+PyObject *policy_names[4], *preference_names[3];
 PyObject *in_bad_fork;
 bool forked;                       // this process is a child of the one that made the set-up, or torch called it a bad fork then
 PyObject *hp_names[7];
@@ -136,6 +144,79 @@ struct Reader {
                 no();
             }
             Py_DECREF(x);
+        }
+    }
+
+    // a tensor of `type` with `count` contiguous elements or more; None where that is an answer
+    template <typename T>
+    T *typed(PyObject *o, int64_t count, at::ScalarType type, bool optional = false)
+    {
+        if (optional && o == Py_None) return nullptr;
+        const at::Tensor *t = tensor(o);
+        if (!t) return nullptr;
+        if (t->scalar_type() != type || t->numel() < count || !t->is_contiguous()) return no(), nullptr;
+        return static_cast<T *>(t->data_ptr());
+    }
+    float *f32(PyObject *o, int64_t count, bool optional = false) { return typed<float>(o, count, at::kFloat, optional); }
+
+    int32_t dtype(const at::Tensor &t)
+    {
+        if (t.scalar_type() == at::kBFloat16) return GS_BF16;
+        if (t.scalar_type() == at::kFloat) return GS_F32;
+        return (int32_t)no();
+    }
+
+    gs_logits matrix(PyObject *o)
+    {
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) return no(), gs_logits{};
+        return {t->data_ptr(), t->size(0), t->size(1), t->stride(0), dtype(*t)};
+    }
+    gs_logits matrix_like(PyObject *o, const gs_logits &x)
+    {
+        const gs_logits m = matrix(o);
+        if (m.rows != x.rows || m.vocab != x.vocab || m.dtype != x.dtype) no();
+        return m;
+    }
+
+    float real(PyObject *o)
+    {
+        if (!PyFloat_CheckExact(o)) return (float)no();
+        return (float)PyFloat_AS_DOUBLE(o);
+    }
+
+    template <int N>
+    void reals(PyObject *o, PyTypeObject *type, PyObject *const (&names)[N], float *const (&to)[N])
+    {
+        if (Py_TYPE(o) != type) return (void)no();
+        for (int i = 0; i < N && usual; ++i) {
+            PyObject *x = PyObject_GetAttr(o, names[i]);
+            if (!x) return (void)no();
+            *to[i] = real(x);
+            Py_DECREF(x);
+        }
+    }
+
+    // a list of tensors, and the list of their outputs unless that is None
+    void tensors(PyObject *o, PyObject *outs, std::vector<gs_tensor> &to)
+    {
+        if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return (void)no();
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+        if (outs != Py_None && ((!PyList_CheckExact(outs) && !PyTuple_CheckExact(outs)) || PySequence_Fast_GET_SIZE(outs) != n)) return (void)no();
+        to.reserve(n);
+        for (Py_ssize_t i = 0; i < n && usual; ++i) {
+            const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(o, i));
+            if (!t || !t->is_contiguous()) return (void)no();
+            gs_tensor x = {t->data_ptr(), nullptr, t->numel(), dtype(*t)};
+            if (outs != Py_None) {
+                PyObject *out = PySequence_Fast_GET_ITEM(outs, i);
+                const at::Tensor *q = out == Py_None ? nullptr : tensor(out);
+                if (q) {
+                    if (q->numel() != x.numel || q->scalar_type() != t->scalar_type() || !q->is_contiguous()) return (void)no();
+                    x.out = q->data_ptr();
+                }
+            }
+            to.push_back(x);
         }
     }
 
@@ -361,6 +442,141 @@ PyObject *accum_adamw_spec(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// logits, targets, logp, row_stats, temperature, d_workspace, workspace_bytes, stream
+PyObject *token_logp(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_logits x = {};
+    const int64_t *targets = nullptr;
+    float *logp = nullptr, *stats = nullptr, temperature = 0;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    return run<8>(n, [&](Reader &r) {
+        x = r.matrix(a[0]);
+        targets = r.typed<const int64_t>(a[1], x.rows, at::kLong), logp = r.f32(a[2], x.rows), stats = r.f32(a[3], 2 * x.rows, true);
+        temperature = r.real(a[4]), ws = r.address(a[5]), bytes = r.workspace_bytes(a[6], a[5]), s = r.stream(a[7]);
+    }, [&] { return f_token_logp(&x, targets, temperature, logp, stats, ws, bytes, s); });
+}
+
+// logits, targets, row_stats, dlogp, dlogits, temperature, stream
+PyObject *token_logp_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_logits x = {}, out = {};
+    const int64_t *targets = nullptr;
+    const float *stats = nullptr, *dlogp = nullptr;
+    float temperature = 0;
+    void *s = nullptr;
+    return run<7>(n, [&](Reader &r) {
+        x = r.matrix(a[0]);
+        targets = r.typed<const int64_t>(a[1], x.rows, at::kLong), stats = r.f32(a[2], 2 * x.rows), dlogp = r.f32(a[3], x.rows);
+        out = r.matrix_like(a[4], x), temperature = r.real(a[5]), s = r.stream(a[6]);
+    }, [&] { return f_token_logp_grad(&x, targets, temperature, stats, dlogp, const_cast<void *>(out.data), out.row_stride, s); });
+}
+
+// logits, targets, old_logp, ref_logp, advantages, weights, hp, logp, dlogits, d_stats, d_workspace, workspace_bytes, accumulate, stream
+PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_logits x = {}, out = {};
+    gs_policy_hparams hp = {};
+    const int64_t *targets = nullptr;
+    const float *old = nullptr, *ref = nullptr, *adv = nullptr, *weights = nullptr;
+    float *logp = nullptr, *stats = nullptr;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    int acc = 0;
+    return run<14>(n, [&](Reader &r) {
+        x = r.matrix(a[0]);
+        targets = r.typed<const int64_t>(a[1], x.rows, at::kLong);
+        old = r.f32(a[2], x.rows), ref = r.f32(a[3], x.rows, true), adv = r.f32(a[4], x.rows), weights = r.f32(a[5], x.rows, true);
+        r.reals(a[6], policy_type, policy_names, {&hp.temperature, &hp.clip_low, &hp.clip_high, &hp.kl_coef});
+        logp = r.f32(a[7], x.rows);
+        if (a[8] != Py_None) out = r.matrix_like(a[8], x);
+        stats = r.f32(a[9], 4);
+        ws = r.address(a[10]), bytes = r.workspace_bytes(a[11], a[10]), acc = r.flag(a[12]), s = r.stream(a[13]);
+    }, [&] {
+        return f_policy_loss(&x, targets, &hp, old, ref, adv, weights, logp, const_cast<void *>(out.data), out.row_stride, stats, acc, ws, bytes, s);
+    });
+}
+
+// logp, ref_logp, weights, offsets, hp, margins, dlogp, d_loss, d_workspace, workspace_bytes, accumulate, stream
+PyObject *preference_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_preference_hparams hp = {};
+    int64_t tokens = 0, pairs = 0;
+    const float *logp = nullptr, *ref = nullptr, *weights = nullptr;
+    const int64_t *offsets = nullptr;
+    float *margins = nullptr, *dlogp = nullptr, *loss = nullptr;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    int acc = 0;
+    return run<12>(n, [&](Reader &r) {
+        const at::Tensor *t = r.tensor(a[0]), *m = r.tensor(a[5]);
+        if (!t || !m) return;
+        tokens = t->numel(), pairs = m->numel();
+        logp = r.f32(a[0], tokens), ref = r.f32(a[1], tokens, true), weights = r.f32(a[2], tokens, true);
+        offsets = r.typed<const int64_t>(a[3], 2 * pairs + 1, at::kLong);
+        r.reals(a[4], preference_type, preference_names, {&hp.beta, &hp.label_smoothing, &hp.scale});
+        margins = r.f32(a[5], pairs), dlogp = r.f32(a[6], tokens), loss = r.f32(a[7], 1);
+        ws = r.address(a[8]), bytes = r.workspace_bytes(a[9], a[8]), acc = r.flag(a[10]), s = r.stream(a[11]);
+    }, [&] { return f_preference_loss(logp, ref, weights, tokens, offsets, pairs, &hp, margins, dlogp, loss, acc, ws, bytes, s); });
+}
+
+// tensors, d_sqnorm, d_workspace, workspace_bytes, accumulate, stream
+PyObject *grads_sqnorm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    std::vector<gs_tensor> list;
+    double *sq = nullptr;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    int acc = 0;
+    return run<6>(n, [&](Reader &r) {
+        r.tensors(a[0], Py_None, list);
+        sq = r.typed<double>(a[1], 1, at::kDouble);
+        ws = r.address(a[2]), bytes = r.workspace_bytes(a[3], a[2]), acc = r.flag(a[4]), s = r.stream(a[5]);
+    }, [&] { return f_grads_sqnorm(list.data(), (int64_t)list.size(), sq, acc, ws, bytes, s); });
+}
+
+// tensors, d_sqnorm, max_norm, d_norm, outs, stream
+PyObject *grads_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    std::vector<gs_tensor> list;
+    const double *sq = nullptr;
+    float max_norm = 0, *norm = nullptr;
+    void *s = nullptr;
+    return run<6>(n, [&](Reader &r) {
+        r.tensors(a[0], a[4], list);
+        sq = r.typed<const double>(a[1], 1, at::kDouble), max_norm = r.real(a[2]), norm = r.f32(a[3], 1, true), s = r.stream(a[5]);
+    }, [&] { return f_grads_clip(list.data(), (int64_t)list.size(), sq, max_norm, norm, s); });
+}
+
+template <int N>
+bool intern(PyObject *(&to)[N], const char *const (&names)[N])
+{
+    for (int i = 0; i < N; ++i)
+        if (!(to[i] = PyUnicode_InternFromString(names[i]))) return false;
+    return true;
+}
+
+// the six entry points above (addresses in that order), PolicyHParams, PreferenceHParams
+PyObject *setup_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *f[6];
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "setup_loss takes 8 arguments"), nullptr;
+    for (int i = 0; i < 6; ++i)
+        if (!(f[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "null entry point");
+    if (!PyType_Check(a[6]) || !PyType_Check(a[7])) return PyErr_Format(PyExc_TypeError, "hyper-parameters are not classes");
+    f_token_logp = reinterpret_cast<decltype(f_token_logp)>(f[0]);
+    f_token_logp_grad = reinterpret_cast<decltype(f_token_logp_grad)>(f[1]);
+    f_policy_loss = reinterpret_cast<decltype(f_policy_loss)>(f[2]);
+    f_preference_loss = reinterpret_cast<decltype(f_preference_loss)>(f[3]);
+    f_grads_sqnorm = reinterpret_cast<decltype(f_grads_sqnorm)>(f[4]);
+    f_grads_clip = reinterpret_cast<decltype(f_grads_clip)>(f[5]);
+    if (!intern(policy_names, {"temperature", "clip_low", "clip_high", "kl_coef"})) return nullptr;
+    if (!intern(preference_names, {"beta", "label_smoothing", "scale"})) return nullptr;
+    policy_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(a[6]));
+    preference_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(a[7]));
+    Py_RETURN_NONE;
+}
+
 // entry points by name (addresses in the order below), HParams, in a bad fork
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -393,7 +609,8 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {
     GS_METHOD(setup), GS_METHOD(grad_sqnorm), GS_METHOD(grad_sqnorm_noalloc), GS_METHOD(grad_accum_sqnorm),
     GS_METHOD(accum_add), GS_METHOD(acc_sqnorm), GS_METHOD(accum_adamw), GS_METHOD(adamw_from_acc),
-    GS_METHOD(accum_adamw_oop), GS_METHOD(accum_adamw_spec), {nullptr, nullptr, 0, nullptr}};
+    GS_METHOD(accum_adamw_oop), GS_METHOD(accum_adamw_spec), GS_METHOD(setup_loss), GS_METHOD(token_logp), GS_METHOD(token_logp_grad),
+    GS_METHOD(policy_loss), GS_METHOD(preference_loss), GS_METHOD(grads_sqnorm), GS_METHOD(grads_clip), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gs_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,583 @@
+// gs_loss.hip -- the losses that post-training takes its gradients from: token log-probabilities over rows of logits and
+// their gradient, the clipped policy loss with a KL term, and the preference loss over pairs of sequences.
+//
+// All the work is one or two passes over rows of logits (2 or 4 bytes an element, one row a token, up to a few hundred
+// thousand elements a row): read, and for a gradient written once, with two exponentials an element and no product of
+// matrices, so HBM is the bound and there is no MFMA here.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "gs_device.h"
+#include "gs_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace gs {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// ---- an element type: 16-byte vectors of it, to fp32 and back -------------------------------
+struct Bf16 {
+    typedef uint16_t T;
+    static constexpr int PER = 8;
+    static __device__ __forceinline__ float load(const T *p) { return __uint_as_float((uint32_t)*p << 16); }
+    static __device__ __forceinline__ void store(T *p, float f) { *p = (T)f32_to_bf16_bits(f); }
+    static __device__ __forceinline__ void widen(u32x4 q, float (&z)[PER])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[2 * i] = bf16_lo(q[i]), z[2 * i + 1] = bf16_hi(q[i]);
+    }
+    static __device__ __forceinline__ u32x4 narrow(const float (&g)[PER])
+    {
+        u32x4 q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                 // rounded to nearest even, NaN stays NaN
+            bf16x2 h = {(__bf16)g[2 * i], (__bf16)g[2 * i + 1]};
+            q[i] = __builtin_bit_cast(uint32_t, h);
+        }
+        return q;
+    }
+};
+struct F32 {
+    typedef float T;
+    static constexpr int PER = 4;
+    static __device__ __forceinline__ float load(const T *p) { return *p; }
+    static __device__ __forceinline__ void store(T *p, float f) { *p = f; }
+    static __device__ __forceinline__ void widen(u32x4 q, float (&z)[PER])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = __uint_as_float(q[i]);
+    }
+    static __device__ __forceinline__ u32x4 narrow(const float (&g)[PER])
+    {
+        return u32x4{__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3])};
+    }
+};
+
+// Elements [0, n) of a row from an address of any alignment: `head` single ones, `vecs` whole aligned vectors, the rest
+// single again.  Only what lies in the row is touched.
+struct Cut {
+    int head, vecs, singles;      // singles: those in front and behind together
+    template <int PER> static __device__ __forceinline__ Cut of(const void *p, int n, bool vectors)
+    {
+        constexpr int SIZE = 16 / PER;
+        Cut c;
+        c.head = vectors ? min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE) : n;
+        c.vecs = (n - c.head) / PER;
+        c.singles = n - c.vecs * PER;
+        return c;
+    }
+    // the element that single i is
+    template <int PER> __device__ __forceinline__ int single(int i) const { return i < head ? i : i + vecs * PER; }
+};
+
+// ---- sums of exponentials ---------------------------------------------------------------------
+// sum of exp2(k (z - m)) with its maximum so far.  With nothing but -inf so far the exponents are taken from 0, which leaves 0.
+struct MaxSum {
+    float m, s;
+    __device__ __forceinline__ void merge(float om, float os, float k)
+    {
+        const float n = fmaxf(m, om), base = n == -INFINITY ? 0.0f : n;
+        s = s * __builtin_amdgcn_exp2f((m - base) * k) + os * __builtin_amdgcn_exp2f((om - base) * k);
+        m = n;
+    }
+};
+
+template <int BLOCK>
+__device__ __forceinline__ MaxSum block_max_sum(MaxSum a, float k, MaxSum *lds)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) a.merge(__shfl_xor(a.m, d), __shfl_xor(a.s, d), k);
+    if constexpr (BLOCK > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = lds[0];
+        for (int w = 1; w < BLOCK / 64; ++w) a.merge(lds[w].m, lds[w].s, k);
+    }
+    return a;
+}
+
+// ---- what one token adds to the policy loss ---------------------------------------------------
+struct Policy {
+    float k;                      // log2(e) / temperature
+    float it;                     // 1 / temperature
+    float low, high, kl;          // bounds of the ratio, factor of the KL term
+    const float *old_logp, *ref_logp, *advantages, *weights;
+};
+struct Terms {
+    float pg, kl, slope;          // slope: of pg + factor kl in logp
+    bool clipped;
+};
+__device__ __forceinline__ Terms policy_terms(float logp, int64_t r, const Policy &P)
+{
+    Terms t;
+    const float a = P.advantages[r], ratio = expf(logp - P.old_logp[r]);
+    const float plain = ratio * a, held = fminf(fmaxf(ratio, P.low), P.high) * a;
+    t.clipped = held < plain;     // NaN: the plain product, which then is one
+    t.pg = -(t.clipped ? held : plain);
+    t.slope = t.clipped ? 0.0f : -plain;
+    t.kl = 0.0f;
+    if (P.ref_logp) {
+        const float d = P.ref_logp[r] - logp, em1 = expm1f(d);      // exp(d) - 1 without cancellation: d is small in earnest
+        t.kl = em1 - d;
+        if (P.kl != 0.0f) t.slope += P.kl * -em1;
+    }
+    return t;
+}
+__device__ __forceinline__ float weight_of(const float *weights, int64_t r) { return weights ? weights[r] : 1.0f; }
+
+struct Logits {
+    const void *x;
+    int64_t stride;
+    const int64_t *targets;
+    int vocab;
+};
+__device__ __forceinline__ int target_of(const Logits &L, int64_t r)
+{
+    const int64_t t = L.targets[r];
+    return t >= 0 && t < L.vocab ? (int)t : -1;
+}
+
+// +0 over a row or a part of one
+template <typename E, int BLOCK>
+__device__ __forceinline__ void zero_row(typename E::T *out, int n)
+{
+    const Cut c = Cut::of<E::PER>(out, n, true);
+    u32x4 *v = reinterpret_cast<u32x4 *>(out + c.head);
+    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) v[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < c.singles; i += BLOCK) out[c.single<E::PER>(i)] = 0;
+}
+
+// Gradient over n elements of a row: d ([i = at] - exp2(k (z - m)) / s), where `at` may lie outside.  out may be in: every element
+// is read and written by the same lane.
+template <typename E, int BLOCK>
+__device__ __forceinline__ void grad_row(const typename E::T *in, typename E::T *out, int n, int at, float m, float s, float k, float d)
+{
+    const float f = d / s;
+    const bool same = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+    const Cut c = Cut::of<E::PER>(in, n, same);
+    const u32x4 *vi = reinterpret_cast<const u32x4 *>(in + c.head);
+    u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head);
+    auto power = [&](float z) { return __builtin_amdgcn_exp2f((z - m) * k); };
+    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) {
+        float raw[E::PER], z[E::PER];
+        E::widen(vi[i], raw);
+#pragma unroll
+        for (int e = 0; e < E::PER; ++e) z[e] = -f * power(raw[e]);
+        const int rel = at - c.head - i * E::PER;
+        if (rel >= 0 && rel < E::PER)
+#pragma unroll
+            for (int e = 0; e < E::PER; ++e) z[e] = e == rel ? d * (1.0f - power(raw[e]) / s) : z[e];
+        vo[i] = E::narrow(z);
+    }
+    for (int i = threadIdx.x; i < c.singles; i += BLOCK) {
+        const int e = c.single<E::PER>(i);
+        const float x = power(E::load(in + e));
+        E::store(out + e, e == at ? d * (1.0f - x / s) : -f * x);
+    }
+}
+
+// One workgroup a row: maximum and sum in one pass, then the token's log-probability and, with POLICY and somewhere to put it,
+// the gradient in a second pass over the row.
+template <typename E, int BLOCK, bool POLICY>
+__global__ __launch_bounds__(BLOCK) void k_rows(Logits L, int64_t row0, Policy P, float *logp, float *row_stats, void *dlogits, int64_t dstride)
+{
+    typedef typename E::T T;
+    __shared__ MaxSum lds[BLOCK / 64];
+    const int64_t r = row0 + blockIdx.x;
+    const int t = target_of(L, r);
+    const float w = POLICY ? weight_of(P.weights, r) : 1.0f;
+    T *out = POLICY && dlogits ? static_cast<T *>(dlogits) + r * dstride : nullptr;
+    if (t < 0 || w == 0.0f) {
+        if (threadIdx.x == 0) {
+            logp[r] = 0.0f;
+            if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
+        }
+        if (out) zero_row<E, BLOCK>(out, L.vocab);
+        return;
+    }
+    const T *row = static_cast<const T *>(L.x) + r * L.stride;
+    const float zt = E::load(row + t);
+    const Cut c = Cut::of<E::PER>(row, L.vocab, true);
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
+    MaxSum a = {-INFINITY, 0.0f};
+    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) {
+        float z[E::PER], m = -INFINITY, s = 0.0f;
+        E::widen(v[i], z);
+#pragma unroll
+        for (int e = 0; e < E::PER; ++e) m = fmaxf(m, z[e]);
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int e = 0; e < E::PER; ++e) s += __builtin_amdgcn_exp2f((z[e] - base) * P.k);
+        a.merge(m, s, P.k);
+    }
+    for (int i = threadIdx.x; i < c.singles; i += BLOCK) {
+        const float z = E::load(row + c.single<E::PER>(i));
+        a.merge(z, z == -INFINITY ? 0.0f : z != z ? z : 1.0f, P.k);
+    }
+    a = block_max_sum<BLOCK>(a, P.k, lds);
+    const float lp = (zt - a.m) * P.it - logf(a.s);
+    if (threadIdx.x == 0) {
+        logp[r] = lp;
+        if (row_stats) row_stats[2 * r] = a.m, row_stats[2 * r + 1] = a.s;
+    }
+    if constexpr (POLICY) {
+        if (!out) return;
+        const float d = w * policy_terms(lp, r, P).slope * P.it;
+        if (d == 0.0f) zero_row<E, BLOCK>(out, L.vocab);
+        else grad_row<E, BLOCK>(row, out, L.vocab, t, a.m, a.s, P.k, d);
+    }
+}
+
+// Gradient of rows whose maximum and sum are known: a workgroup takes GRAD_RUN elements of a row.
+constexpr int GRAD_BLOCK = 256;
+constexpr int GRAD_RUN = GRAD_BLOCK * 32;
+template <typename E>
+__global__ __launch_bounds__(GRAD_BLOCK) void k_grad(Logits L, int64_t row0, uint32_t runs, float k, float it, const float *row_stats, const float *dlogp,
+                                                     void *dlogits, int64_t dstride)
+{
+    typedef typename E::T T;
+    const uint32_t part = blockIdx.x / runs;
+    const int64_t r = row0 + part;
+    const int from = (int)(blockIdx.x - part * runs) * GRAD_RUN, n = min(GRAD_RUN, L.vocab - from);
+    const int t = target_of(L, r);
+    T *out = static_cast<T *>(dlogits) + r * dstride + from;
+    const float d = dlogp[r] * it;
+    if (t < 0 || d == 0.0f) return zero_row<E, GRAD_BLOCK>(out, n);
+    const T *row = static_cast<const T *>(L.x) + r * L.stride + from;
+    const int at = t >= from && t < from + n ? t - from : -1;
+    grad_row<E, GRAD_BLOCK>(row, out, n, at, row_stats[2 * r], row_stats[2 * r + 1], k, d);
+}
+
+// ---- sums over tokens -------------------------------------------------------------------------
+// Workgroups leave N sums each, one workgroup folds them in a fixed order; a single one finishes by itself.
+constexpr int SUM_BLOCK = 256;
+constexpr int SUM_MAX_BLOCKS = 512;
+template <int N, int BLOCK>
+__device__ __forceinline__ void finish_sums(const double (&x)[N], double *partials, float *out, int accumulate, bool last)
+{
+    __shared__ double lds[N][BLOCK / 64];
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const double t = block_sum<BLOCK>(x[q], lds[q]);
+        if (threadIdx.x == 0) {
+            if (last) out[q] = (float)((accumulate ? (double)out[q] : 0.0) + t);
+            else partials[(int64_t)blockIdx.x * N + q] = t;
+        }
+    }
+}
+template <int N>
+__global__ __launch_bounds__(SUM_BLOCK) void k_fold_sums(const double *partials, int count, float *out, int accumulate)
+{
+    double x[N] = {};
+    for (int i = threadIdx.x; i < count; i += SUM_BLOCK)
+#pragma unroll
+        for (int q = 0; q < N; ++q) x[q] += partials[(int64_t)i * N + q];
+    finish_sums<N, SUM_BLOCK>(x, nullptr, out, accumulate, true);
+}
+
+__global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *targets, int vocab, int64_t rows, Policy P, const float *logp, double *partials,
+                                                           float *out, int accumulate)
+{
+    double x[4] = {};
+    for (int64_t r = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; r < rows; r += (int64_t)gridDim.x * SUM_BLOCK) {
+        const float w = weight_of(P.weights, r);
+        const int64_t t = targets[r];
+        if (t < 0 || t >= vocab || w == 0.0f) continue;
+        const Terms e = policy_terms(logp[r], r, P);
+        const double pg = (double)w * e.pg, kl = (double)w * e.kl;
+        x[0] += P.kl != 0.0f ? pg + P.kl * kl : pg;
+        x[1] += pg;
+        x[2] += kl;
+        x[3] += e.clipped ? (double)w : 0.0;
+    }
+    finish_sums<4, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
+}
+
+// ---- preference loss --------------------------------------------------------------------------
+constexpr int PAIR_BLOCK = 512;
+struct Pairs {
+    const float *logp, *ref_logp, *weights;
+    const int64_t *offsets;
+    int64_t tokens, pairs;
+    float beta, smoothing, scale;
+    float *margins, *dlogp;
+};
+__device__ __forceinline__ int64_t offset_of(const Pairs &A, int64_t s)
+{
+    const int64_t o = A.offsets[s];
+    return o < 0 ? 0 : o > A.tokens ? A.tokens : o;
+}
+__device__ __forceinline__ double log_ratio_sum(const Pairs &A, int64_t from, int64_t to)
+{
+    double x = 0.0;
+    for (int64_t i = from + threadIdx.x; i < to; i += PAIR_BLOCK) {
+        const float w = weight_of(A.weights, i);
+        if (w != 0.0f) x += (double)w * ((double)A.logp[i] - (A.ref_logp ? (double)A.ref_logp[i] : 0.0));
+    }
+    return x;
+}
+__device__ __forceinline__ void spread(const Pairs &A, int64_t from, int64_t to, float d)
+{
+    for (int64_t i = from + threadIdx.x; i < to; i += PAIR_BLOCK) {
+        const float w = weight_of(A.weights, i);
+        A.dlogp[i] = w != 0.0f ? d * w : 0.0f;
+    }
+}
+// ln(1 + exp(x))
+__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+
+// One workgroup a pair.  Both sums are held in 64 bits: a margin is a small difference of sums over thousands of tokens.
+__global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
+{
+    __shared__ double lds[2][PAIR_BLOCK / 64];
+    __shared__ float slope;
+    const int64_t p = blockIdx.x, q = A.pairs + p;
+    const int64_t a0 = offset_of(A, p), a1 = offset_of(A, p + 1), b0 = offset_of(A, q), b1 = offset_of(A, q + 1);
+    const double chosen = block_sum<PAIR_BLOCK>(log_ratio_sum(A, a0, a1), lds[0]);
+    const double rejected = block_sum<PAIR_BLOCK>(log_ratio_sum(A, b0, b1), lds[1]);
+    if (threadIdx.x == 0) {
+        const double h = (double)A.beta * (chosen - rejected), e = A.smoothing;
+        const double up = 1.0 / (1.0 + exp(-h)), down = 1.0 / (1.0 + exp(h));       // sigmoid(h), sigmoid(-h)
+        A.margins[p] = (float)h;
+        slope = (float)((double)A.scale * A.beta * (e * up - (1.0 - e) * down));
+    }
+    __syncthreads();
+    spread(A, a0, a1, slope);
+    spread(A, b0, b1, -slope);
+    if (p == 0) spread(A, 0, offset_of(A, 0), 0.0f);
+    if (q + 1 == 2 * A.pairs) spread(A, b1, A.tokens, 0.0f);
+}
+// The loss from the margins, which are fp32: its relative error from that is at most that of a margin.
+__global__ __launch_bounds__(SUM_BLOCK) void k_pair_sums(const float *margins, int64_t pairs, float smoothing, float scale, double *partials, float *out, int accumulate)
+{
+    double x[1] = {};
+    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) {
+        const double h = margins[p], e = smoothing;
+        x[0] += (double)scale * ((1.0 - e) * softplus(-h) + (e != 0.0 ? e * softplus(h) : 0.0));
+    }
+    finish_sums<1, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
+}
+__global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; i < n; i += (int64_t)gridDim.x * SUM_BLOCK) p[i] = 0.0f;
+}
+
+// ---- launchers --------------------------------------------------------------------------------
+static int sum_blocks(int64_t n)
+{
+    const int64_t b = (n + 4 * SUM_BLOCK - 1) / (4 * SUM_BLOCK);
+    return (int)(b < 1 ? 1 : b > SUM_MAX_BLOCKS ? SUM_MAX_BLOCKS : b);
+}
+
+constexpr int ROW_BLOCK = 256;
+static constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
+
+template <bool POLICY>
+static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride,
+                              hipStream_t stream)
+{
+    const int64_t most = kMaxItems / ROW_BLOCK;
+    for (int64_t r = 0; r < X.rows; r += most) {
+        const int grid = (int)(X.rows - r < most ? X.rows - r : most);
+        if (X.dtype == GS_BF16) k_rows<Bf16, ROW_BLOCK, POLICY><<<grid, ROW_BLOCK, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
+        else k_rows<F32, ROW_BLOCK, POLICY><<<grid, ROW_BLOCK, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// ---- checks -----------------------------------------------------------------------------------
+struct Span {
+    uintptr_t lo, hi;
+    bool out;
+};
+static Span span_of(const void *p, int64_t bytes, bool out)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, p ? a + (uintptr_t)bytes : a, out};
+}
+// no output overlaps another array; spans `a` and `b` may, where `skip` says so (an output that is its own input)
+static bool apart(const Span *s, int n, bool skip = false, int a = -1, int b = -1)
+{
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n; ++j)
+            if ((s[i].out || s[j].out) && !(skip && i == a && j == b) && s[i].lo < s[j].hi && s[j].lo < s[i].hi) return false;
+    return true;
+}
+static bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+static bool good(const void *p, uintptr_t to) { return p && aligned(p, to); }
+static int64_t size_of(int32_t dtype) { return dtype == GS_BF16 ? 2 : 4; }
+
+// bytes from a matrix's first element to behind its last one; -1 if they do not fit an address
+static int64_t extent(int64_t rows, int64_t cols, int64_t stride, int64_t size)
+{
+    int64_t n;
+    if (rows > 1 && (__builtin_mul_overflow(rows - 1, stride, &n) || __builtin_add_overflow(n, cols, &n) || __builtin_mul_overflow(n, size, &n))) return -1;
+    return rows > 1 ? n : rows * cols * size;
+}
+static bool good_matrix(const gs_logits *x)
+{
+    if (!x || (x->dtype != GS_BF16 && x->dtype != GS_F32)) return false;
+    if (x->rows < 0 || x->vocab < 1 || x->vocab > (int64_t)1 << 30) return false;
+    if (x->rows > (int64_t)1 << 40 || (x->rows > 1 && x->row_stride < x->vocab)) return false;
+    if (extent(x->rows, x->vocab, x->row_stride, size_of(x->dtype)) < 0) return false;
+    return x->rows == 0 || good(x->data, size_of(x->dtype));
+}
+static bool good_output(const gs_logits &x, const void *out, int64_t stride)
+{
+    if (x.rows > 1 && stride < x.vocab) return false;
+    return good(out, size_of(x.dtype)) && extent(x.rows, x.vocab, stride, size_of(x.dtype)) >= 0;
+}
+static bool good_temperature(float t) { return t >= 1e-4f && t <= 1e4f; }
+static bool finite_from(float x, float lo) { return std::isfinite(x) && x >= lo; }
+static bool good_workspace(const void *ws, size_t bytes) { return ws && bytes >= gs_sqnorm_workspace_bytes() && aligned(ws, 8); }
+
+static Logits logits_of(const gs_logits &x, const int64_t *targets)
+{
+    return {x.data, x.rows > 1 ? x.row_stride : x.vocab, targets, (int)x.vocab};
+}
+static Policy scaled_by(float temperature)
+{
+    Policy P = {};
+    P.it = 1.0f / temperature;
+    P.k = kLog2e / temperature;
+    return P;
+}
+
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float temperature, float *logp, float *row_stats,
+                        void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (!good_matrix(logits) || !good_temperature(temperature)) return GS_ERR_INVALID_ARG;
+    const int64_t rows = logits->rows;
+    if (rows && (!good(targets, 8) || !good(logp, 4) || !aligned(row_stats, 4))) return GS_ERR_INVALID_ARG;
+    if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
+    if (rows == 0) return GS_OK;
+    const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size_of(logits->dtype)), false),
+                      span_of(targets, rows * 8, false), span_of(logp, rows * 4, true), span_of(row_stats, rows * 8, true),
+                      span_of(d_workspace, (int64_t)workspace_bytes, true)};
+    if (!apart(s, 5)) return GS_ERR_INVALID_ARG;
+    hipError_t e = launch_rows<false>(*logits, logits_of(*logits, targets), scaled_by(temperature), logp, row_stats, nullptr, 0,
+                                      static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? GS_OK : hip_fail(e, "gs_token_logp launch");
+}
+
+gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, float temperature, const float *row_stats,
+                             const float *dlogp, void *dlogits, int64_t dlogits_stride, void *stream)
+{
+    if (!good_matrix(logits) || !good_temperature(temperature)) return GS_ERR_INVALID_ARG;
+    const int64_t rows = logits->rows, size = size_of(logits->dtype);
+    if (rows == 0) return GS_OK;
+    if (!good(targets, 8) || !good(row_stats, 4) || !good(dlogp, 4) || !good_output(*logits, dlogits, dlogits_stride)) return GS_ERR_INVALID_ARG;
+    const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
+    const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
+                      span_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), span_of(targets, rows * 8, false),
+                      span_of(row_stats, rows * 8, false), span_of(dlogp, rows * 4, false)};
+    if (!apart(s, 5, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
+    const Logits L = logits_of(*logits, targets);
+    const Policy P = scaled_by(temperature);
+    const uint32_t runs = (uint32_t)((logits->vocab + GRAD_RUN - 1) / GRAD_RUN);
+    const int64_t most = kMaxItems / GRAD_BLOCK / runs;           // at least 127 rows
+    const int64_t dstride = rows > 1 ? dlogits_stride : logits->vocab;
+    for (int64_t r = 0; r < rows; r += most) {
+        const uint32_t grid = (uint32_t)(rows - r < most ? rows - r : most) * runs;
+        if (logits->dtype == GS_BF16)
+            k_grad<Bf16><<<grid, GRAD_BLOCK, 0, static_cast<hipStream_t>(stream)>>>(L, r, runs, P.k, P.it, row_stats, dlogp, dlogits, dstride);
+        else
+            k_grad<F32><<<grid, GRAD_BLOCK, 0, static_cast<hipStream_t>(stream)>>>(L, r, runs, P.k, P.it, row_stats, dlogp, dlogits, dstride);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_fail(e, "gs_token_logp_grad launch");
+    }
+    return GS_OK;
+}
+
+gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const gs_policy_hparams *hp, const float *old_logp,
+                         const float *ref_logp, const float *advantages, const float *weights, float *logp, void *dlogits,
+                         int64_t dlogits_stride, float *d_stats, int accumulate, void *d_workspace, size_t workspace_bytes,
+                         void *stream)
+{
+    if (!good_matrix(logits) || !hp || !good_temperature(hp->temperature)) return GS_ERR_INVALID_ARG;
+    if (!finite_from(hp->clip_low, 0.0f) || hp->clip_low > 1.0f || !finite_from(hp->clip_high, 0.0f) || !finite_from(hp->kl_coef, 0.0f))
+        return GS_ERR_INVALID_ARG;
+    const int64_t rows = logits->rows, size = size_of(logits->dtype);
+    if (!good(d_stats, 4)) return GS_ERR_INVALID_ARG;
+    if (rows) {
+        if (!good(targets, 8) || !good(old_logp, 4) || !good(advantages, 4) || !aligned(ref_logp, 4) || !aligned(weights, 4) || !good(logp, 4))
+            return GS_ERR_INVALID_ARG;
+        if (dlogits && !good_output(*logits, dlogits, dlogits_stride)) return GS_ERR_INVALID_ARG;
+    }
+    if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
+    if (rows == 0 && accumulate) return GS_OK;
+    if (rows) {
+        const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
+        const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
+                          span_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), span_of(targets, rows * 8, false),
+                          span_of(old_logp, rows * 4, false), span_of(ref_logp, rows * 4, false), span_of(advantages, rows * 4, false),
+                          span_of(weights, rows * 4, false), span_of(logp, rows * 4, true), span_of(d_stats, 16, true),
+                          span_of(d_workspace, (int64_t)workspace_bytes, true)};
+        if (!apart(s, 10, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    Policy P = scaled_by(hp->temperature);
+    P.low = 1.0f - hp->clip_low;
+    P.high = 1.0f + hp->clip_high;
+    P.kl = hp->kl_coef;
+    P.old_logp = old_logp;
+    P.ref_logp = ref_logp;
+    P.advantages = advantages;
+    P.weights = weights;
+    hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, st);
+    if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
+    const int blocks = sum_blocks(rows);
+    double *partials = static_cast<double *>(d_workspace);
+    k_policy_sums<<<blocks, SUM_BLOCK, 0, st>>>(targets, (int)logits->vocab, rows, P, logp, partials, d_stats, accumulate);
+    if (blocks > 1) k_fold_sums<4><<<1, SUM_BLOCK, 0, st>>>(partials, blocks, d_stats, accumulate);
+    e = hipGetLastError();
+    return e == hipSuccess ? GS_OK : hip_fail(e, "gs_policy_loss launch");
+}
+
+gs_status gs_preference_loss(const float *logp, const float *ref_logp, const float *weights, int64_t tokens,
+                             const int64_t *offsets, int64_t pairs, const gs_preference_hparams *hp, float *margins, float *dlogp,
+                             float *d_loss, int accumulate, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (!hp || !std::isfinite(hp->beta) || !(hp->beta > 0.0f) || !finite_from(hp->label_smoothing, 0.0f) || hp->label_smoothing >= 1.0f ||
+        !std::isfinite(hp->scale))
+        return GS_ERR_INVALID_ARG;
+    if (tokens < 0 || tokens > (int64_t)1 << 40 || pairs < 0 || pairs > kMaxItems / PAIR_BLOCK) return GS_ERR_INVALID_ARG;
+    if (tokens && (!good(logp, 4) || !good(dlogp, 4) || !aligned(ref_logp, 4) || !aligned(weights, 4))) return GS_ERR_INVALID_ARG;
+    if (pairs && (!good(offsets, 8) || !good(margins, 4))) return GS_ERR_INVALID_ARG;
+    if (!good(d_loss, 4)) return GS_ERR_INVALID_ARG;
+    if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
+    const Span s[] = {span_of(logp, tokens * 4, false), span_of(ref_logp, tokens * 4, false), span_of(weights, tokens * 4, false),
+                      span_of(offsets, pairs ? (2 * pairs + 1) * 8 : 0, false), span_of(margins, pairs * 4, true), span_of(dlogp, tokens * 4, true),
+                      span_of(d_loss, 4, true), span_of(d_workspace, (int64_t)workspace_bytes, true)};
+    if (!apart(s, 8)) return GS_ERR_INVALID_ARG;
+    if (pairs == 0 && tokens == 0 && accumulate) return GS_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (pairs) {
+        const Pairs A = {logp, ref_logp, weights, offsets, tokens, pairs, hp->beta, hp->label_smoothing, hp->scale, margins, dlogp};
+        k_pairs<<<(int)pairs, PAIR_BLOCK, 0, st>>>(A);
+    } else if (tokens) {
+        k_zero<<<sum_blocks(tokens), SUM_BLOCK, 0, st>>>(dlogp, tokens);
+    }
+    if (!(pairs == 0 && accumulate)) {
+        const int blocks = sum_blocks(pairs);
+        double *partials = static_cast<double *>(d_workspace);
+        k_pair_sums<<<blocks, SUM_BLOCK, 0, st>>>(margins, pairs, hp->label_smoothing, hp->scale, partials, d_loss, accumulate);
+        if (blocks > 1) k_fold_sums<1><<<1, SUM_BLOCK, 0, st>>>(partials, blocks, d_loss, accumulate);
+    }
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? GS_OK : hip_fail(e, "gs_preference_loss launch");
+}
+
+}  // extern "C"

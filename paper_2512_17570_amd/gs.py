@@ -30,6 +30,9 @@ GS_ERR_IO = -5
 GS_ERR_TOO_LARGE = -6
 GS_NOALLOC_MAX_ELEMS = 1 << 33
 GS_MAX_K = 32
+GS_BF16 = 0
+GS_F32 = 1
+GS_MAX_TENSORS = 65536
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -80,6 +83,45 @@ class HParams:
                                 self.max_grad_norm, self.step)
 
 
+class gs_policy_hparams(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float),
+                ("kl_coef", ctypes.c_float)]
+
+
+@dataclass
+class PolicyHParams:
+    temperature: float = 1.0
+    clip_low: float = 0.2
+    clip_high: float = 0.2
+    kl_coef: float = 0.0
+
+    def c_struct(self) -> gs_policy_hparams:
+        return gs_policy_hparams(self.temperature, self.clip_low, self.clip_high, self.kl_coef)
+
+
+class gs_preference_hparams(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_float), ("label_smoothing", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+@dataclass
+class PreferenceHParams:
+    beta: float = 0.1
+    label_smoothing: float = 0.0
+    scale: float = 1.0
+
+    def c_struct(self) -> gs_preference_hparams:
+        return gs_preference_hparams(self.beta, self.label_smoothing, self.scale)
+
+
+class gs_logits(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+class gs_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _pp = ctypes.c_void_p      # a table of addresses, as bytes
@@ -127,6 +169,20 @@ _lib.gs_stream_ctx_sync.restype = ctypes.c_int
 _lib.gs_stream_layer_step.argtypes = [_vp, _vp, _vp, _vp, _vp, _pp, ctypes.c_int, _i64,
                                       ctypes.POINTER(gs_adamw_hparams), _vp, _vp]
 _lib.gs_stream_layer_step.restype = ctypes.c_int
+_lib.gs_token_logp.argtypes = [ctypes.POINTER(gs_logits), _vp, ctypes.c_float, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.gs_token_logp.restype = ctypes.c_int
+_lib.gs_token_logp_grad.argtypes = [ctypes.POINTER(gs_logits), _vp, ctypes.c_float, _vp, _vp, _vp, _i64, _vp]
+_lib.gs_token_logp_grad.restype = ctypes.c_int
+_lib.gs_policy_loss.argtypes = [ctypes.POINTER(gs_logits), _vp, ctypes.POINTER(gs_policy_hparams), _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp,
+                                ctypes.c_int, _vp, ctypes.c_size_t, _vp]
+_lib.gs_policy_loss.restype = ctypes.c_int
+_lib.gs_preference_loss.argtypes = [_vp, _vp, _vp, _i64, _vp, _i64, ctypes.POINTER(gs_preference_hparams), _vp, _vp, _vp, ctypes.c_int,
+                                    _vp, ctypes.c_size_t, _vp]
+_lib.gs_preference_loss.restype = ctypes.c_int
+_lib.gs_grads_sqnorm.argtypes = [_vp, _i64, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp]
+_lib.gs_grads_sqnorm.restype = ctypes.c_int
+_lib.gs_grads_clip.argtypes = [_vp, _i64, _vp, ctypes.c_float, _vp, _vp]
+_lib.gs_grads_clip.restype = ctypes.c_int
 _lib.gs_pinned_alloc.argtypes = [ctypes.c_size_t]
 _lib.gs_pinned_alloc.restype = _vp
 _lib.gs_pinned_free.argtypes = [_vp]
@@ -217,10 +273,15 @@ _call.setup(*[ctypes.cast(getattr(_lib, name), _vp).value for name in (
     "gs_adamw_from_acc", "gs_accum_adamw_oop", "gs_accum_adamw_spec")], HParams, _in_bad_fork)
 
 
+_call.setup_loss(*[ctypes.cast(getattr(_lib, name), _vp).value for name in (
+    "gs_token_logp", "gs_token_logp_grad", "gs_policy_loss", "gs_preference_loss", "gs_grads_sqnorm", "gs_grads_clip")],
+    PolicyHParams, PreferenceHParams)
+
+
 def _hp(hp):
     if hp is None:
         return None
-    return ctypes.byref(hp.c_struct() if isinstance(hp, HParams) else hp)
+    return ctypes.byref(hp.c_struct() if isinstance(hp, (HParams, PolicyHParams, PreferenceHParams)) else hp)
 
 
 def _check(status: int, where: str, check: bool) -> int:
@@ -386,6 +447,159 @@ def gs_accum_adamw_spec(p, m, v, p_out, m_out, v_out, w_bf16, grads, begin: int,
 
 def gs_clip_coefficient(sqnorm_total: float, max_grad_norm: float) -> float:
     return float(_lib.gs_clip_coefficient(float(sqnorm_total), float(max_grad_norm)))
+
+
+# ---- losses on rows of logits; norm and clip over many tensors ----------------------------------------
+
+_DTYPES = {torch.bfloat16: GS_BF16, torch.float32: GS_F32}
+
+
+def _gpu(x, count: int, dtype, name: str, optional: bool = False) -> int | None:
+    """Address of a contiguous GPU tensor of `dtype` with at least `count` elements (raw addresses are taken as they are)."""
+    if not isinstance(x, torch.Tensor):
+        if x is None and not optional:
+            raise TypeError(f"{name}: a tensor is needed")
+        return _addr(x)
+    if x.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if x.numel() < count:
+        raise ValueError(f"{name}: holds {x.numel()} elements, {count} are needed")
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    return x.data_ptr()
+
+
+def _matrix(x, name: str = "logits") -> gs_logits:
+    """Rows of logits: a 2-D GPU tensor whose rows are contiguous, at any distance from each other, or a gs_logits."""
+    if isinstance(x, gs_logits):
+        return x
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is needed")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"{name}: expected bfloat16 or float32, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if x.dim() != 2 or (x.size(1) > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: a 2-D tensor with contiguous rows is needed")
+    return gs_logits(x.data_ptr(), x.size(0), x.size(1), x.stride(0), _DTYPES[x.dtype])
+
+
+def _like(x, like: gs_logits, name: str):
+    """(address, row stride) of a matrix of the type and shape of `like`."""
+    m = _matrix(x, name)
+    if (m.rows, m.vocab, m.dtype) != (like.rows, like.vocab, like.dtype):
+        raise ValueError(f"{name}: needs the logits' shape and type")
+    return m.data, m.row_stride
+
+
+def _workspace_bytes(d_workspace, given):
+    if given is not None:
+        return given
+    return d_workspace.numel() * d_workspace.element_size() if hasattr(d_workspace, "numel") else 0
+
+
+def gs_token_logp(logits, targets, logp, row_stats=None, temperature: float = 1.0, d_workspace=None,
+                  workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
+    st = _call.token_logp(logits, targets, logp, row_stats, temperature, d_workspace, workspace_bytes, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_token_logp", check)
+    x = _matrix(logits)
+    st = _lib.gs_token_logp(ctypes.byref(x), _gpu(targets, x.rows, torch.int64, "targets"), temperature,
+                            _gpu(logp, x.rows, torch.float32, "logp"), _gpu(row_stats, 2 * x.rows, torch.float32, "row_stats", True),
+                            _addr(d_workspace), _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_token_logp", check)
+
+
+def gs_token_logp_grad(logits, targets, row_stats, dlogp, dlogits, temperature: float = 1.0, stream=None,
+                       check: bool = True) -> int:
+    st = _call.token_logp_grad(logits, targets, row_stats, dlogp, dlogits, temperature, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_token_logp_grad", check)
+    x = _matrix(logits)
+    out, stride = _like(dlogits, x, "dlogits")
+    st = _lib.gs_token_logp_grad(ctypes.byref(x), _gpu(targets, x.rows, torch.int64, "targets"), temperature,
+                                 _gpu(row_stats, 2 * x.rows, torch.float32, "row_stats"),
+                                 _gpu(dlogp, x.rows, torch.float32, "dlogp"), out, stride, _stream(stream))
+    return _check(st, "gs_token_logp_grad", check)
+
+
+def gs_policy_loss(logits, targets, old_logp, ref_logp, advantages, weights, hp, logp, dlogits, d_stats, d_workspace,
+                   workspace_bytes: int | None = None, accumulate: bool = False, stream=None, check: bool = True) -> int:
+    st = _call.policy_loss(logits, targets, old_logp, ref_logp, advantages, weights, hp, logp, dlogits, d_stats, d_workspace,
+                           workspace_bytes, accumulate, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_policy_loss", check)
+    x = _matrix(logits)
+    out, stride = (None, 0) if dlogits is None else _like(dlogits, x, "dlogits")
+    f32 = lambda t, name, optional=False: _gpu(t, x.rows, torch.float32, name, optional)  # noqa: E731
+    st = _lib.gs_policy_loss(ctypes.byref(x), _gpu(targets, x.rows, torch.int64, "targets"), _hp(hp), f32(old_logp, "old_logp"),
+                             f32(ref_logp, "ref_logp", True), f32(advantages, "advantages"), f32(weights, "weights", True),
+                             f32(logp, "logp"), out, stride, _gpu(d_stats, 4, torch.float32, "d_stats"), int(bool(accumulate)),
+                             _addr(d_workspace), _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_policy_loss", check)
+
+
+def gs_preference_loss(logp, ref_logp, weights, offsets, hp, margins, dlogp, d_loss, d_workspace,
+                       workspace_bytes: int | None = None, accumulate: bool = False, stream=None, check: bool = True) -> int:
+    """The pairs are counted by `margins`, the tokens by `logp`."""
+    st = _call.preference_loss(logp, ref_logp, weights, offsets, hp, margins, dlogp, d_loss, d_workspace, workspace_bytes,
+                               accumulate, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_preference_loss", check)
+    tokens, pairs = logp.numel(), margins.numel()
+    f32 = lambda t, name, optional=False: _gpu(t, tokens, torch.float32, name, optional)  # noqa: E731
+    st = _lib.gs_preference_loss(f32(logp, "logp"), f32(ref_logp, "ref_logp", True), f32(weights, "weights", True), tokens,
+                                 _gpu(offsets, 2 * pairs + 1, torch.int64, "offsets"), pairs, _hp(hp),
+                                 _gpu(margins, pairs, torch.float32, "margins"), f32(dlogp, "dlogp"),
+                                 _gpu(d_loss, 1, torch.float32, "d_loss"), int(bool(accumulate)), _addr(d_workspace),
+                                 _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_preference_loss", check)
+
+
+def _tensors(tensors, outs=None):
+    """The library's list of contiguous GPU tensors (and their outputs, of the same types and sizes)."""
+    if isinstance(tensors, torch.Tensor):
+        raise TypeError("tensors: a list of tensors is needed")
+    tensors = list(tensors)
+    outs = [None] * len(tensors) if outs is None else list(outs)
+    if len(outs) != len(tensors):
+        raise ValueError(f"outs: {len(outs)} tensors for {len(tensors)}")
+    table = (gs_tensor * max(1, len(tensors)))()
+    for i, (t, o) in enumerate(zip(tensors, outs)):
+        if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
+            raise TypeError(f"tensors[{i}]: a bfloat16 or float32 tensor is needed")
+        data = _gpu(t, t.numel(), t.dtype, f"tensors[{i}]")
+        out = None
+        if o is not None:
+            if o.numel() != t.numel():
+                raise ValueError(f"outs[{i}]: holds {o.numel()} elements, {t.numel()} are needed")
+            out = _gpu(o, t.numel(), t.dtype, f"outs[{i}]")
+        table[i] = gs_tensor(data, out, t.numel(), _DTYPES[t.dtype])
+    return table, len(tensors)
+
+
+def gs_grads_sqnorm(tensors, d_sqnorm, d_workspace, workspace_bytes: int | None = None, accumulate: bool = False,
+                    stream=None, check: bool = True) -> int:
+    st = _call.grads_sqnorm(tensors, d_sqnorm, d_workspace, workspace_bytes, accumulate, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_grads_sqnorm", check)
+    table, count = _tensors(tensors)
+    st = _lib.gs_grads_sqnorm(table, count, _gpu(d_sqnorm, 1, torch.float64, "d_sqnorm"), int(bool(accumulate)), _addr(d_workspace),
+                              _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_grads_sqnorm", check)
+
+
+def gs_grads_clip(tensors, d_sqnorm, max_norm: float, d_norm=None, outs=None, stream=None, check: bool = True) -> int:
+    """In place, or into `outs`, one for each tensor."""
+    st = _call.grads_clip(tensors, d_sqnorm, max_norm, d_norm, outs, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_grads_clip", check)
+    table, count = _tensors(tensors, outs)
+    st = _lib.gs_grads_clip(table, count, _gpu(d_sqnorm, 1, torch.float64, "d_sqnorm"), max_norm,
+                            _gpu(d_norm, 1, torch.float32, "d_norm", True), _stream(stream))
+    return _check(st, "gs_grads_clip", check)
 
 
 def gs_cu_stream_create(num_cus: int, check: bool = True):
