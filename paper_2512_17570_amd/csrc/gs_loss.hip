@@ -18,6 +18,8 @@ namespace gs {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -25,6 +27,28 @@ constexpr float kLog2e = 1.44269504088896340736f;
 struct Bf16 {
     typedef uint16_t T;
     static constexpr int PER = 8;
+    static constexpr uint32_t LOWEST = 0xff80ff80u;   // -inf, twice
+    // Maximum so far, two elements at a time as whole numbers.  Positive values are ordered as signed numbers, and lie above
+    // negative ones; negative ones are ordered the other way round, which as unsigned numbers makes the largest the least.  One
+    // operation an element where unpacked floats take one and a half.  NaN: either sign may be lost, the sum is NaN all the same.
+    struct Max {
+        i16x2 up = {-32768, -32768};
+        u16x2 down = {65535, 65535};
+        __device__ __forceinline__ void add(u32x4 q)
+        {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                up = __builtin_elementwise_max(up, __builtin_bit_cast(i16x2, (uint32_t)q[i]));
+                down = __builtin_elementwise_min(down, __builtin_bit_cast(u16x2, (uint32_t)q[i]));
+            }
+        }
+        __device__ __forceinline__ float get() const
+        {
+            const int u = up[0] > up[1] ? up[0] : up[1];
+            const uint32_t d = down[0] < down[1] ? down[0] : down[1];
+            return __uint_as_float((u >= 0 ? (uint32_t)u : d) << 16);
+        }
+    };
     static __device__ __forceinline__ float load(const T *p) { return __uint_as_float((uint32_t)*p << 16); }
     static __device__ __forceinline__ void store(T *p, float f) { *p = (T)f32_to_bf16_bits(f); }
     static __device__ __forceinline__ void widen(u32x4 q, float (&z)[PER])
@@ -46,6 +70,17 @@ struct Bf16 {
 struct F32 {
     typedef float T;
     static constexpr int PER = 4;
+    static constexpr uint32_t LOWEST = 0xff800000u;
+    struct Max {
+        float m = -INFINITY;
+        __device__ __forceinline__ void add(u32x4 q)
+        {
+            // fmaxf would first make each element a quiet number
+            asm("v_max3_f32 %0, %1, %2, %0" : "+v"(m) : "v"(q[0]), "v"(q[1]));
+            asm("v_max3_f32 %0, %1, %2, %0" : "+v"(m) : "v"(q[2]), "v"(q[3]));
+        }
+        __device__ __forceinline__ float get() const { return m; }
+    };
     static __device__ __forceinline__ float load(const T *p) { return *p; }
     static __device__ __forceinline__ void store(T *p, float f) { *p = f; }
     static __device__ __forceinline__ void widen(u32x4 q, float (&z)[PER])
@@ -234,6 +269,131 @@ __global__ __launch_bounds__(BLOCK) void k_rows(Logits L, int64_t row0, Policy P
     }
 }
 
+// ---- rows held in registers -------------------------------------------------------------------
+// One workgroup a row, as before, but the row is read once: its lanes keep NV vectors each, from the first maximum to the
+// gradient.  The first LO vectors of a lane lie in the row whatever its length; the rest may not, and are -inf.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float from_dpp(float x, float none)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <bool MAX>
+__device__ __forceinline__ float join(float x, float y)
+{
+    if constexpr (MAX) return fmaxf(x, y);
+    else return x + y;
+}
+template <bool MAX>
+__device__ __forceinline__ float row_join(float x)
+{
+    x = join<MAX>(x, from_dpp<0xb1>(x, x));
+    x = join<MAX>(x, from_dpp<0x4e>(x, x));
+    x = join<MAX>(x, from_dpp<0x141>(x, x));
+    return join<MAX>(x, from_dpp<0x140>(x, x));
+}
+template <bool MAX, int BLOCK>
+__device__ __forceinline__ float block_join(float x, float *lds)
+{
+    constexpr float none = MAX ? -INFINITY : 0.0f;
+    x = row_join<MAX>(x);
+    x = join<MAX>(x, from_dpp<0x142, 0xa>(x, none));
+    x = join<MAX>(x, from_dpp<0x143, 0xc>(x, none));
+    x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+    if constexpr (BLOCK > 64) {
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = row_join<MAX>(lane < BLOCK / 64 ? lds[lane] : none);
+        x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 0));
+    }
+    return x;
+}
+
+template <typename E, int BLOCK, int NV, int LO, bool POLICY>
+__global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, Policy P, float *logp, float *row_stats, void *dlogits, int64_t dstride)
+{
+    typedef typename E::T T;
+    constexpr int PER = E::PER;
+    __shared__ float lds[2][BLOCK / 64];
+    const int64_t r = row0 + blockIdx.x;
+    const int t = target_of(L, r);
+    const float w = POLICY ? weight_of(P.weights, r) : 1.0f;
+    T *out = POLICY && dlogits ? static_cast<T *>(dlogits) + r * dstride : nullptr;
+    if (t < 0 || w == 0.0f) {
+        if (threadIdx.x == 0) {
+            logp[r] = 0.0f;
+            if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
+        }
+        if (out) zero_row<E, BLOCK>(out, L.vocab);
+        return;
+    }
+    const T *row = static_cast<const T *>(L.x) + r * L.stride;
+    const Cut c = Cut::of<PER>(row, L.vocab, true);
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
+    const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
+    u32x4 q[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = j * BLOCK + threadIdx.x;
+        if (j < LO) {
+            q[j] = __builtin_nontemporal_load(v + j * BLOCK + threadIdx.x);
+        } else {
+            q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
+            if (i < c.vecs) q[j] = __builtin_nontemporal_load(v + j * BLOCK + threadIdx.x);
+        }
+    }
+    const int single = (int)threadIdx.x < c.singles ? c.single<PER>(threadIdx.x) : -1;
+    const float zs = single >= 0 ? E::load(row + single) : -INFINITY;
+    const float zt = E::load(row + t);
+    auto used = [&](int j) { return j < LO || j * BLOCK + wave0 < c.vecs; };      // by any lane of the wave
+
+    typename E::Max most;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) most.add(q[j]);
+    const float m = block_join<true, BLOCK>(fmaxf(most.get(), zs), lds[0]);
+    auto power = [&](float z) { return __builtin_amdgcn_exp2f((z - m) * P.k); };
+    float sum[4] = {power(zs), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (used(j)) {
+            float z[PER];
+            E::widen(q[j], z);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) sum[e & 3] += power(z[e]);
+        }
+    const float s = block_join<false, BLOCK>((sum[0] + sum[1]) + (sum[2] + sum[3]), lds[1]);
+    const float lp = (zt - m) * P.it - logf(s);
+    if (threadIdx.x == 0) {
+        logp[r] = lp;
+        if (row_stats) row_stats[2 * r] = m, row_stats[2 * r + 1] = s;
+    }
+    if constexpr (POLICY) {
+        if (!out) return;
+        const float d = w * policy_terms(lp, r, P).slope * P.it;
+        if (d == 0.0f) return zero_row<E, BLOCK>(out, L.vocab);
+        if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0)      // no vectors in common: the row is read again
+            return grad_row<E, BLOCK>(row, out, L.vocab, t, m, s, P.k, d);
+        const float f = -d / s;
+        u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head);
+        // the exponentials are taken again: kept, they would be four bytes an element
+#pragma unroll
+        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(q[j]));
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (used(j)) {
+                float z[PER];
+                E::widen(q[j], z);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) z[e] = f * power(z[e]);
+                if (j < LO || j * BLOCK + (int)threadIdx.x < c.vecs) __builtin_nontemporal_store(E::narrow(z), vo + j * BLOCK + threadIdx.x);
+            }
+        if (single >= 0) E::store(out + single, f * power(zs));
+        // the token's own element a second time, by the lane that has just stored it
+        const int at = t - c.head;
+        if (at >= 0 && at < c.vecs * PER ? (at / PER) % BLOCK == (int)threadIdx.x : single == t) E::store(out + t, d * (1.0f - power(zt) / s));
+    }
+}
+
 // Gradient of rows whose maximum and sum are known: a workgroup takes GRAD_RUN elements of a row.
 constexpr int GRAD_BLOCK = 256;
 constexpr int GRAD_RUN = GRAD_BLOCK * 32;
@@ -375,18 +535,45 @@ static int sum_blocks(int64_t n)
     return (int)(b < 1 ? 1 : b > SUM_MAX_BLOCKS ? SUM_MAX_BLOCKS : b);
 }
 
-constexpr int ROW_BLOCK = 256;
 static constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
+
+typedef void (*RowKernel)(Logits, int64_t, Policy, float *, float *, void *, int64_t);
+struct RowShape {
+    RowKernel kernel;
+    int block;
+};
+// The kernel for rows of `vecs` vectors: the least that holds a row, or the one that reads it again.
+template <typename E, bool POLICY>
+static RowShape row_shape(int64_t vecs)
+{
+#define GS_HELD(BLOCK, NV, LO) if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, POLICY>, BLOCK}
+    GS_HELD(64, 4, 0);
+    GS_HELD(256, 4, 0);
+    GS_HELD(256, 6, 4);
+    GS_HELD(256, 8, 6);
+    GS_HELD(512, 6, 4);
+    GS_HELD(512, 8, 6);
+    GS_HELD(1024, 6, 4);
+    GS_HELD(1024, 8, 6);
+    GS_HELD(1024, 12, 8);
+    GS_HELD(1024, 16, 12);
+    GS_HELD(1024, 20, 16);
+    GS_HELD(1024, 24, 20);
+#undef GS_HELD
+    return {k_rows<E, 256, POLICY>, 256};
+}
 
 template <bool POLICY>
 static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride,
                               hipStream_t stream)
 {
-    const int64_t most = kMaxItems / ROW_BLOCK;
+    // a row that starts off a vector's boundary has up to one vector less, so of a row that the next smaller shape does not hold
+    // at least as many are there as that one has: LO
+    const RowShape s = X.dtype == GS_BF16 ? row_shape<Bf16, POLICY>(X.vocab / Bf16::PER) : row_shape<F32, POLICY>(X.vocab / F32::PER);
+    const int64_t most = kMaxItems / s.block;
     for (int64_t r = 0; r < X.rows; r += most) {
         const int grid = (int)(X.rows - r < most ? X.rows - r : most);
-        if (X.dtype == GS_BF16) k_rows<Bf16, ROW_BLOCK, POLICY><<<grid, ROW_BLOCK, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
-        else k_rows<F32, ROW_BLOCK, POLICY><<<grid, ROW_BLOCK, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
+        s.kernel<<<grid, s.block, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
