@@ -8,6 +8,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "gs_device.h"
 #include "gs_internal.h"
@@ -110,32 +111,13 @@ struct Cut {
     // the element that single i is
     template <int PER> __device__ __forceinline__ int single(int i) const { return i < head ? i : i + vecs * PER; }
 };
-
-// ---- sums of exponentials ---------------------------------------------------------------------
-// sum of exp2(k (z - m)) with its maximum so far.  With nothing but -inf so far the exponents are taken from 0, which leaves 0.
-struct MaxSum {
-    float m, s;
-    __device__ __forceinline__ void merge(float om, float os, float k)
-    {
-        const float n = fmaxf(m, om), base = n == -INFINITY ? 0.0f : n;
-        s = s * __builtin_amdgcn_exp2f((m - base) * k) + os * __builtin_amdgcn_exp2f((om - base) * k);
-        m = n;
-    }
-};
-
-template <int BLOCK>
-__device__ __forceinline__ MaxSum block_max_sum(MaxSum a, float k, MaxSum *lds)
+// whether two rows are cut in the same places
+__device__ __forceinline__ bool common(const void *a, const void *b)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) a.merge(__shfl_xor(a.m, d), __shfl_xor(a.s, d), k);
-    if constexpr (BLOCK > 64) {
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
-        __syncthreads();
-        a = lds[0];
-        for (int w = 1; w < BLOCK / 64; ++w) a.merge(lds[w].m, lds[w].s, k);
-    }
-    return a;
+    return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0;
 }
+// vectors that a 128-byte line holds before this one
+__device__ __forceinline__ int in_line(const void *v) { return (int)(reinterpret_cast<uintptr_t>(v) >> 4) & 7; }
 
 // ---- what one token adds to the policy loss ---------------------------------------------------
 struct Policy {
@@ -178,100 +160,34 @@ __device__ __forceinline__ int target_of(const Logits &L, int64_t r)
     return t >= 0 && t < L.vocab ? (int)t : -1;
 }
 
-// +0 over a row or a part of one
+// +0 over a row
 template <typename E, int BLOCK>
 __device__ __forceinline__ void zero_row(typename E::T *out, int n)
 {
     const Cut c = Cut::of<E::PER>(out, n, true);
     u32x4 *v = reinterpret_cast<u32x4 *>(out + c.head);
-    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) v[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, v + i);
     for (int i = threadIdx.x; i < c.singles; i += BLOCK) out[c.single<E::PER>(i)] = 0;
 }
 
-// Gradient over n elements of a row: d ([i = at] - exp2(k (z - m)) / s), where `at` may lie outside.  out may be in: every element
-// is read and written by the same lane.
+// Gradient over elements [from, to) of a row one by one, for an output that has no vectors in common with the row:
+// d ([i = t] - exp2(k (z - m)) / s)
 template <typename E, int BLOCK>
-__device__ __forceinline__ void grad_row(const typename E::T *in, typename E::T *out, int n, int at, float m, float s, float k, float d)
+__device__ __forceinline__ void grad_singly(const typename E::T *row, typename E::T *out, int from, int to, int t, float m, float s, float k, float d)
 {
-    const float f = d / s;
-    const bool same = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-    const Cut c = Cut::of<E::PER>(in, n, same);
-    const u32x4 *vi = reinterpret_cast<const u32x4 *>(in + c.head);
-    u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head);
-    auto power = [&](float z) { return __builtin_amdgcn_exp2f((z - m) * k); };
-    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) {
-        float raw[E::PER], z[E::PER];
-        E::widen(vi[i], raw);
-#pragma unroll
-        for (int e = 0; e < E::PER; ++e) z[e] = -f * power(raw[e]);
-        const int rel = at - c.head - i * E::PER;
-        if (rel >= 0 && rel < E::PER)
-#pragma unroll
-            for (int e = 0; e < E::PER; ++e) z[e] = e == rel ? d * (1.0f - power(raw[e]) / s) : z[e];
-        vo[i] = E::narrow(z);
-    }
-    for (int i = threadIdx.x; i < c.singles; i += BLOCK) {
-        const int e = c.single<E::PER>(i);
-        const float x = power(E::load(in + e));
-        E::store(out + e, e == at ? d * (1.0f - x / s) : -f * x);
-    }
-}
-
-// One workgroup a row: maximum and sum in one pass, then the token's log-probability and, with POLICY and somewhere to put it,
-// the gradient in a second pass over the row.
-template <typename E, int BLOCK, bool POLICY>
-__global__ __launch_bounds__(BLOCK) void k_rows(Logits L, int64_t row0, Policy P, float *logp, float *row_stats, void *dlogits, int64_t dstride)
-{
-    typedef typename E::T T;
-    __shared__ MaxSum lds[BLOCK / 64];
-    const int64_t r = row0 + blockIdx.x;
-    const int t = target_of(L, r);
-    const float w = POLICY ? weight_of(P.weights, r) : 1.0f;
-    T *out = POLICY && dlogits ? static_cast<T *>(dlogits) + r * dstride : nullptr;
-    if (t < 0 || w == 0.0f) {
-        if (threadIdx.x == 0) {
-            logp[r] = 0.0f;
-            if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
-        }
-        if (out) zero_row<E, BLOCK>(out, L.vocab);
-        return;
-    }
-    const T *row = static_cast<const T *>(L.x) + r * L.stride;
-    const float zt = E::load(row + t);
-    const Cut c = Cut::of<E::PER>(row, L.vocab, true);
-    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
-    MaxSum a = {-INFINITY, 0.0f};
-    for (int i = threadIdx.x; i < c.vecs; i += BLOCK) {
-        float z[E::PER], m = -INFINITY, s = 0.0f;
-        E::widen(v[i], z);
-#pragma unroll
-        for (int e = 0; e < E::PER; ++e) m = fmaxf(m, z[e]);
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int e = 0; e < E::PER; ++e) s += __builtin_amdgcn_exp2f((z[e] - base) * P.k);
-        a.merge(m, s, P.k);
-    }
-    for (int i = threadIdx.x; i < c.singles; i += BLOCK) {
-        const float z = E::load(row + c.single<E::PER>(i));
-        a.merge(z, z == -INFINITY ? 0.0f : z != z ? z : 1.0f, P.k);
-    }
-    a = block_max_sum<BLOCK>(a, P.k, lds);
-    const float lp = (zt - a.m) * P.it - logf(a.s);
-    if (threadIdx.x == 0) {
-        logp[r] = lp;
-        if (row_stats) row_stats[2 * r] = a.m, row_stats[2 * r + 1] = a.s;
-    }
-    if constexpr (POLICY) {
-        if (!out) return;
-        const float d = w * policy_terms(lp, r, P).slope * P.it;
-        if (d == 0.0f) zero_row<E, BLOCK>(out, L.vocab);
-        else grad_row<E, BLOCK>(row, out, L.vocab, t, a.m, a.s, P.k, d);
+    for (int i = from + threadIdx.x; i < to; i += BLOCK) {
+        const float p = __builtin_amdgcn_exp2f((E::load(row + i) - m) * k) / s;
+        E::store(out + i, i == t ? d * (1.0f - p) : -d * p);
     }
 }
 
 // ---- rows held in registers -------------------------------------------------------------------
 // One workgroup a row, as before, but the row is read once: its lanes keep NV vectors each, from the first maximum to the
 // gradient.  The first LO vectors of a lane lie in the row whatever its length; the rest may not, and are -inf.
+//
+// A wave takes its exponentials from a maximum of its own, as soon as its vectors are there, and waits for the others once, for the
+// row's maximum and sum; its gradient is then f exp2((m_wave - m) k) times those exponentials.  Of the first KEEP vectors the
+// exponentials stay (four bytes an element), of the others the logits (two in bf16), and the exponential is taken again.
 template <int CTRL, int ROWS = 0xf>
 __device__ __forceinline__ float from_dpp(float x, float none)
 {
@@ -283,6 +199,7 @@ __device__ __forceinline__ float join(float x, float y)
     if constexpr (MAX) return fmaxf(x, y);
     else return x + y;
 }
+// over 16 lanes, in all of them
 template <bool MAX>
 __device__ __forceinline__ float row_join(float x)
 {
@@ -291,30 +208,40 @@ __device__ __forceinline__ float row_join(float x)
     x = join<MAX>(x, from_dpp<0x141>(x, x));
     return join<MAX>(x, from_dpp<0x140>(x, x));
 }
-template <bool MAX, int BLOCK>
-__device__ __forceinline__ float block_join(float x, float *lds)
+__device__ __forceinline__ float of_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+template <bool MAX>
+__device__ __forceinline__ float wave_join(float x)
 {
     constexpr float none = MAX ? -INFINITY : 0.0f;
     x = row_join<MAX>(x);
     x = join<MAX>(x, from_dpp<0x142, 0xa>(x, none));
     x = join<MAX>(x, from_dpp<0x143, 0xc>(x, none));
-    x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
-    if constexpr (BLOCK > 64) {
-        const int lane = threadIdx.x & 63;
-        if (lane == 0) lds[threadIdx.x >> 6] = x;
-        __syncthreads();
-        x = row_join<MAX>(lane < BLOCK / 64 ? lds[lane] : none);
-        x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 0));
-    }
-    return x;
+    return of_lane(x, 63);
 }
 
-template <typename E, int BLOCK, int NV, int LO, bool POLICY>
-__global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, Policy P, float *logp, float *row_stats, void *dlogits, int64_t dstride)
+// exp2(k z - c) in place of exp2(k (z - m)): one rounding and one operation.  c is k m rounded, and `off` what the rounding took
+// (k m - c, exact), by which all exponentials are too large together.  Where it could be more than 64, so that |k m| is over 2^31, logits
+// that are not m itself lie so far below it that they count nothing: any k that keeps them there will do, and a power of two has no rounding.
+struct Shift {
+    float k, c, off;
+    __device__ __forceinline__ static Shift from(float m, float k)
+    {
+        const float base = m == -INFINITY ? 0.0f : m, a = fabsf(base);          // nothing but -inf: all exponentials 0
+        Shift s;
+        s.k = a * k < 0x1p31f ? k : a < 0x1p80f ? 0x1p40f : 0x1p-20f;
+        s.c = base * s.k;
+        s.off = fmaf(base, s.k, -s.c);
+        return s;
+    }
+    __device__ __forceinline__ float power(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, k, -c)); }
+};
+
+template <typename E, int BLOCK, int NV, int LO, int KEEP, bool POLICY>
+__global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t keep_row, Policy P, float *logp, float *row_stats, void *dlogits, int64_t dstride)
 {
     typedef typename E::T T;
-    constexpr int PER = E::PER;
-    __shared__ float lds[2][BLOCK / 64];
+    constexpr int PER = E::PER, NW = BLOCK / 64;
+    __shared__ float lds_m[NW], lds_s[NW];
     const int64_t r = row0 + blockIdx.x;
     const int t = target_of(L, r);
     const float w = POLICY ? weight_of(P.weights, r) : 1.0f;
@@ -329,39 +256,58 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, Policy P
     }
     const T *row = static_cast<const T *>(L.x) + r * L.stride;
     const Cut c = Cut::of<PER>(row, L.vocab, true);
-    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
-    const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
+    // vectors counted from the start of the first one's 128-byte line, so that a wave's accesses are whole lines
+    const int skip = in_line(row + c.head), end = skip + c.vecs;
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head) - skip;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto inside = [&](int j) {         // whether the lane's vector j is the row's
+        const int i = j * BLOCK + (int)threadIdx.x;
+        return (j > 0 || i >= skip) && (j < LO || i < end);
+    };
     u32x4 q[NV];
+    auto load = [&](auto keep) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = j * BLOCK + threadIdx.x;
-        if (j < LO) {
-            q[j] = __builtin_nontemporal_load(v + j * BLOCK + threadIdx.x);
-        } else {
-            q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
-            if (i < c.vecs) q[j] = __builtin_nontemporal_load(v + j * BLOCK + threadIdx.x);
+        for (int j = 0; j < NV; ++j) {
+            if (j == 0 || j >= LO) q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
+            if (inside(j)) q[j] = decltype(keep)::value ? v[j * BLOCK + threadIdx.x] : __builtin_nontemporal_load(v + j * BLOCK + threadIdx.x);
         }
-    }
+    };
+    if (!POLICY && r >= keep_row) load(std::true_type{});
+    else load(std::false_type{});
     const int single = (int)threadIdx.x < c.singles ? c.single<PER>(threadIdx.x) : -1;
     const float zs = single >= 0 ? E::load(row + single) : -INFINITY;
     const float zt = E::load(row + t);
-    auto used = [&](int j) { return j < LO || j * BLOCK + wave0 < c.vecs; };      // by any lane of the wave
+    auto used = [&](int j) { return j < LO || j * BLOCK + wave * 64 < end; };      // by any lane of the wave
 
     typename E::Max most;
 #pragma unroll
     for (int j = 0; j < NV; ++j) most.add(q[j]);
-    const float m = block_join<true, BLOCK>(fmaxf(most.get(), zs), lds[0]);
-    auto power = [&](float z) { return __builtin_amdgcn_exp2f((z - m) * P.k); };
-    float sum[4] = {power(zs), 0.0f, 0.0f, 0.0f};
+    const float mw = wave_join<true>(fmaxf(most.get(), zs));
+    const Shift shift = Shift::from(mw, P.k);
+    const float es = shift.power(zs);
+    float e[KEEP > 0 ? KEEP : 1][PER], sum[4] = {es, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
         if (used(j)) {
             float z[PER];
             E::widen(q[j], z);
 #pragma unroll
-            for (int e = 0; e < PER; ++e) sum[e & 3] += power(z[e]);
+            for (int i = 0; i < PER; ++i) {
+                const float x = shift.power(z[i]);
+                sum[i & 3] += x;
+                if (POLICY && j < KEEP) e[j < KEEP ? j : 0][i] = x;
+            }
         }
-    const float s = block_join<false, BLOCK>((sum[0] + sum[1]) + (sum[2] + sum[3]), lds[1]);
+    float m = mw, s = wave_join<false>((sum[0] + sum[1]) + (sum[2] + sum[3])) * __builtin_amdgcn_exp2f(-shift.off);
+    if constexpr (NW > 1) {
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) lds_m[wave] = m, lds_s[wave] = s;
+        asm volatile("" ::"v"(zt));        // is there before another wave may store in its place
+        __syncthreads();
+        const float ml = lane < NW ? lds_m[lane] : -INFINITY, sl = lane < NW ? lds_s[lane] : 0.0f;
+        m = of_lane(row_join<true>(ml), 0);
+        s = of_lane(row_join<false>(lane < NW ? sl * __builtin_amdgcn_exp2f((ml - m) * P.k) : 0.0f), 0);
+    }
     const float lp = (zt - m) * P.it - logf(s);
     if (threadIdx.x == 0) {
         logp[r] = lp;
@@ -371,47 +317,224 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, Policy P
         if (!out) return;
         const float d = w * policy_terms(lp, r, P).slope * P.it;
         if (d == 0.0f) return zero_row<E, BLOCK>(out, L.vocab);
-        if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0)      // no vectors in common: the row is read again
-            return grad_row<E, BLOCK>(row, out, L.vocab, t, m, s, P.k, d);
-        const float f = -d / s;
-        u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head);
-        // the exponentials are taken again: kept, they would be four bytes an element
+        if (!common(row, out)) return grad_singly<E, BLOCK>(row, out, 0, L.vocab, t, m, s, P.k, d);       // reads the row again
+        const float f = -d / s * __builtin_amdgcn_exp2f((mw - m) * P.k - shift.off);
+        u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head) - skip;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(q[j]));
+        for (int j = KEEP; j < NV; ++j) asm volatile("" : "+v"(q[j]));       // what was made of them is not kept
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (used(j)) {
                 float z[PER];
                 E::widen(q[j], z);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) z[e] = f * power(z[e]);
-                if (j < LO || j * BLOCK + (int)threadIdx.x < c.vecs) __builtin_nontemporal_store(E::narrow(z), vo + j * BLOCK + threadIdx.x);
+                for (int i = 0; i < PER; ++i) z[i] = f * (j < KEEP ? e[j < KEEP ? j : 0][i] : shift.power(z[i]));
+                if (inside(j)) __builtin_nontemporal_store(E::narrow(z), vo + j * BLOCK + threadIdx.x);
             }
-        if (single >= 0) E::store(out + single, f * power(zs));
+        if (single >= 0) E::store(out + single, f * es);
         // the token's own element a second time, by the lane that has just stored it
         const int at = t - c.head;
-        if (at >= 0 && at < c.vecs * PER ? (at / PER) % BLOCK == (int)threadIdx.x : single == t) E::store(out + t, d * (1.0f - power(zt) / s));
+        if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
+            E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
     }
 }
 
-// Gradient of rows whose maximum and sum are known: a workgroup takes GRAD_RUN elements of a row.
-constexpr int GRAD_BLOCK = 256;
-constexpr int GRAD_RUN = GRAD_BLOCK * 32;
+// ---- rows in parts ----------------------------------------------------------------------------
+// Rows too long to be held, and rows of which there are too few to fill the chip: parts of PART_MIN elements or more, a
+// workgroup each, leave a maximum and a sum, and what comes after joins those of a row, one to a lane.
+constexpr int PART_BLOCK = 256;
+constexpr int PART_MIN = 8192;
+constexpr int PARTS = 64;
+constexpr int64_t SPLIT_ROWS = 128;
+constexpr int64_t SPLIT_VOCAB = 40000;
+
+struct MaxSum {
+    float m, s;
+};
+
+// The part's maximum and its sum of exp2(k (z - maximum)).  Read again afterwards, so the lines stay in the caches.  A row has one
+// entry more than parts: the token's own logit, which a gradient written in place would not leave for the others to read.
 template <typename E>
-__global__ __launch_bounds__(GRAD_BLOCK) void k_grad(Logits L, int64_t row0, uint32_t runs, float k, float it, const float *row_stats, const float *dlogp,
-                                                     void *dlogits, int64_t dstride)
+__global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int parts, int len, float k, const float *weights, MaxSum *partials)
+{
+    constexpr int NV = PART_MIN / PART_BLOCK / E::PER, NW = PART_BLOCK / 64;
+    __shared__ float lds_m[NW], lds_s[NW];
+    const uint32_t which = blockIdx.x / (uint32_t)parts, part = blockIdx.x - which * (uint32_t)parts;
+    const int64_t r = row0 + which;
+    const int t = target_of(L, r);
+    if (t < 0 || weight_of(weights, r) == 0.0f) return;
+    partials += (int64_t)which * (parts + 1);
+    const int from = (int)part * len, n = min(len, L.vocab - from);
+    const typename E::T *row = static_cast<const typename E::T *>(L.x) + r * L.stride + from;
+    const Cut c = Cut::of<E::PER>(row, n, true);
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
+    const float zs = (int)threadIdx.x < c.singles ? E::load(row + c.single<E::PER>(threadIdx.x)) : -INFINITY;
+    float m = -INFINITY, s = 0.0f;
+    for (int i0 = 0; i0 == 0 || i0 < c.vecs; i0 += NV * PART_BLOCK) {
+        u32x4 q[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = i0 + j * PART_BLOCK + (int)threadIdx.x;
+            q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
+            if (i < c.vecs) q[j] = v[i];
+        }
+        typename E::Max most;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) most.add(q[j]);
+        const float extra = i0 == 0 ? zs : -INFINITY, mi = wave_join<true>(fmaxf(most.get(), extra));
+        const Shift shift = Shift::from(mi, k);
+        float sum[4] = {shift.power(extra), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float z[E::PER];
+            E::widen(q[j], z);
+#pragma unroll
+            for (int e = 0; e < E::PER; ++e) sum[e & 3] += shift.power(z[e]);
+        }
+        const float si = wave_join<false>((sum[0] + sum[1]) + (sum[2] + sum[3])) * __builtin_amdgcn_exp2f(-shift.off);
+        const float both = fmaxf(m, mi), base = both == -INFINITY ? 0.0f : both;
+        s = s * __builtin_amdgcn_exp2f((m - base) * k) + si * __builtin_amdgcn_exp2f((mi - base) * k);
+        m = both;
+    }
+    if ((threadIdx.x & 63) == 0) lds_m[threadIdx.x >> 6] = m, lds_s[threadIdx.x >> 6] = s;
+    __syncthreads();
+    const int lane = threadIdx.x & 63;
+    const float ml = lane < NW ? lds_m[lane] : -INFINITY, sl = lane < NW ? lds_s[lane] : 0.0f;
+    m = of_lane(row_join<true>(ml), 0);
+    const float base = m == -INFINITY ? 0.0f : m;
+    s = of_lane(row_join<false>(lane < NW ? sl * __builtin_amdgcn_exp2f((ml - base) * k) : 0.0f), 0);
+    if (threadIdx.x == 0) {
+        partials[part] = {m, s};
+        if (t >= from && t < from + n) partials[parts].m = E::load(row + t - from);
+    }
+}
+
+// The row's maximum and sum from those of its parts.  A row of nothing but -inf has a sum of 0 here, from which all is NaN as well.
+__device__ __forceinline__ MaxSum joined(const MaxSum *partials, int parts, float k)
+{
+    const int lane = threadIdx.x & 63;
+    const MaxSum a = lane < parts ? partials[lane] : MaxSum{-INFINITY, 0.0f};
+    MaxSum j;
+    j.m = wave_join<true>(a.m);
+    const float base = j.m == -INFINITY ? 0.0f : j.m;
+    j.s = wave_join<false>(a.s * __builtin_amdgcn_exp2f((a.m - base) * k));
+    return j;
+}
+
+// Log-probabilities of rows in parts, a wave each.
+__global__ __launch_bounds__(PART_BLOCK) void k_join(Logits L, int64_t row0, int rows, int parts, float k, float it, const float *weights,
+                                                     const MaxSum *partials, float *logp, float *row_stats)
+{
+    const int which = (int)blockIdx.x * (PART_BLOCK / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (which >= rows) return;
+    const int64_t r = row0 + which;
+    const int t = target_of(L, r);
+    MaxSum a = {0.0f, 1.0f};
+    float lp = 0.0f;
+    if (t >= 0 && weight_of(weights, r) != 0.0f) {
+        partials += (int64_t)which * (parts + 1);
+        a = joined(partials, parts, k);
+        lp = (partials[parts].m - a.m) * it - logf(a.s);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        logp[r] = lp;
+        if (row_stats) row_stats[2 * r] = a.m, row_stats[2 * r + 1] = a.s;
+    }
+}
+
+// ---- gradient of rows whose maximum and sum are known -------------------------------------------
+// A workgroup takes a run of GRAD_VECS vectors of a row, counted from the start of the row's first line; the first one has the single elements
+// too.  PARTS: maximum and sum come from a row's parts, and its policy loss is worked out here; else they and the loss's gradient in logp
+// are given, and the rows are taken from the last one on: the end of what was read before is still in the memory-side cache.
+constexpr int GRAD_BLOCK = 256;
+constexpr int GRAD_NV = 2;
+constexpr int GRAD_VECS = GRAD_BLOCK * GRAD_NV;
+struct GradArgs {
+    Logits L;
+    int64_t row0, rows, dstride;
+    Policy P;
+    const float *row_stats, *dlogp;
+    const MaxSum *partials;
+    float *logp;
+    void *dlogits;
+    uint32_t runs;
+    int parts;
+};
+template <typename E, bool FROM_PARTS>
+__global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
 {
     typedef typename E::T T;
-    const uint32_t part = blockIdx.x / runs;
-    const int64_t r = row0 + part;
-    const int from = (int)(blockIdx.x - part * runs) * GRAD_RUN, n = min(GRAD_RUN, L.vocab - from);
+    constexpr int PER = E::PER;
+    const uint32_t which = blockIdx.x / A.runs, run = blockIdx.x - which * A.runs;
+    const int64_t r = A.row0 + (FROM_PARTS ? (int64_t)which : A.rows - 1 - which);
+    const Logits &L = A.L;
     const int t = target_of(L, r);
-    T *out = static_cast<T *>(dlogits) + r * dstride + from;
-    const float d = dlogp[r] * it;
-    if (t < 0 || d == 0.0f) return zero_row<E, GRAD_BLOCK>(out, n);
-    const T *row = static_cast<const T *>(L.x) + r * L.stride + from;
-    const int at = t >= from && t < from + n ? t - from : -1;
-    grad_row<E, GRAD_BLOCK>(row, out, n, at, row_stats[2 * r], row_stats[2 * r + 1], k, d);
+    const T *row = static_cast<const T *>(L.x) + r * L.stride;
+    T *out = static_cast<T *>(A.dlogits) + r * A.dstride;
+    float d = 0.0f;
+    MaxSum a = {0.0f, 1.0f};
+    if constexpr (FROM_PARTS) {
+        const float w = weight_of(A.P.weights, r);
+        float lp = 0.0f;
+        if (t >= 0 && w != 0.0f) {
+            const MaxSum *partials = A.partials + (int64_t)which * (A.parts + 1);
+            a = joined(partials, A.parts, A.P.k);
+            lp = (partials[A.parts].m - a.m) * A.P.it - logf(a.s);
+            d = w * policy_terms(lp, r, A.P).slope * A.P.it;
+        }
+        if (run == 0 && threadIdx.x == 0) A.logp[r] = lp;
+    } else if (t >= 0) {
+        d = A.dlogp[r] * A.P.it;
+        a = {A.row_stats[2 * r], A.row_stats[2 * r + 1]};
+    }
+    const bool vectors = d == 0.0f || common(row, out);
+    const Cut c = Cut::of<PER>(d == 0.0f ? out : row, L.vocab, true);
+    const int skip = in_line((d == 0.0f ? out : row) + c.head), end = skip + c.vecs;
+    const int i0 = (int)run * GRAD_VECS + (int)threadIdx.x;
+    u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head) - skip;
+    const int single = run == 0 && (int)threadIdx.x < c.singles ? c.single<PER>(threadIdx.x) : -1;
+    if (d == 0.0f) {
+#pragma unroll
+        for (int j = 0; j < GRAD_NV; ++j)
+            if (i0 + j * GRAD_BLOCK >= skip && i0 + j * GRAD_BLOCK < end) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, vo + i0 + j * GRAD_BLOCK);
+        if (single >= 0) out[single] = 0;
+        return;
+    }
+    if (!vectors) {
+        const int from = (int)run * GRAD_VECS * PER;
+        return grad_singly<E, GRAD_BLOCK>(row, out, from, min(from + GRAD_VECS * PER, L.vocab), t, a.m, a.s, A.P.k, d);
+    }
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head) - skip;
+    u32x4 q[GRAD_NV];
+#pragma unroll
+    for (int j = 0; j < GRAD_NV; ++j)
+        if (i0 + j * GRAD_BLOCK >= skip && i0 + j * GRAD_BLOCK < end) q[j] = __builtin_nontemporal_load(v + i0 + j * GRAD_BLOCK);
+    const Shift shift = Shift::from(a.m, A.P.k);
+    const float f = -d / a.s * __builtin_amdgcn_exp2f(-shift.off);
+    const int at = t - c.head + skip * PER;                  // as an element of the vectors
+#pragma unroll
+    for (int j = 0; j < GRAD_NV; ++j) {
+        const int i = i0 + j * GRAD_BLOCK;
+        if (i < skip || i >= end) continue;
+        float z[PER];
+        E::widen(q[j], z);
+        const int rel = at - i * PER;
+        if (rel >= 0 && rel < PER) {                         // the lane with the token's own element
+            const float zt = E::load(row + t);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) z[e] = f * shift.power(z[e]);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) z[e] = e == rel ? d * (1.0f - __builtin_amdgcn_exp2f((zt - a.m) * A.P.k) / a.s) : z[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) z[e] = f * shift.power(z[e]);
+        }
+        __builtin_nontemporal_store(E::narrow(z), vo + i);
+    }
+    if (single >= 0) {
+        const float p = __builtin_amdgcn_exp2f((E::load(row + single) - a.m) * A.P.k) / a.s;
+        E::store(out + single, single == t ? d * (1.0f - p) : -d * p);
+    }
 }
 
 // ---- sums over tokens -------------------------------------------------------------------------
@@ -537,46 +660,123 @@ static int sum_blocks(int64_t n)
 
 static constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
 
-typedef void (*RowKernel)(Logits, int64_t, Policy, float *, float *, void *, int64_t);
+typedef void (*RowKernel)(Logits, int64_t, int64_t, Policy, float *, float *, void *, int64_t);
 struct RowShape {
     RowKernel kernel;
     int block;
 };
-// The kernel for rows of `vecs` vectors: the least that holds a row, or the one that reads it again.
+// The kernel for rows of up to `vecs` vectors, counted from the start of the first one's line: the least that holds one, or none.
 template <typename E, bool POLICY>
 static RowShape row_shape(int64_t vecs)
 {
-#define GS_HELD(BLOCK, NV, LO) if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, POLICY>, BLOCK}
-    GS_HELD(64, 4, 0);
-    GS_HELD(256, 4, 0);
-    GS_HELD(256, 6, 4);
-    GS_HELD(256, 8, 6);
-    GS_HELD(512, 6, 4);
-    GS_HELD(512, 8, 6);
-    GS_HELD(1024, 6, 4);
-    GS_HELD(1024, 8, 6);
-    GS_HELD(1024, 12, 8);
-    GS_HELD(1024, 16, 12);
-    GS_HELD(1024, 20, 16);
-    GS_HELD(1024, 24, 20);
+    // KEEP: as many as there is room for in a workgroup's share of the registers; an fp32 vector takes as much as its exponentials
+#define GS_HELD(BLOCK, NV, LO, KEEP) \
+    if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, !POLICY ? 0 : E::PER == 4 ? NV : KEEP, POLICY>, BLOCK}
+    GS_HELD(64, 4, 0, 4);
+    GS_HELD(128, 4, 1, 4);
+    GS_HELD(256, 4, 1, 4);
+    GS_HELD(512, 4, 1, 4);
+    GS_HELD(1024, 3, 1, 3);
+    GS_HELD(1024, 4, 2, 4);
+    GS_HELD(1024, 6, 3, 6);
+    GS_HELD(1024, 8, 5, 8);
+    GS_HELD(1024, 12, 7, 12);
+    GS_HELD(1024, 16, 11, 8);
+    GS_HELD(1024, 20, 15, 4);
+    GS_HELD(1024, 24, 19, 0);
 #undef GS_HELD
-    return {k_rows<E, 256, POLICY>, 256};
+    return {nullptr, 0};
 }
 
-template <bool POLICY>
-static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride,
-                              hipStream_t stream)
+struct Grid {
+    int64_t rows;          // of a launch
+    int parts, len;
+};
+// Rows in parts: as many parts as a wave joins, and rows as the workspace holds partials for.
+static Grid parts_of(const gs_logits &X)
 {
-    // a row that starts off a vector's boundary has up to one vector less, so of a row that the next smaller shape does not hold
-    // at least as many are there as that one has: LO
-    const RowShape s = X.dtype == GS_BF16 ? row_shape<Bf16, POLICY>(X.vocab / Bf16::PER) : row_shape<F32, POLICY>(X.vocab / F32::PER);
-    const int64_t most = kMaxItems / s.block;
-    for (int64_t r = 0; r < X.rows; r += most) {
-        const int grid = (int)(X.rows - r < most ? X.rows - r : most);
-        s.kernel<<<grid, s.block, 0, stream>>>(L, r, P, logp, row_stats, dlogits, dstride);
+    Grid g;
+    const int64_t len = (X.vocab + PARTS - 1) / PARTS;
+    g.len = (int)(len <= PART_MIN ? PART_MIN : (len + PART_MIN - 1) / PART_MIN * PART_MIN);
+    g.parts = (int)((X.vocab + g.len - 1) / g.len);
+    g.rows = GS_SQNORM_MAX_BLOCKS / (g.parts + 1);
+    return g;
+}
+static bool in_parts(const gs_logits &X)
+{
+    return X.rows <= SPLIT_ROWS && X.vocab > SPLIT_VOCAB;
+}
+
+template <typename E>
+static uint32_t grad_runs(int64_t vocab) { return (uint32_t)((vocab / E::PER + 7) / GRAD_VECS + 1); }
+
+template <typename E, bool FROM_PARTS>
+static hipError_t launch_grad(GradArgs A, int64_t rows, hipStream_t stream)
+{
+    A.runs = grad_runs<E>(A.L.vocab);
+    const int64_t most = kMaxItems / GRAD_BLOCK / A.runs;               // 15 rows of 2^30 elements
+    const int64_t first = A.row0;
+    for (int64_t done = 0; done < rows; done += A.rows) {
+        A.rows = rows - done < most ? rows - done : most;
+        A.row0 = FROM_PARTS ? first + done : first + rows - done - A.rows;
+        k_grad<E, FROM_PARTS><<<(uint32_t)A.rows * A.runs, GRAD_BLOCK, 0, stream>>>(A);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <typename E, bool POLICY>
+static hipError_t launch_in_parts(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride,
+                                  MaxSum *partials, hipStream_t stream)
+{
+    const Grid g = parts_of(X);
+    for (int64_t r = 0; r < X.rows; r += g.rows) {
+        const int rows = (int)(X.rows - r < g.rows ? X.rows - r : g.rows);
+        k_part<E><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, P.weights, partials);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if (POLICY && dlogits) {
+            const GradArgs A = {L, r, rows, dstride, P, nullptr, nullptr, partials, logp, dlogits, 0, g.parts};
+            // a launch takes as many rows as it can, and joins the partials of its own from the first on: no more than those
+            const int64_t most = kMaxItems / GRAD_BLOCK / grad_runs<E>(X.vocab);
+            for (int64_t q = 0; q < rows; q += most) {
+                GradArgs B = A;
+                B.row0 = r + q;
+                B.partials = partials + q * (g.parts + 1);
+                if (hipError_t e = launch_grad<E, true>(B, rows - q < most ? rows - q : most, stream); e != hipSuccess) return e;
+            }
+        } else {
+            k_join<<<(rows + PART_BLOCK / 64 - 1) / (PART_BLOCK / 64), PART_BLOCK, 0, stream>>>(L, r, rows, g.parts, P.k, P.it, P.weights, partials, logp, row_stats);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+template <typename E, bool POLICY>
+static hipError_t launch_rows_of(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride, void *ws,
+                                 hipStream_t stream)
+{
+    // rows that all start on a line have no vectors missing from their first one
+    constexpr int64_t LINE = 128 / sizeof(typename E::T);
+    const bool on_lines = (reinterpret_cast<uintptr_t>(X.data) & 127) == 0 && (X.rows == 1 || X.row_stride % LINE == 0);
+    const RowShape s = row_shape<E, POLICY>(X.vocab / E::PER + (on_lines ? 0 : 7));
+    if (!s.kernel || in_parts(X)) return launch_in_parts<E, POLICY>(X, L, P, logp, row_stats, dlogits, dstride, static_cast<MaxSum *>(ws), stream);
+    // with the row statistics asked for, the rows are read again for a gradient: what the memory-side cache holds is left there
+    const int64_t kept = GS_KEEP_BYTES / (L.stride * (int64_t)sizeof(typename E::T)), keep_row = row_stats ? X.rows - kept : INT64_MAX;
+    const int64_t most = kMaxItems / s.block;
+    for (int64_t r = 0; r < X.rows; r += most) {
+        const int grid = (int)(X.rows - r < most ? X.rows - r : most);
+        s.kernel<<<grid, s.block, 0, stream>>>(L, r, keep_row, P, logp, row_stats, dlogits, dstride);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <bool POLICY>
+static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride, void *ws,
+                              hipStream_t stream)
+{
+    if (X.dtype == GS_BF16) return launch_rows_of<Bf16, POLICY>(X, L, P, logp, row_stats, dlogits, dstride, ws, stream);
+    return launch_rows_of<F32, POLICY>(X, L, P, logp, row_stats, dlogits, dstride, ws, stream);
 }
 
 // ---- checks -----------------------------------------------------------------------------------
@@ -655,7 +855,7 @@ gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float t
                       span_of(targets, rows * 8, false), span_of(logp, rows * 4, true), span_of(row_stats, rows * 8, true),
                       span_of(d_workspace, (int64_t)workspace_bytes, true)};
     if (!apart(s, 5)) return GS_ERR_INVALID_ARG;
-    hipError_t e = launch_rows<false>(*logits, logits_of(*logits, targets), scaled_by(temperature), logp, row_stats, nullptr, 0,
+    hipError_t e = launch_rows<false>(*logits, logits_of(*logits, targets), scaled_by(temperature), logp, row_stats, nullptr, 0, d_workspace,
                                       static_cast<hipStream_t>(stream));
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_token_logp launch");
 }
@@ -672,20 +872,16 @@ gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, fl
                       span_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), span_of(targets, rows * 8, false),
                       span_of(row_stats, rows * 8, false), span_of(dlogp, rows * 4, false)};
     if (!apart(s, 5, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
-    const Logits L = logits_of(*logits, targets);
-    const Policy P = scaled_by(temperature);
-    const uint32_t runs = (uint32_t)((logits->vocab + GRAD_RUN - 1) / GRAD_RUN);
-    const int64_t most = kMaxItems / GRAD_BLOCK / runs;           // at least 127 rows
-    const int64_t dstride = rows > 1 ? dlogits_stride : logits->vocab;
-    for (int64_t r = 0; r < rows; r += most) {
-        const uint32_t grid = (uint32_t)(rows - r < most ? rows - r : most) * runs;
-        if (logits->dtype == GS_BF16)
-            k_grad<Bf16><<<grid, GRAD_BLOCK, 0, static_cast<hipStream_t>(stream)>>>(L, r, runs, P.k, P.it, row_stats, dlogp, dlogits, dstride);
-        else
-            k_grad<F32><<<grid, GRAD_BLOCK, 0, static_cast<hipStream_t>(stream)>>>(L, r, runs, P.k, P.it, row_stats, dlogp, dlogits, dstride);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_fail(e, "gs_token_logp_grad launch");
-    }
-    return GS_OK;
+    GradArgs A = {};
+    A.L = logits_of(*logits, targets);
+    A.P = scaled_by(temperature);
+    A.dstride = rows > 1 ? dlogits_stride : logits->vocab;
+    A.row_stats = row_stats;
+    A.dlogp = dlogp;
+    A.dlogits = dlogits;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const hipError_t e = logits->dtype == GS_BF16 ? launch_grad<Bf16, false>(A, rows, st) : launch_grad<F32, false>(A, rows, st);
+    return e == hipSuccess ? GS_OK : hip_fail(e, "gs_token_logp_grad launch");
 }
 
 gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const gs_policy_hparams *hp, const float *old_logp,
@@ -723,7 +919,7 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     P.ref_logp = ref_logp;
     P.advantages = advantages;
     P.weights = weights;
-    hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, st);
+    hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, d_workspace, st);
     if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
     const int blocks = sum_blocks(rows);
     double *partials = static_cast<double *>(d_workspace);
