@@ -2,6 +2,7 @@
 // Every check runs before the first HIP call, so the error paths need no GPU.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -16,6 +17,13 @@ gs_status hip_fail(hipError_t e, const char *what)
 {
     snprintf(g_hip_err, sizeof g_hip_err, "%s: %s", what, hipGetErrorString(e));
     return GS_ERR_HIP;
+}
+
+// Upper halves of signalling NaNs, one after another.
+uint32_t next_tag()
+{
+    static std::atomic<uint32_t> count{0};
+    return 0x7ff00001u + count.fetch_add(1, std::memory_order_relaxed) % 0x7fffeu;
 }
 
 static bool finite_f(float x) { return std::isfinite(x); }

@@ -21,6 +21,15 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f)
     return ((u & 0x7fffffffu) > 0x7f800000u) ? nan : r;
 }
 
+// Past the die's L2 too, which otherwise keeps the line dirty and sends it out later, in an order of its own.  No builtin gives this
+// pair of cache bits.  A store of more than 64 bits goes on reading its registers for up to two cycles, in which none may be written:
+// hence the s_nop.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store_through(u32x4 *p, u32x4 v)
+{
+    asm volatile("global_store_dwordx4 %0, %1, off sc1 nt\n\ts_nop 1" ::"v"(p), "v"(v) : "memory");
+}
+
 // Clip coefficient from the total squared norm (Sec. 2.1: global L2 norm for clipping).
 __device__ __forceinline__ float clip_from(double sqnorm, float max_norm)
 {
@@ -74,6 +83,81 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
     double t = 0.0;
     if (wave == 0) t = row_sum(lane < NW ? lds[lane] : 0.0);
     return t;   // valid in thread 0
+}
+
+// ---- the last of a launch's workgroups finishes it ----------------------------------------------
+// Of a small launch a second one, for what its workgroups leave, is the larger part: 3.7 us of a stream's time each, whatever they
+// do.  So each leaves W 32-bit words in the caller's workspace, then looks whether all n have, and the last to look sees that they have.
+//   - Nothing has to be in the workspace before: a word lies beside a tag of this launch, in one 64-bit store, and counts only with
+//     it.  Tags are the upper halves of signalling NaNs, which no sum that was left there before has.
+//   - Two may see all n: the one that takes the tag out of the first slot finishes.
+//   - It clears the slots, so a graph, whose launches have the same tag every time, finds none of its own.
+//   - Nobody waits for another workgroup.
+// The words go to memory and come from there by atomic accesses of the device's scope: the dies' caches do not see each other's
+// lines.  A workgroup's own are there (vmcnt) before it looks at the others'.
+struct Meeting {
+    uint64_t *slots;
+    uint32_t tag;
+    int n;                        // 0: no meeting, another launch finishes
+};
+constexpr int MEET_MAX = 256;     // every workgroup reads the slots of all
+
+// by one lane of the wave that looks afterwards
+template <int W>
+__device__ __forceinline__ void leave(const Meeting &M, int me, const uint32_t (&w)[W])
+{
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+        __hip_atomic_store(M.slots + (int64_t)me * W + i, (uint64_t)M.tag << 32 | w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// By the whole wave: true in one workgroup of the launch, which reads the words with left() and then clears them.
+template <int W>
+__device__ __forceinline__ bool last_of(const Meeting &M)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const int lane = threadIdx.x & 63;
+    bool here = true;
+#pragma unroll 1
+    for (int i = lane; i < M.n; i += 64) {
+        uint64_t x[W];
+#pragma unroll
+        for (int q = 0; q < W; ++q) x[q] = __hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int q = 0; q < W; ++q) here = here && (uint32_t)(x[q] >> 32) == M.tag;
+    }
+    if (__ballot(here) != ~0ull) return false;
+    uint32_t tag = 0;
+    if (lane == 0) tag = (uint32_t)(__hip_atomic_fetch_and(M.slots, (uint64_t)0xffffffffu, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)tag) == M.tag;
+}
+template <int W>
+__device__ __forceinline__ uint32_t left(const Meeting &M, int i, int q)
+{
+    return (uint32_t)__hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int W>
+__device__ __forceinline__ void clear(const Meeting &M)
+{
+    for (int i = threadIdx.x & 63; i < M.n * W; i += 64) __hip_atomic_store(M.slots + i, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// D doubles a slot, summed over all of them in a fixed order, in the wave's last lane
+template <int D>
+__device__ __forceinline__ void left_sums(const Meeting &M, double (&x)[D])
+{
+#pragma unroll
+    for (int q = 0; q < D; ++q) x[q] = 0.0;
+#pragma unroll 1
+    for (int i = threadIdx.x & 63; i < M.n; i += 64)
+#pragma unroll
+        for (int q = 0; q < D; ++q) x[q] += __hiloint2double((int)left<2 * D>(M, i, 2 * q + 1), (int)left<2 * D>(M, i, 2 * q));
+#pragma unroll
+    for (int q = 0; q < D; ++q) x[q] = wave_sum(x[q]);
+    clear<2 * D>(M);
+}
+__device__ __forceinline__ void halves(double x, uint32_t &lo, uint32_t &hi)
+{
+    lo = (uint32_t)__double2loint(x);
+    hi = (uint32_t)__double2hiint(x);
 }
 
 }  // namespace gs

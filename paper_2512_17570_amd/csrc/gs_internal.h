@@ -141,6 +141,7 @@ gs_status validate_hparams(const gs_adamw_hparams *hp);
 gs_status validate_grads(const uint16_t *const *grads, int k);
 StepConsts make_consts(const gs_adamw_hparams &hp);
 gs_status hip_fail(hipError_t e, const char *what);
+uint32_t next_tag();      // of a launch whose last workgroup finishes it (gs_device.h)
 
 }  // namespace gs
 #endif

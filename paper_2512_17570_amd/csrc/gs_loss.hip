@@ -17,7 +17,6 @@
 
 namespace gs {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -125,22 +124,33 @@ struct Policy {
     float it;                     // 1 / temperature
     float low, high, kl;          // bounds of the ratio, factor of the KL term
     const float *old_logp, *ref_logp, *advantages, *weights;
+    Meeting meet;                 // of a launch with few rows
+    float *stats;
+    int accumulate;
 };
 struct Terms {
     float pg, kl, slope;          // slope: of pg + factor kl in logp
     bool clipped;
 };
-__device__ __forceinline__ Terms policy_terms(float logp, int64_t r, const Policy &P)
+// what it takes besides the log-probability
+struct Token {
+    float old_logp, ref_logp, advantage;
+};
+__device__ __forceinline__ Token token_of(const Policy &P, int64_t r)
+{
+    return {P.old_logp[r], P.ref_logp ? P.ref_logp[r] : 0.0f, P.advantages[r]};
+}
+__device__ __forceinline__ Terms policy_terms(float logp, const Token &k, const Policy &P)
 {
     Terms t;
-    const float a = P.advantages[r], ratio = expf(logp - P.old_logp[r]);
+    const float a = k.advantage, ratio = expf(logp - k.old_logp);
     const float plain = ratio * a, held = fminf(fmaxf(ratio, P.low), P.high) * a;
     t.clipped = held < plain;     // NaN: the plain product, which then is one
     t.pg = -(t.clipped ? held : plain);
     t.slope = t.clipped ? 0.0f : -plain;
     t.kl = 0.0f;
     if (P.ref_logp) {
-        const float d = P.ref_logp[r] - logp, em1 = expm1f(d);      // exp(d) - 1 without cancellation: d is small in earnest
+        const float d = k.ref_logp - logp, em1 = expm1f(d);      // exp(d) - 1 without cancellation: d is small in earnest
         t.kl = em1 - d;
         if (P.kl != 0.0f) t.slope += P.kl * -em1;
     }
@@ -153,11 +163,39 @@ struct Logits {
     int64_t stride;
     const int64_t *targets;
     int vocab;
+    bool few;                     // rows: what they take is a chain of latencies
 };
 __device__ __forceinline__ int target_of(const Logits &L, int64_t r)
 {
     const int64_t t = L.targets[r];
     return t >= 0 && t < L.vocab ? (int)t : -1;
+}
+
+// What a row adds to the four sums of the policy loss.
+struct Sums {
+    double x[4];
+};
+__device__ __forceinline__ Sums sums_of(const Terms &e, float w, float kl_coef)
+{
+    const double pg = (double)w * e.pg, kl = (double)w * e.kl;
+    return {{kl_coef != 0.0f ? pg + kl_coef * kl : pg, pg, kl, e.clipped ? (double)w : 0.0}};
+}
+__device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Sums &s)
+{
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) halves(s.x[i], w[2 * i], w[2 * i + 1]);
+    leave(M, (int)r, w);
+}
+// by the wave whose lane has left a row's sums
+__device__ __forceinline__ void finish_policy(const Meeting &M, float *out, int accumulate)
+{
+    if (!last_of<8>(M)) return;
+    double x[4];
+    left_sums(M, x);
+    if ((threadIdx.x & 63) == 63)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = (float)((accumulate ? (double)out[i] : 0.0) + x[i]);
 }
 
 // +0 over a row
@@ -246,14 +284,20 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     const int t = target_of(L, r);
     const float w = POLICY ? weight_of(P.weights, r) : 1.0f;
     T *out = POLICY && dlogits ? static_cast<T *>(dlogits) + r * dstride : nullptr;
-    if (t < 0 || w == 0.0f) {
+    const bool meets = POLICY && P.meet.n > 0;
+    auto no_token = [&] {
         if (threadIdx.x == 0) {
             logp[r] = 0.0f;
             if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
+            if (meets) leave_sums(P.meet, r, Sums{});
         }
         if (out) zero_row<E, BLOCK>(out, L.vocab);
-        return;
-    }
+        if (meets && threadIdx.x < 64) finish_policy(P.meet, P.stats, P.accumulate);
+    };
+    // With few rows a workgroup does not wait to learn whether its row counts before it asks for it.
+    if (!L.few && (t < 0 || w == 0.0f)) return no_token();
+    Token token = {};
+    if constexpr (POLICY) token = token_of(P, r);
     const T *row = static_cast<const T *>(L.x) + r * L.stride;
     const Cut c = Cut::of<PER>(row, L.vocab, true);
     // vectors counted from the start of the first one's 128-byte line, so that a wave's accesses are whole lines
@@ -276,6 +320,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     else load(std::false_type{});
     const int single = (int)threadIdx.x < c.singles ? c.single<PER>(threadIdx.x) : -1;
     const float zs = single >= 0 ? E::load(row + single) : -INFINITY;
+    if (L.few && (t < 0 || w == 0.0f)) return no_token();
     const float zt = E::load(row + t);
     auto used = [&](int j) { return j < LO || j * BLOCK + wave * 64 < end; };      // by any lane of the wave
 
@@ -314,28 +359,35 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
         if (row_stats) row_stats[2 * r] = m, row_stats[2 * r + 1] = s;
     }
     if constexpr (POLICY) {
-        if (!out) return;
-        const float d = w * policy_terms(lp, r, P).slope * P.it;
-        if (d == 0.0f) return zero_row<E, BLOCK>(out, L.vocab);
-        if (!common(row, out)) return grad_singly<E, BLOCK>(row, out, 0, L.vocab, t, m, s, P.k, d);       // reads the row again
-        const float f = -d / s * __builtin_amdgcn_exp2f((mw - m) * P.k - shift.off);
-        u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head) - skip;
+        const Terms terms = policy_terms(lp, token, P);
+        if (meets && threadIdx.x == 0) leave_sums(P.meet, r, sums_of(terms, w, P.kl));
+        const float d = w * terms.slope * P.it;
+        if (!out) {
+        } else if (d == 0.0f) {
+            zero_row<E, BLOCK>(out, L.vocab);
+        } else if (!common(row, out)) {
+            grad_singly<E, BLOCK>(row, out, 0, L.vocab, t, m, s, P.k, d);       // reads the row again
+        } else {
+            const float f = -d / s * __builtin_amdgcn_exp2f((mw - m) * P.k - shift.off);
+            u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head) - skip;
 #pragma unroll
-        for (int j = KEEP; j < NV; ++j) asm volatile("" : "+v"(q[j]));       // what was made of them is not kept
+            for (int j = KEEP; j < NV; ++j) asm volatile("" : "+v"(q[j]));       // what was made of them is not kept
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (used(j)) {
-                float z[PER];
-                E::widen(q[j], z);
+            for (int j = 0; j < NV; ++j)
+                if (used(j)) {
+                    float z[PER];
+                    E::widen(q[j], z);
 #pragma unroll
-                for (int i = 0; i < PER; ++i) z[i] = f * (j < KEEP ? e[j < KEEP ? j : 0][i] : shift.power(z[i]));
-                if (inside(j)) __builtin_nontemporal_store(E::narrow(z), vo + j * BLOCK + threadIdx.x);
-            }
-        if (single >= 0) E::store(out + single, f * es);
-        // the token's own element a second time, by the lane that has just stored it
-        const int at = t - c.head;
-        if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
-            E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
+                    for (int i = 0; i < PER; ++i) z[i] = f * (j < KEEP ? e[j < KEEP ? j : 0][i] : shift.power(z[i]));
+                    if (inside(j)) __builtin_nontemporal_store(E::narrow(z), vo + j * BLOCK + threadIdx.x);
+                }
+            if (single >= 0) E::store(out + single, f * es);
+            // the token's own element a second time, by the lane that has just stored it
+            const int at = t - c.head;
+            if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
+                E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
+        }
+        if (meets && threadIdx.x < 64) finish_policy(P.meet, P.stats, P.accumulate);
     }
 }
 
@@ -345,25 +397,43 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
 constexpr int PART_BLOCK = 256;
 constexpr int PART_MIN = 8192;
 constexpr int PARTS = 64;
-constexpr int64_t SPLIT_ROWS = 128;
-constexpr int64_t SPLIT_VOCAB = 40000;
+constexpr int64_t FEW_ROWS = 512;
+constexpr int HELD_MAX = 24 * 1024;          // vectors of the longest row that is held
 
 struct MaxSum {
     float m, s;
 };
+// The row's maximum and sum from those of its parts, one in each lane.  A row of nothing but -inf has a sum of 0 here, from which all
+// is NaN as well.
+__device__ __forceinline__ MaxSum join_parts(MaxSum a, float k)
+{
+    const float m = wave_join<true>(a.m), base = m == -INFINITY ? 0.0f : m;
+    return {m, wave_join<false>(a.s * __builtin_amdgcn_exp2f((a.m - base) * k))};
+}
 
 // The part's maximum and its sum of exp2(k (z - maximum)).  Read again afterwards, so the lines stay in the caches.  A row has one
 // entry more than parts: the token's own logit, which a gradient written in place would not leave for the others to read.
-template <typename E>
-__global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int parts, int len, float k, const float *weights, MaxSum *partials)
+//   FINISH: the last of a row's workgroups also joins them, for a log-probability with no gradient after it
+struct Finish {
+    Meeting meet;
+    float it;
+    float *logp, *row_stats;
+};
+template <typename E, bool FINISH>
+__global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int parts, int len, float k, const float *weights, MaxSum *partials, Finish F)
 {
     constexpr int NV = PART_MIN / PART_BLOCK / E::PER, NW = PART_BLOCK / 64;
     __shared__ float lds_m[NW], lds_s[NW];
     const uint32_t which = blockIdx.x / (uint32_t)parts, part = blockIdx.x - which * (uint32_t)parts;
     const int64_t r = row0 + which;
     const int t = target_of(L, r);
-    if (t < 0 || weight_of(weights, r) == 0.0f) return;
-    partials += (int64_t)which * (parts + 1);
+    if (t < 0 || weight_of(weights, r) == 0.0f) {
+        if (FINISH && part == 0 && threadIdx.x == 0) {
+            F.logp[r] = 0.0f;
+            if (F.row_stats) F.row_stats[2 * r] = 0.0f, F.row_stats[2 * r + 1] = 1.0f;
+        }
+        return;
+    }
     const int from = (int)part * len, n = min(len, L.vocab - from);
     const typename E::T *row = static_cast<const typename E::T *>(L.x) + r * L.stride + from;
     const Cut c = Cut::of<E::PER>(row, n, true);
@@ -403,43 +473,49 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
     m = of_lane(row_join<true>(ml), 0);
     const float base = m == -INFINITY ? 0.0f : m;
     s = of_lane(row_join<false>(lane < NW ? sl * __builtin_amdgcn_exp2f((ml - base) * k) : 0.0f), 0);
-    if (threadIdx.x == 0) {
+    if constexpr (FINISH) {
+        if (threadIdx.x >= 64) return;
+        F.meet.slots += (int64_t)which * parts * 2;
+        const uint32_t mine[2] = {__float_as_uint(m), __float_as_uint(s)};
+        if (threadIdx.x == 0) leave(F.meet, (int)part, mine);
+        const float zt = E::load(row + t - from);
+        if (!last_of<2>(F.meet)) return;
+        MaxSum a = {-INFINITY, 0.0f};
+        if (lane < parts) a = {__uint_as_float(left<2>(F.meet, lane, 0)), __uint_as_float(left<2>(F.meet, lane, 1))};
+        clear<2>(F.meet);
+        a = join_parts(a, k);
+        if (lane == 0) {
+            F.logp[r] = (zt - a.m) * F.it - logf(a.s);
+            if (F.row_stats) F.row_stats[2 * r] = a.m, F.row_stats[2 * r + 1] = a.s;
+        }
+    } else if (threadIdx.x == 0) {
+        partials += (int64_t)which * (parts + 1);
         partials[part] = {m, s};
         if (t >= from && t < from + n) partials[parts].m = E::load(row + t - from);
     }
 }
 
-// The row's maximum and sum from those of its parts.  A row of nothing but -inf has a sum of 0 here, from which all is NaN as well.
 __device__ __forceinline__ MaxSum joined(const MaxSum *partials, int parts, float k)
 {
     const int lane = threadIdx.x & 63;
-    const MaxSum a = lane < parts ? partials[lane] : MaxSum{-INFINITY, 0.0f};
-    MaxSum j;
-    j.m = wave_join<true>(a.m);
-    const float base = j.m == -INFINITY ? 0.0f : j.m;
-    j.s = wave_join<false>(a.s * __builtin_amdgcn_exp2f((a.m - base) * k));
-    return j;
+    return join_parts(lane < parts ? partials[lane] : MaxSum{-INFINITY, 0.0f}, k);
 }
 
-// Log-probabilities of rows in parts, a wave each.
+// Log-probabilities of rows in parts whose gradient is not asked for, a wave each.
 __global__ __launch_bounds__(PART_BLOCK) void k_join(Logits L, int64_t row0, int rows, int parts, float k, float it, const float *weights,
-                                                     const MaxSum *partials, float *logp, float *row_stats)
+                                                     const MaxSum *partials, float *logp)
 {
     const int which = (int)blockIdx.x * (PART_BLOCK / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (which >= rows) return;
     const int64_t r = row0 + which;
     const int t = target_of(L, r);
-    MaxSum a = {0.0f, 1.0f};
     float lp = 0.0f;
     if (t >= 0 && weight_of(weights, r) != 0.0f) {
         partials += (int64_t)which * (parts + 1);
-        a = joined(partials, parts, k);
+        const MaxSum a = joined(partials, parts, k);
         lp = (partials[parts].m - a.m) * it - logf(a.s);
     }
-    if ((threadIdx.x & 63) == 0) {
-        logp[r] = lp;
-        if (row_stats) row_stats[2 * r] = a.m, row_stats[2 * r + 1] = a.s;
-    }
+    if ((threadIdx.x & 63) == 0) logp[r] = lp;
 }
 
 // ---- gradient of rows whose maximum and sum are known -------------------------------------------
@@ -476,13 +552,23 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
     if constexpr (FROM_PARTS) {
         const float w = weight_of(A.P.weights, r);
         float lp = 0.0f;
+        Sums sums = {};
         if (t >= 0 && w != 0.0f) {
+            const Token token = token_of(A.P, r);
             const MaxSum *partials = A.partials + (int64_t)which * (A.parts + 1);
             a = joined(partials, A.parts, A.P.k);
             lp = (partials[A.parts].m - a.m) * A.P.it - logf(a.s);
-            d = w * policy_terms(lp, r, A.P).slope * A.P.it;
+            const Terms terms = policy_terms(lp, token, A.P);
+            sums = sums_of(terms, w, A.P.kl);
+            d = w * terms.slope * A.P.it;
         }
-        if (run == 0 && threadIdx.x == 0) A.logp[r] = lp;
+        if (run == 0 && threadIdx.x < 64) {
+            if (threadIdx.x == 0) A.logp[r] = lp;
+            if (A.P.meet.n > 0) {
+                if (threadIdx.x == 0) leave_sums(A.P.meet, r, sums);
+                finish_policy(A.P.meet, A.P.stats, A.P.accumulate);
+            }
+        }
     } else if (t >= 0) {
         d = A.dlogp[r] * A.P.it;
         a = {A.row_stats[2 * r], A.row_stats[2 * r + 1]};
@@ -529,7 +615,7 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
 #pragma unroll
             for (int e = 0; e < PER; ++e) z[e] = f * shift.power(z[e]);
         }
-        __builtin_nontemporal_store(E::narrow(z), vo + i);
+        store_through(vo + i, E::narrow(z));
     }
     if (single >= 0) {
         const float p = __builtin_amdgcn_exp2f((E::load(row + single) - a.m) * A.P.k) / a.s;
@@ -572,12 +658,9 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *target
         const float w = weight_of(P.weights, r);
         const int64_t t = targets[r];
         if (t < 0 || t >= vocab || w == 0.0f) continue;
-        const Terms e = policy_terms(logp[r], r, P);
-        const double pg = (double)w * e.pg, kl = (double)w * e.kl;
-        x[0] += P.kl != 0.0f ? pg + P.kl * kl : pg;
-        x[1] += pg;
-        x[2] += kl;
-        x[3] += e.clipped ? (double)w : 0.0;
+        const Sums e = sums_of(policy_terms(logp[r], token_of(P, r), P), w, P.kl);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] += e.x[q];
     }
     finish_sums<4, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
 }
@@ -590,6 +673,9 @@ struct Pairs {
     int64_t tokens, pairs;
     float beta, smoothing, scale;
     float *margins, *dlogp;
+    Meeting meet;                 // of a launch with few pairs
+    float *loss;
+    int accumulate;
 };
 __device__ __forceinline__ int64_t offset_of(const Pairs &A, int64_t s)
 {
@@ -600,8 +686,8 @@ __device__ __forceinline__ double log_ratio_sum(const Pairs &A, int64_t from, in
 {
     double x = 0.0;
     for (int64_t i = from + threadIdx.x; i < to; i += PAIR_BLOCK) {
-        const float w = weight_of(A.weights, i);
-        if (w != 0.0f) x += (double)w * ((double)A.logp[i] - (A.ref_logp ? (double)A.ref_logp[i] : 0.0));
+        const float w = weight_of(A.weights, i), lp = A.logp[i], ref = A.ref_logp ? A.ref_logp[i] : 0.0f;
+        x += w != 0.0f ? (double)w * ((double)lp - (double)ref) : 0.0;
     }
     return x;
 }
@@ -614,6 +700,12 @@ __device__ __forceinline__ void spread(const Pairs &A, int64_t from, int64_t to,
 }
 // ln(1 + exp(x))
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+// A pair's loss from its margin as it is given out, in 32 bits: its relative error from that is at most that of the margin.
+__device__ __forceinline__ double pair_loss(float margin, float smoothing, float scale)
+{
+    const double h = margin, e = smoothing;
+    return (double)scale * ((1.0 - e) * softplus(-h) + (e != 0.0 ? e * softplus(h) : 0.0));
+}
 
 // One workgroup a pair.  Both sums are held in 64 bits: a margin is a small difference of sums over thousands of tokens.
 __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
@@ -628,6 +720,11 @@ __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
         const double h = (double)A.beta * (chosen - rejected), e = A.smoothing;
         const double up = 1.0 / (1.0 + exp(-h)), down = 1.0 / (1.0 + exp(h));       // sigmoid(h), sigmoid(-h)
         A.margins[p] = (float)h;
+        if (A.meet.n > 0) {
+            uint32_t w[2];
+            halves(pair_loss((float)h, A.smoothing, A.scale), w[0], w[1]);
+            leave(A.meet, (int)p, w);
+        }
         slope = (float)((double)A.scale * A.beta * (e * up - (1.0 - e) * down));
     }
     __syncthreads();
@@ -635,15 +732,17 @@ __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
     spread(A, b0, b1, -slope);
     if (p == 0) spread(A, 0, offset_of(A, 0), 0.0f);
     if (q + 1 == 2 * A.pairs) spread(A, b1, A.tokens, 0.0f);
+    if (A.meet.n > 0 && threadIdx.x < 64) {
+        if (!last_of<2>(A.meet)) return;
+        double x[1];
+        left_sums(A.meet, x);
+        if (threadIdx.x == 63) *A.loss = (float)((A.accumulate ? (double)*A.loss : 0.0) + x[0]);
+    }
 }
-// The loss from the margins, which are fp32: its relative error from that is at most that of a margin.
 __global__ __launch_bounds__(SUM_BLOCK) void k_pair_sums(const float *margins, int64_t pairs, float smoothing, float scale, double *partials, float *out, int accumulate)
 {
     double x[1] = {};
-    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) {
-        const double h = margins[p], e = smoothing;
-        x[0] += (double)scale * ((1.0 - e) * softplus(-h) + (e != 0.0 ? e * softplus(h) : 0.0));
-    }
+    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) x[0] += pair_loss(margins[p], smoothing, scale);
     finish_sums<1, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
 }
 __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
@@ -665,27 +764,36 @@ struct RowShape {
     RowKernel kernel;
     int block;
 };
-// The kernel for rows of up to `vecs` vectors, counted from the start of the first one's line: the least that holds one, or none.
+// The kernel for rows of up to `vecs` vectors: the least that holds one.
 template <typename E, bool POLICY>
 static RowShape row_shape(int64_t vecs)
 {
-    // KEEP: as many as there is room for in a workgroup's share of the registers; an fp32 vector takes as much as its exponentials
 #define GS_HELD(BLOCK, NV, LO, KEEP) \
-    if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, !POLICY ? 0 : E::PER == 4 ? NV : KEEP, POLICY>, BLOCK}
-    GS_HELD(64, 4, 0, 4);
-    GS_HELD(128, 4, 1, 4);
-    GS_HELD(256, 4, 1, 4);
-    GS_HELD(512, 4, 1, 4);
-    GS_HELD(1024, 3, 1, 3);
-    GS_HELD(1024, 4, 2, 4);
-    GS_HELD(1024, 6, 3, 6);
-    GS_HELD(1024, 8, 5, 8);
-    GS_HELD(1024, 12, 7, 12);
-    GS_HELD(1024, 16, 11, 8);
-    GS_HELD(1024, 20, 15, 4);
-    GS_HELD(1024, 24, 19, 0);
+    if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, KEEP, POLICY>, BLOCK}
+    GS_HELD(64, 4, 0, POLICY ? 4 : 0);
+    GS_HELD(128, 4, 1, POLICY ? 4 : 0);
+    GS_HELD(256, 4, 1, POLICY ? 4 : 0);
+    if constexpr (POLICY) {
+        // wide workgroups: half the registers a wave
+        GS_HELD(512, 4, 1, 4);
+        GS_HELD(1024, 3, 1, 3);
+        GS_HELD(1024, 4, 2, 4);
+        GS_HELD(1024, 6, 3, 6);
+        GS_HELD(1024, 8, 5, 8);
+    } else {
+        GS_HELD(256, 8, 3, 0);
+        GS_HELD(512, 6, 3, 0);
+        GS_HELD(512, 8, 5, 0);
+        GS_HELD(512, 12, 7, 0);
+        GS_HELD(512, 16, 11, 0);
+    }
+    // KEEP: as many as there is room for in a workgroup's share of the registers; an fp32 vector takes as much as its exponentials
+    constexpr bool ALL = E::PER == 4;
+    GS_HELD(1024, 12, 7, !POLICY ? 0 : 12);
+    GS_HELD(1024, 16, 11, !POLICY ? 0 : ALL ? 16 : 8);
+    GS_HELD(1024, 20, 15, !POLICY ? 0 : ALL ? 20 : 4);
 #undef GS_HELD
-    return {nullptr, 0};
+    return {k_held<E, 1024, HELD_MAX / 1024, 19, POLICY && E::PER == 4 ? HELD_MAX / 1024 : 0, POLICY>, 1024};
 }
 
 struct Grid {
@@ -699,12 +807,28 @@ static Grid parts_of(const gs_logits &X)
     const int64_t len = (X.vocab + PARTS - 1) / PARTS;
     g.len = (int)(len <= PART_MIN ? PART_MIN : (len + PART_MIN - 1) / PART_MIN * PART_MIN);
     g.parts = (int)((X.vocab + g.len - 1) / g.len);
-    g.rows = GS_SQNORM_MAX_BLOCKS / (g.parts + 1);
+    g.rows = GS_SQNORM_MAX_BLOCKS / (2 * g.parts);      // a slot has 16 bytes a part, a row of partials 8 and 8 more
     return g;
 }
-static bool in_parts(const gs_logits &X)
+// Vectors of a row from the start of its first one's line on.  Rows that start on a line each have none missing there.
+static int64_t vecs_of(const gs_logits &X)
 {
-    return X.rows <= SPLIT_ROWS && X.vocab > SPLIT_VOCAB;
+    const bool on_lines = (reinterpret_cast<uintptr_t>(X.data) & 127) == 0 && (X.rows == 1 || X.row_stride % (X.dtype == GS_BF16 ? 64 : 32) == 0);
+    return X.vocab / (X.dtype == GS_BF16 ? Bf16::PER : F32::PER) + (on_lines ? 0 : 7);
+}
+// Whether rows go in parts though they could be held: a long row takes one CU's share of the memory's rate, unless there are about as many
+// rows as CUs.  One launch against one without a gradient, two with one.  us, held against parts, bf16:
+//   rows              1           16           64           128          256
+//   65536, scored     6.1/4.3     6.7/5.7      6.9/6.6      7.2/7.9      8.7/10.5
+//   131072, scored    8.8/4.3     9.7/5.1      10.1/8.2     11.6/10.7    17.9/17.0
+//   65536, policy     7.6/6.5     8.1/7.8      8.4/10.7     9.7/14.0
+//   131072, policy    12.7/6.6    13.4/8.5     13.9/13.8    16.7/21.0
+// (32000: scored 4.4/3.8 with one row and 4.8/4.8 with 16, policy 5.5/6.4.)
+static bool in_parts(const gs_logits &X, bool gradient)
+{
+    const int64_t vecs = vecs_of(X);
+    if (vecs > HELD_MAX) return true;
+    return X.rows <= (vecs > 12 * 1024 ? (gradient ? 64 : 256) : vecs > 5000 ? (gradient ? 16 : 64) : 0);
 }
 
 template <typename E>
@@ -732,9 +856,15 @@ static hipError_t launch_in_parts(const gs_logits &X, const Logits &L, const Pol
     const Grid g = parts_of(X);
     for (int64_t r = 0; r < X.rows; r += g.rows) {
         const int rows = (int)(X.rows - r < g.rows ? X.rows - r : g.rows);
-        k_part<E><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, P.weights, partials);
+        if (!POLICY) {
+            const Finish F = {{reinterpret_cast<uint64_t *>(partials), next_tag(), g.parts}, P.it, logp, row_stats};
+            k_part<E, true><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, nullptr, nullptr, F);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            continue;
+        }
+        k_part<E, false><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, P.weights, partials, Finish{});
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if (POLICY && dlogits) {
+        if (dlogits) {
             const GradArgs A = {L, r, rows, dstride, P, nullptr, nullptr, partials, logp, dlogits, 0, g.parts};
             // a launch takes as many rows as it can, and joins the partials of its own from the first on: no more than those
             const int64_t most = kMaxItems / GRAD_BLOCK / grad_runs<E>(X.vocab);
@@ -745,7 +875,7 @@ static hipError_t launch_in_parts(const gs_logits &X, const Logits &L, const Pol
                 if (hipError_t e = launch_grad<E, true>(B, rows - q < most ? rows - q : most, stream); e != hipSuccess) return e;
             }
         } else {
-            k_join<<<(rows + PART_BLOCK / 64 - 1) / (PART_BLOCK / 64), PART_BLOCK, 0, stream>>>(L, r, rows, g.parts, P.k, P.it, P.weights, partials, logp, row_stats);
+            k_join<<<(rows + PART_BLOCK / 64 - 1) / (PART_BLOCK / 64), PART_BLOCK, 0, stream>>>(L, r, rows, g.parts, P.k, P.it, P.weights, partials, logp);
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         }
     }
@@ -756,11 +886,8 @@ template <typename E, bool POLICY>
 static hipError_t launch_rows_of(const gs_logits &X, const Logits &L, const Policy &P, float *logp, float *row_stats, void *dlogits, int64_t dstride, void *ws,
                                  hipStream_t stream)
 {
-    // rows that all start on a line have no vectors missing from their first one
-    constexpr int64_t LINE = 128 / sizeof(typename E::T);
-    const bool on_lines = (reinterpret_cast<uintptr_t>(X.data) & 127) == 0 && (X.rows == 1 || X.row_stride % LINE == 0);
-    const RowShape s = row_shape<E, POLICY>(X.vocab / E::PER + (on_lines ? 0 : 7));
-    if (!s.kernel || in_parts(X)) return launch_in_parts<E, POLICY>(X, L, P, logp, row_stats, dlogits, dstride, static_cast<MaxSum *>(ws), stream);
+    if (in_parts(X, POLICY)) return launch_in_parts<E, POLICY>(X, L, P, logp, row_stats, dlogits, dstride, static_cast<MaxSum *>(ws), stream);
+    const RowShape s = row_shape<E, POLICY>(vecs_of(X));
     // with the row statistics asked for, the rows are read again for a gradient: what the memory-side cache holds is left there
     const int64_t kept = GS_KEEP_BYTES / (L.stride * (int64_t)sizeof(typename E::T)), keep_row = row_stats ? X.rows - kept : INT64_MAX;
     const int64_t most = kMaxItems / s.block;
@@ -827,7 +954,7 @@ static bool good_workspace(const void *ws, size_t bytes) { return ws && bytes >=
 
 static Logits logits_of(const gs_logits &x, const int64_t *targets)
 {
-    return {x.data, x.rows > 1 ? x.row_stride : x.vocab, targets, (int)x.vocab};
+    return {x.data, x.rows > 1 ? x.row_stride : x.vocab, targets, (int)x.vocab, x.rows <= FEW_ROWS};
 }
 static Policy scaled_by(float temperature)
 {
@@ -919,8 +1046,14 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     P.ref_logp = ref_logp;
     P.advantages = advantages;
     P.weights = weights;
+    P.stats = d_stats;
+    P.accumulate = accumulate;
+    // with few rows the last of them adds up their sums; the workspace's end is theirs, its start holds parts
+    const bool meets = rows > 0 && rows <= MEET_MAX && (dlogits || !in_parts(*logits, true));
+    if (meets) P.meet = {reinterpret_cast<uint64_t *>(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_MAX * 64), next_tag(), (int)rows};
     hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, d_workspace, st);
     if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
+    if (meets) return GS_OK;
     const int blocks = sum_blocks(rows);
     double *partials = static_cast<double *>(d_workspace);
     k_policy_sums<<<blocks, SUM_BLOCK, 0, st>>>(targets, (int)logits->vocab, rows, P, logp, partials, d_stats, accumulate);
@@ -948,12 +1081,13 @@ gs_status gs_preference_loss(const float *logp, const float *ref_logp, const flo
     if (pairs == 0 && tokens == 0 && accumulate) return GS_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (pairs) {
-        const Pairs A = {logp, ref_logp, weights, offsets, tokens, pairs, hp->beta, hp->label_smoothing, hp->scale, margins, dlogp};
+        Pairs A = {logp, ref_logp, weights, offsets, tokens, pairs, hp->beta, hp->label_smoothing, hp->scale, margins, dlogp, {}, d_loss, accumulate};
+        if (pairs <= MEET_MAX) A.meet = {static_cast<uint64_t *>(d_workspace), next_tag(), (int)pairs};
         k_pairs<<<(int)pairs, PAIR_BLOCK, 0, st>>>(A);
     } else if (tokens) {
         k_zero<<<sum_blocks(tokens), SUM_BLOCK, 0, st>>>(dlogp, tokens);
     }
-    if (!(pairs == 0 && accumulate)) {
+    if (pairs > MEET_MAX || (pairs == 0 && !accumulate)) {
         const int blocks = sum_blocks(pairs);
         double *partials = static_cast<double *>(d_workspace);
         k_pair_sums<<<blocks, SUM_BLOCK, 0, st>>>(margins, pairs, hp->label_smoothing, hp->scale, partials, d_loss, accumulate);

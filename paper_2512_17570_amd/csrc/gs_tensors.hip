@@ -17,38 +17,78 @@
 
 namespace gs {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TENSOR_BLOCK = 256;
-constexpr int TABLE = 120;             // tensors of one launch: 3848 of the 4096 bytes that a launch's arguments may have
+constexpr int TABLE = 128;             // tensors of one launch: 3600 of the 4096 bytes that a launch's arguments may have
+constexpr int TABLE_SMALL = 16;
 
 struct Entry {
     const void *in;
     void *out;
     int64_t numel;
-    uint32_t first;                    // its first tile, of this launch's
     int32_t dtype;
+    uint32_t first;                    // its first tile, of this launch's
 };
-struct Table {
-    int32_t count;
-    uint32_t tile_vecs;                // 16-byte vectors of a tile
-    Entry e[TABLE];
+// First tiles beside each other, so that looking for a tile's tensor takes few lines of memory; ~0 behind the last tensor.
+template <int N> struct Table {
+    uint32_t first[N];
+    uint32_t tiles, keep_tile;         // norm: tiles from this one on are left in the memory-side cache, for the clip
+    int32_t count, runs;               // runs: of NV vectors a lane, one after another in a tile
+    struct {
+        const void *in;
+        void *out;
+        int64_t numel_bf16;            // elements, twice, and 1 for bf16
+    } e[N];
 };
 
-// The tensor that a tile belongs to: the last one whose first tile is not behind it.  Every lane looks at two of them.
-__device__ __forceinline__ int tensor_of(const Table &t, uint32_t tile)
+// The tensor that a tile belongs to: the last one whose first tile is not behind it.  A short list is gone through by the scalar unit, of
+// a long one every lane looks at two.
+template <int N>
+__device__ __forceinline__ Entry entry_of(const Table<N> &t, uint32_t tile)
 {
-    const int lane = threadIdx.x & 63;
-    const int a = __popcll(__ballot(lane < t.count && t.e[lane].first <= tile));
-    const int b = __popcll(__ballot(lane + 64 < t.count && t.e[lane + 64 < TABLE ? lane + 64 : 0].first <= tile));
-    return __builtin_amdgcn_readfirstlane(a + b - 1);
+    int n = 0;
+    if constexpr (N <= TABLE_SMALL) {
+#pragma unroll
+        for (int i = 1; i < N; ++i) n += t.first[i] <= tile ? 1 : 0;
+    } else {
+        static_assert(N == 128, "two for each lane");
+        const int lane = threadIdx.x & 63;
+        n = __popcll(__ballot(t.first[lane] <= tile)) + __popcll(__ballot(t.first[lane + 64] <= tile)) - 1;
+        n = __builtin_amdgcn_readfirstlane(n);
+    }
+    const auto &e = t.e[n];
+    return {e.in, e.out, e.numel_bf16 >> 1, e.numel_bf16 & 1 ? GS_BF16 : GS_F32, t.first[n]};
 }
 
-__device__ __forceinline__ void square(u32x4 q, bool bf16, double &x, double &y)
+// A tile's part of a tensor: the vectors [at, end) behind `head` single elements, counted from the start of the first one's 128-byte line
+// (`skip` of that line are not the tensor's), and whether it has the single ones of both ends (the tensor's first tile does).
+struct Part {
+    int64_t at, end, rest;             // rest: elements from the first of them behind the vectors
+    int skip, head, singles;
+};
+template <int PER>
+__device__ __forceinline__ Part part_of(const Entry &e, const void *p, uint32_t tile, uint32_t tile_vecs)
+{
+    Part c;
+    const int64_t off = ((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (16 / PER);
+    c.head = (int)(off < e.numel ? off : e.numel);
+    const int64_t vecs = (e.numel - c.head) / PER;
+    c.skip = (int)((reinterpret_cast<uintptr_t>(p) + 15) >> 4) & 7;
+    c.at = (int64_t)(tile - e.first) * tile_vecs;
+    c.end = c.skip + vecs;
+    c.rest = c.head + vecs * PER;
+    c.singles = tile == e.first ? c.head + (int)(e.numel - c.rest) : 0;          // at most 14
+    return c;
+}
+__device__ __forceinline__ int64_t single(const Part &c, int i) { return i < c.head ? i : c.rest + (i - c.head); }
+
+template <int PER>
+__device__ __forceinline__ void square(u32x4 q, double &x, double &y)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (bf16) {
+        if constexpr (PER == 8) {
             const double lo = bf16_lo(q[i]), hi = bf16_hi(q[i]);
             x = fma(lo, lo, x);
             y = fma(hi, hi, y);
@@ -59,122 +99,183 @@ __device__ __forceinline__ void square(u32x4 q, bool bf16, double &x, double &y)
         }
     }
 }
-
-// A tile's part of a tensor: whole aligned vectors [v0, v1) behind `head` single elements, and whether it has the single ones
-// of both ends (the tensor's first tile does).
-struct Part {
-    int64_t v0, v1;
-    int head, singles;
-};
-__device__ __forceinline__ Part part_of(const Table &t, const Entry &e, const void *aligned_for, bool vectors, uint32_t tile)
+template <int PER> __device__ __forceinline__ float load_one(const void *p, int64_t i)
 {
-    const int size = e.dtype == GS_BF16 ? 2 : 4, per = 16 / size;
-    Part p;
-    const int64_t off = ((16 - (reinterpret_cast<uintptr_t>(aligned_for) & 15)) & 15) / size;
-    const int64_t head = vectors ? (off < e.numel ? off : e.numel) : 0;
-    const int64_t vecs = vectors ? (e.numel - head) / per : 0;
-    p.head = (int)head;
-    p.v0 = (int64_t)(tile - e.first) * t.tile_vecs;
-    p.v1 = p.v0 + t.tile_vecs < vecs ? p.v0 + t.tile_vecs : vecs;
-    p.singles = tile == e.first ? (int)(e.numel - vecs * per) : 0;
-    return p;
+    if constexpr (PER == 8) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
+    else return static_cast<const float *>(p)[i];
 }
 
-__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table t, double *partials)
+template <int PER, int NV, bool KEEP>
+__device__ __forceinline__ double tile_squares(const Entry &e, uint32_t tile, int runs)
+{
+    const Part c = part_of<PER>(e, e.in, tile, (uint32_t)(TENSOR_BLOCK * NV) * runs);
+    const u32x4 *v = reinterpret_cast<const u32x4 *>(static_cast<const char *>(e.in) + c.head * (16 / PER)) - c.skip + c.at;
+    int64_t from = c.skip - c.at, to = c.end - c.at;               // of the tile's vectors
+    double x = 0.0, y = 0.0;
+    if ((int)threadIdx.x < c.singles) {
+        const double g = load_one<PER>(e.in, single(c, threadIdx.x));
+        x = g * g;
+    }
+    for (int run = 0; run < runs && to > 0; ++run, v += TENSOR_BLOCK * NV, from -= TENSOR_BLOCK * NV, to -= TENSOR_BLOCK * NV) {
+        u32x4 q[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = j * TENSOR_BLOCK + (int)threadIdx.x;
+            q[j] = u32x4{0, 0, 0, 0};
+            if (i >= from && i < to) q[j] = KEEP ? v[i] : __builtin_nontemporal_load(v + i);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) square<PER>(q[j], x, y);
+    }
+    return x + y;
+}
+
+template <int N, int NV>
+__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, double *partials, Meeting meet, double *out, int accumulate)
 {
     __shared__ double lds[TENSOR_BLOCK / 64];
-    const Entry &e = t.e[tensor_of(t, blockIdx.x)];
-    const Part p = part_of(t, e, e.in, true, blockIdx.x);
-    const bool bf16 = e.dtype == GS_BF16;
-    const int size = bf16 ? 2 : 4, per = 16 / size;
-    const char *base = static_cast<const char *>(e.in);
-    const u32x4 *v = reinterpret_cast<const u32x4 *>(base + p.head * size);
-    double x = 0.0, y = 0.0;
-    for (int64_t i = p.v0 + threadIdx.x; i < p.v1; i += TENSOR_BLOCK) square(v[i], bf16, x, y);
-    if ((int)threadIdx.x < p.singles) {                // at most 14
-        const int64_t vecs = (e.numel - p.head) / per, i = (int)threadIdx.x < p.head ? (int64_t)threadIdx.x : threadIdx.x + vecs * per;
-        const double g = bf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(base)[i] << 16) : reinterpret_cast<const float *>(base)[i];
-        x = fma(g, g, x);
+    const uint32_t tile = blockIdx.x;
+    const Entry e = entry_of(t, tile);
+    double x;
+    if (e.dtype == GS_BF16) x = tile < t.keep_tile ? tile_squares<8, NV, false>(e, tile, t.runs) : tile_squares<8, NV, true>(e, tile, t.runs);
+    else x = tile < t.keep_tile ? tile_squares<4, NV, false>(e, tile, t.runs) : tile_squares<4, NV, true>(e, tile, t.runs);
+    const double s = block_sum<TENSOR_BLOCK>(x, lds);
+    if (meet.n == 0) {
+        if (threadIdx.x == 0) partials[tile] = s;
+        return;
     }
-    const double s = block_sum<TENSOR_BLOCK>(x + y, lds);
-    if (threadIdx.x == 0) partials[blockIdx.x] = s;
+    if (threadIdx.x >= 64) return;
+    if (threadIdx.x == 0) {
+        uint32_t w[2];
+        halves(s, w[0], w[1]);
+        leave(meet, (int)tile, w);
+    }
+    if (!last_of<2>(meet)) return;
+    double all[1];
+    left_sums(meet, all);
+    if (threadIdx.x == 63) *out = accumulate ? *out + all[0] : all[0];
 }
 
-// Where the coefficient is 1, tensors that stay where they are are left alone.
-__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_clip(Table t, const double *d_sqnorm, float max_norm, float *d_norm)
+template <int PER> __device__ __forceinline__ u32x4 scaled(u32x4 q, float c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (PER == 8) {                     // rounded to nearest even, NaN stays NaN
+            const bf16x2 h = {(__bf16)(c * bf16_lo(q[i])), (__bf16)(c * bf16_hi(q[i]))};
+            q[i] = __builtin_bit_cast(uint32_t, h);
+        } else {
+            q[i] = __float_as_uint(c * __uint_as_float(q[i]));
+        }
+    }
+    return q;
+}
+
+template <int PER, int NV>
+__device__ __forceinline__ void tile_scaled(const Entry &e, uint32_t tile, int runs, float c)
+{
+    const int64_t tile_vecs = (int64_t)(TENSOR_BLOCK * NV) * runs;
+    auto one = [&](int64_t i) {
+        const float g = c * load_one<PER>(e.in, i);
+        if constexpr (PER == 8) static_cast<uint16_t *>(e.out)[i] = (uint16_t)f32_to_bf16_bits(g);
+        else static_cast<float *>(e.out)[i] = g;
+    };
+    if (((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15) != 0) {      // no vectors in common
+        const int64_t a = (int64_t)(tile - e.first) * tile_vecs * PER, b = a + tile_vecs * PER;
+        for (int64_t i = a + threadIdx.x; i < b && i < e.numel; i += TENSOR_BLOCK) one(i);
+        return;
+    }
+    const Part p = part_of<PER>(e, e.in, tile, (uint32_t)tile_vecs);
+    const int64_t shift = p.at - p.skip;
+    int64_t from = p.skip - p.at, to = p.end - p.at;
+    const u32x4 *vi = reinterpret_cast<const u32x4 *>(static_cast<const char *>(e.in) + p.head * (16 / PER)) + shift;
+    u32x4 *vo = reinterpret_cast<u32x4 *>(static_cast<char *>(e.out) + p.head * (16 / PER)) + shift;
+    for (int run = 0; run < runs && to > 0; ++run, vi += TENSOR_BLOCK * NV, vo += TENSOR_BLOCK * NV, from -= TENSOR_BLOCK * NV, to -= TENSOR_BLOCK * NV) {
+        u32x4 q[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = j * TENSOR_BLOCK + (int)threadIdx.x;
+            if (i >= from && i < to) q[j] = __builtin_nontemporal_load(vi + i);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = j * TENSOR_BLOCK + (int)threadIdx.x;
+            if (i >= from && i < to) store_through(vo + i, scaled<PER>(q[j], c));
+        }
+    }
+    if ((int)threadIdx.x < p.singles) one(single(p, threadIdx.x));
+}
+
+// From the last tile on: the end of what the norm read is still in the memory-side cache.  Where the coefficient is 1, tensors
+// that stay where they are are left alone.
+template <int N, int NV>
+__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_clip(Table<N> t, const double *d_sqnorm, float max_norm, float *d_norm)
 {
     const double S = *d_sqnorm;
     if (d_norm && blockIdx.x == 0 && threadIdx.x == 0) *d_norm = (float)sqrt(S);
     if (t.count == 0) return;
+    const uint32_t tile = t.tiles - 1 - blockIdx.x;
+    const Entry e = entry_of(t, tile);
     const float c = clip_from(S, max_norm);
-    const Entry &e = t.e[tensor_of(t, blockIdx.x)];
     if (c == 1.0f && e.out == e.in) return;
-    const bool bf16 = e.dtype == GS_BF16;
-    const int size = bf16 ? 2 : 4, per = 16 / size;
-    // without a common alignment, element by element
-    const bool same = ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15) == 0;
-    const char *in = static_cast<const char *>(e.in);
-    char *out = static_cast<char *>(e.out);
-    auto one = [&](int64_t i) {
-        if (bf16) reinterpret_cast<uint16_t *>(out)[i] = (uint16_t)f32_to_bf16_bits(c * __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(in)[i] << 16));
-        else reinterpret_cast<float *>(out)[i] = c * reinterpret_cast<const float *>(in)[i];
-    };
-    if (!same) {
-        const int64_t a = (int64_t)(blockIdx.x - e.first) * t.tile_vecs * per, b = a + (int64_t)t.tile_vecs * per;
-        for (int64_t i = a + threadIdx.x; i < b && i < e.numel; i += TENSOR_BLOCK) one(i);
-        return;
-    }
-    const Part p = part_of(t, e, e.in, true, blockIdx.x);
-    const u32x4 *vi = reinterpret_cast<const u32x4 *>(in + p.head * size);
-    u32x4 *vo = reinterpret_cast<u32x4 *>(out + p.head * size);
-    for (int64_t i = p.v0 + threadIdx.x; i < p.v1; i += TENSOR_BLOCK) {
-        u32x4 q = vi[i];
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            q[w] = bf16 ? f32_to_bf16_bits(c * bf16_lo(q[w])) | f32_to_bf16_bits(c * bf16_hi(q[w])) << 16 : __float_as_uint(c * __uint_as_float(q[w]));
-        vo[i] = q;
-    }
-    if ((int)threadIdx.x < p.singles) {
-        const int64_t vecs = (e.numel - p.head) / per;
-        one((int)threadIdx.x < p.head ? (int64_t)threadIdx.x : threadIdx.x + vecs * per);
-    }
+    if (e.dtype == GS_BF16) tile_scaled<8, NV>(e, tile, t.runs, c);
+    else tile_scaled<4, NV>(e, tile, t.runs, c);
 }
 
 // ---- launchers --------------------------------------------------------------------------------
+constexpr int NORM_NV = 4, CLIP_NV = 2;              // vectors of a lane
 static int64_t size_of(const gs_tensor &t) { return t.dtype == GS_BF16 ? 2 : 4; }
-
-// Vectors of a tile so that all tiles together leave no more partials than the workspace holds: every tensor may have one that
-// is not full.
-static uint32_t tile_vecs_for(const gs_tensor *tensors, int64_t count)
+// tiles of a tensor: its vectors counted from the start of the first one's line
+static uint32_t tiles_of(const gs_tensor &t, int64_t tile_vecs)
 {
-    int64_t vecs = 0;
-    for (int64_t i = 0; i < count; ++i) vecs += tensors[i].numel / (16 / size_of(tensors[i])) + 1;
-    uint32_t tile = TENSOR_BLOCK * 8;
-    while (vecs / tile + count > GS_SQNORM_MAX_BLOCKS) tile *= 2;
-    return tile;
+    return (uint32_t)((t.numel / (16 / size_of(t)) + 7) / tile_vecs + 1);
+}
+static uint64_t tiles_of(const gs_tensor *t, int64_t count, int64_t tile_vecs)
+{
+    uint64_t n = 0;
+    for (int64_t i = 0; i < count; ++i) n += t[i].numel ? tiles_of(t[i], tile_vecs) : 0;
+    return n;
 }
 
-// Calls launch(table, tiles) for tables that hold all tensors between them.
-template <typename F>
-static hipError_t for_tables(const gs_tensor *tensors, int64_t count, uint32_t tile_vecs, F launch)
+// Runs of a tile so that there are no more than `most` tiles.
+static int runs_for(const gs_tensor *t, int64_t count, int nv, uint64_t most)
 {
-    Table t;
-    t.count = 0;
-    t.tile_vecs = tile_vecs;
-    uint32_t tiles = 0;
-    for (int64_t i = 0; i < count; ++i) {
-        const gs_tensor &x = tensors[i];
-        if (x.numel == 0) continue;
-        const int64_t per_tile = (int64_t)tile_vecs * (16 / size_of(x));
-        t.e[t.count++] = {x.data, x.out ? x.out : const_cast<void *>(x.data), x.numel, tiles, x.dtype};
-        tiles += (uint32_t)((x.numel + per_tile - 1) / per_tile);
-        if (t.count == TABLE) {
-            if (hipError_t e = launch(t, tiles); e != hipSuccess) return e;
-            t.count = 0;
-            tiles = 0;
+    int runs = 1;
+    while (tiles_of(t, count, (int64_t)TENSOR_BLOCK * nv * runs) > most) runs *= 2;
+    return runs;
+}
+
+// Calls launch(table) for tables of up to N tensors that hold all of them between them; `back`: from the last one on.  Bytes of the list
+// from keep_from on are marked to be kept.
+template <int N, typename F>
+static hipError_t for_tables(const gs_tensor *tensors, int64_t count, int nv, int runs, bool back, int64_t keep_from, F launch)
+{
+    const int64_t tile_vecs = (int64_t)TENSOR_BLOCK * nv * runs;
+    Table<N> t;
+    int64_t at = 0;                    // bytes before this tensor
+    for (int64_t left = count; left > 0;) {
+        // the next N tensors with elements, or the last N of those that are left
+        int64_t a = back ? left : count - left, b = a;
+        for (int n = 0; n < N && (back ? a > 0 : b < count); back ? --a : ++b) n += tensors[back ? a - 1 : b].numel != 0;
+        left -= b - a;
+        t.count = 0;
+        t.runs = runs;
+        t.tiles = 0;
+        t.keep_tile = ~0u;
+        for (int64_t i = a; i < b; ++i) {
+            const gs_tensor &x = tensors[i];
+            if (x.numel == 0) continue;
+            const int64_t bytes = x.numel * size_of(x);
+            if (t.keep_tile == ~0u && at + bytes > keep_from) t.keep_tile = t.tiles + (uint32_t)(keep_from > at ? (keep_from - at) / (16 * tile_vecs) : 0);
+            at += bytes;
+            t.first[t.count] = t.tiles;
+            t.e[t.count++] = {x.data, x.out ? x.out : const_cast<void *>(x.data), x.numel * 2 + (x.dtype == GS_BF16)};
+            t.tiles += tiles_of(x, tile_vecs);
         }
+        if (t.count == 0) continue;
+        for (int i = t.count; i < N; ++i) t.first[i] = ~0u;
+        if (hipError_t e = launch(t); e != hipSuccess) return e;
     }
-    return t.count ? launch(t, tiles) : hipSuccess;
+    return hipSuccess;
 }
 
 static bool good_tensors(const gs_tensor *tensors, int64_t count, bool outs)
@@ -224,6 +325,43 @@ static gs_status outputs_apart(const gs_tensor *tensors, int64_t count)
     return good ? GS_OK : GS_ERR_INVALID_ARG;
 }
 
+template <int N>
+static hipError_t norm(const gs_tensor *tensors, int64_t count, double *d_sqnorm, int accumulate, void *ws, hipStream_t stream)
+{
+    const int runs = runs_for(tensors, count, NORM_NV, GS_SQNORM_MAX_BLOCKS);
+    const int64_t tiles = (int64_t)tiles_of(tensors, count, (int64_t)TENSOR_BLOCK * NORM_NV * runs);
+    Meeting meet = {};
+    if (tiles > 0 && tiles <= MEET_MAX && count <= N) meet = {static_cast<uint64_t *>(ws), next_tag(), (int)tiles};
+    int64_t bytes = 0, done = 0;
+    for (int64_t i = 0; i < count; ++i) bytes += tensors[i].numel * size_of(tensors[i]);
+    double *partials = static_cast<double *>(ws);
+    hipError_t e = for_tables<N>(tensors, count, NORM_NV, runs, false, bytes - GS_KEEP_BYTES, [&](const Table<N> &t) {
+        k_tensors_sqnorm<N, NORM_NV><<<t.tiles, TENSOR_BLOCK, 0, stream>>>(t, partials + done, meet, d_sqnorm, accumulate);
+        done += t.tiles;
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || meet.n || (done == 0 && accumulate)) return e;
+    return launch_fold(partials, GS_SQNORM_MAX_BLOCKS, (int)done, d_sqnorm, accumulate, stream);
+}
+
+template <int N>
+static hipError_t clip(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, float max_norm, float *d_norm, hipStream_t stream)
+{
+    const int runs = runs_for(tensors, count, CLIP_NV, 1u << 23);
+    hipError_t e = for_tables<N>(tensors, count, CLIP_NV, runs, true, INT64_MAX, [&](const Table<N> &t) {
+        k_tensors_clip<N, CLIP_NV><<<t.tiles, TENSOR_BLOCK, 0, stream>>>(t, d_sqnorm, max_norm, d_norm);
+        d_norm = nullptr;              // written by the first launch
+        return hipGetLastError();
+    });
+    if (e == hipSuccess && d_norm) {   // nothing to scale, but a norm is asked for
+        Table<TABLE_SMALL> none;
+        memset(&none, 0, sizeof none);
+        k_tensors_clip<TABLE_SMALL, CLIP_NV><<<1, TENSOR_BLOCK, 0, stream>>>(none, d_sqnorm, max_norm, d_norm);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
 }  // namespace gs
 
 using namespace gs;
@@ -237,14 +375,8 @@ gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqn
     if (!d_sqnorm || (reinterpret_cast<uintptr_t>(d_sqnorm) & 7u)) return GS_ERR_INVALID_ARG;
     if (!d_workspace || workspace_bytes < gs_sqnorm_workspace_bytes() || (reinterpret_cast<uintptr_t>(d_workspace) & 7u)) return GS_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    double *partials = static_cast<double *>(d_workspace);
-    int64_t done = 0;
-    hipError_t e = for_tables(tensors, count, tile_vecs_for(tensors, count), [&](const Table &t, uint32_t tiles) {
-        k_tensors_sqnorm<<<tiles, TENSOR_BLOCK, 0, st>>>(t, partials + done);
-        done += tiles;
-        return hipGetLastError();
-    });
-    if (e == hipSuccess && (done || !accumulate)) e = launch_fold(partials, GS_SQNORM_MAX_BLOCKS, (int)done, d_sqnorm, accumulate, st);
+    hipError_t e = count <= TABLE_SMALL ? norm<TABLE_SMALL>(tensors, count, d_sqnorm, accumulate, d_workspace, st)
+                                        : norm<TABLE>(tensors, count, d_sqnorm, accumulate, d_workspace, st);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_grads_sqnorm launch");
 }
 
@@ -255,18 +387,8 @@ gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d
     if (!(max_norm > 0.0f)) return GS_ERR_INVALID_ARG;
     if (gs_status s = outputs_apart(tensors, count); s != GS_OK) return s;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    float *norm = d_norm;
-    hipError_t e = for_tables(tensors, count, tile_vecs_for(tensors, count), [&](const Table &t, uint32_t tiles) {
-        k_tensors_clip<<<tiles, TENSOR_BLOCK, 0, st>>>(t, d_sqnorm, max_norm, norm);
-        norm = nullptr;                // written by the first launch
-        return hipGetLastError();
-    });
-    if (e == hipSuccess && norm) {     // nothing to scale, but a norm is asked for
-        Table none;
-        memset(&none, 0, sizeof none);
-        k_tensors_clip<<<1, TENSOR_BLOCK, 0, st>>>(none, d_sqnorm, max_norm, norm);
-        e = hipGetLastError();
-    }
+    hipError_t e = count <= TABLE_SMALL ? clip<TABLE_SMALL>(tensors, count, d_sqnorm, max_norm, d_norm, st)
+                                        : clip<TABLE>(tensors, count, d_sqnorm, max_norm, d_norm, st);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_grads_clip launch");
 }
 
