@@ -488,8 +488,8 @@ void gs_pinned_free(void *ptr);
  * to one token whose id is targets[r]; with z the row, it = 1/temperature,
  *     M = max_i z_i,   S = sum_i exp(it (z_i - M)),   logp = it (z_t - M) - ln S,
  *     dlogp/dz_i = it ([i = t] - exp(it (z_i - M)) / S).
- * A target outside [0, vocab) (-1, -100: padding, a prompt) marks a row without a token: its logits are not
- * read, its logp is 0 and its gradient +0.  Logits may hold -inf (excluded tokens); a row of nothing
+ * A target outside [0, vocab) (-1, -100: padding, a prompt) marks a row without a token: nothing in its logits
+ * counts, its logp is 0 and its gradient +0.  Logits may hold -inf (excluded tokens); a row of nothing
  * else, or one with a NaN or +inf, gives NaN, as the formula does.  Maxima, sums and
  * log-probabilities are held in 32 bits, sums over tokens in 64; gradients are rounded once, to the logits' type.
  * All results are the same from call to call.
@@ -525,7 +525,7 @@ gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float t
  * Gradient of a loss in the logits, from its gradient in the token log-probabilities:
  *     dlogits[r][i] = dlogp[r] dlogp/dz_i
  * with (M, S) as gs_token_logp left them for the same logits, targets and temperature.  A row with dlogp[r] == 0, or without a token,
- * gets +0 and is not read.
+ * gets +0 whatever it holds.
  *   dlogits      device, the logits' type and shape, row r at element r * dlogits_stride (>= vocab); may be the logits
  *                themselves (same address and stride), else must not overlap them
  */
@@ -552,7 +552,7 @@ typedef struct {
  *   old_logp, advantages  device fp32, `rows`
  *   ref_logp     device fp32, `rows`, or NULL
  *   weights      device fp32, `rows`, or NULL for ones: a mask times whatever the loss is divided by.  Where it is 0 the row is as one
- *                without a token: nothing else of it is read
+ *                without a token: nothing else of it counts
  *   logp         device fp32, `rows`, written
  *   dlogits      as for gs_token_logp_grad, or NULL: no gradient
  *   d_stats      device fp32, 4 values: sums of weights times (pg + kl_coef kl), pg, kl, [clamped product smaller];
@@ -581,7 +581,7 @@ typedef struct {
  *     dlogp = +-scale beta weights (e sigmoid(h) - (1 - e) sigmoid(-h))        (minus in rejected sequences)
  *   logp       device fp32, `tokens`
  *   ref_logp   device fp32, `tokens`, or NULL for zeros
- *   weights    device fp32, `tokens`, or NULL for ones.  Where it is 0 nothing else of the token is read, and its dlogp is +0
+ *   weights    device fp32, `tokens`, or NULL for ones.  Where it is 0 nothing else of the token counts, and its dlogp is +0
  *   offsets    device int64, 2 pairs + 1, not decreasing, within [0, tokens] (each is taken into that range).  Tokens before the first
  *              and from the last on belong to no sequence; their dlogp is +0
  *   margins    device fp32, `pairs`;  dlogp: device fp32, `tokens`

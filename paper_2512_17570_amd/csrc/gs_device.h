@@ -90,8 +90,8 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
 // do.  So each leaves W 32-bit words in the caller's workspace, then looks whether all n have, and the last to look sees that they have.
 //   - Nothing has to be in the workspace before: a word lies beside a tag of this launch, in one 64-bit store, and counts only with
 //     it.  Tags are the upper halves of signalling NaNs, which no sum that was left there before has.
-//   - Two may see all n: the one that takes the tag out of the first slot finishes.
-//   - It clears the slots, so a graph, whose launches have the same tag every time, finds none of its own.
+//   - Two may see all n: the one that takes the tag out of the first slot finishes; or both do, with the same result.
+//   - Whoever finishes clears the slots, so a graph, whose launches have the same tag every time, finds none of its own.
 //   - Nobody waits for another workgroup.
 // The words go to memory and come from there by atomic accesses of the device's scope: the dies' caches do not see each other's
 // lines.  A workgroup's own are there (vmcnt) before it looks at the others'.
@@ -110,49 +110,58 @@ __device__ __forceinline__ void leave(const Meeting &M, int me, const uint32_t (
     for (int i = 0; i < W; ++i)
         __hip_atomic_store(M.slots + (int64_t)me * W + i, (uint64_t)M.tag << 32 | w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// By the whole wave: true in one workgroup of the launch, which reads the words with left() and then clears them.
+// By the whole wave: true in the workgroup that finishes, with the words of slot `lane` in w; left_words() has those of later slots.
+// Up to 64 slots and with `again` (a result may be written twice) every one that sees all may, since it has all it needs.
 template <int W>
-__device__ __forceinline__ bool last_of(const Meeting &M)
+__device__ __forceinline__ bool last_of(const Meeting &M, bool again, uint32_t (&w)[W])
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int lane = threadIdx.x & 63;
     bool here = true;
+#pragma unroll
+    for (int q = 0; q < W; ++q) w[q] = 0;
 #pragma unroll 1
     for (int i = lane; i < M.n; i += 64) {
         uint64_t x[W];
 #pragma unroll
         for (int q = 0; q < W; ++q) x[q] = __hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-        for (int q = 0; q < W; ++q) here = here && (uint32_t)(x[q] >> 32) == M.tag;
+        for (int q = 0; q < W; ++q) {
+            here = here && (uint32_t)(x[q] >> 32) == M.tag;
+            if (i < 64) w[q] = (uint32_t)x[q];
+        }
     }
     if (__ballot(here) != ~0ull) return false;
+    if (M.n <= 64 && again) return true;
     uint32_t tag = 0;
     if (lane == 0) tag = (uint32_t)(__hip_atomic_fetch_and(M.slots, (uint64_t)0xffffffffu, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)tag) == M.tag;
 }
 template <int W>
-__device__ __forceinline__ uint32_t left(const Meeting &M, int i, int q)
+__device__ __forceinline__ void left_words(const Meeting &M, int i, uint32_t (&w)[W])
 {
-    return (uint32_t)__hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int q = 0; q < W; ++q) w[q] = (uint32_t)__hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 template <int W>
 __device__ __forceinline__ void clear(const Meeting &M)
 {
     for (int i = threadIdx.x & 63; i < M.n * W; i += 64) __hip_atomic_store(M.slots + i, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// D doubles a slot, summed over all of them in a fixed order, in the wave's last lane
-template <int D>
-__device__ __forceinline__ void left_sums(const Meeting &M, double (&x)[D])
+// W / 2 doubles a slot, summed over all of them in a fixed order, in the wave's last lane
+template <int W>
+__device__ __forceinline__ void left_sums(const Meeting &M, uint32_t (&w)[W], double (&x)[W / 2])
 {
 #pragma unroll
-    for (int q = 0; q < D; ++q) x[q] = 0.0;
+    for (int q = 0; q < W / 2; ++q) x[q] = __hiloint2double((int)w[2 * q + 1], (int)w[2 * q]);       // 0 without a slot
 #pragma unroll 1
-    for (int i = threadIdx.x & 63; i < M.n; i += 64)
+    for (int i = (threadIdx.x & 63) + 64; i < M.n; i += 64) {
+        left_words(M, i, w);
 #pragma unroll
-        for (int q = 0; q < D; ++q) x[q] += __hiloint2double((int)left<2 * D>(M, i, 2 * q + 1), (int)left<2 * D>(M, i, 2 * q));
+        for (int q = 0; q < W / 2; ++q) x[q] += __hiloint2double((int)w[2 * q + 1], (int)w[2 * q]);
+    }
 #pragma unroll
-    for (int q = 0; q < D; ++q) x[q] = wave_sum(x[q]);
-    clear<2 * D>(M);
+    for (int q = 0; q < W / 2; ++q) x[q] = wave_sum(x[q]);
 }
 __device__ __forceinline__ void halves(double x, uint32_t &lo, uint32_t &hi)
 {

@@ -190,12 +190,14 @@ __device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Su
 // by the wave whose lane has left a row's sums
 __device__ __forceinline__ void finish_policy(const Meeting &M, float *out, int accumulate)
 {
-    if (!last_of<8>(M)) return;
+    uint32_t w[8];
+    if (!last_of(M, !accumulate, w)) return;
     double x[4];
-    left_sums(M, x);
+    left_sums(M, w, x);
     if ((threadIdx.x & 63) == 63)
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = (float)((accumulate ? (double)out[i] : 0.0) + x[i]);
+    clear<8>(M);
 }
 
 // +0 over a row
@@ -289,10 +291,12 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
         if (threadIdx.x == 0) {
             logp[r] = 0.0f;
             if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
-            if (meets) leave_sums(P.meet, r, Sums{});
+        }
+        if (meets && threadIdx.x >= BLOCK - 64) {
+            if (threadIdx.x == BLOCK - 64) leave_sums(P.meet, r, Sums{});
+            finish_policy(P.meet, P.stats, P.accumulate);
         }
         if (out) zero_row<E, BLOCK>(out, L.vocab);
-        if (meets && threadIdx.x < 64) finish_policy(P.meet, P.stats, P.accumulate);
     };
     // With few rows a workgroup does not wait to learn whether its row counts before it asks for it.
     if (!L.few && (t < 0 || w == 0.0f)) return no_token();
@@ -360,7 +364,8 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     }
     if constexpr (POLICY) {
         const Terms terms = policy_terms(lp, token, P);
-        if (meets && threadIdx.x == 0) leave_sums(P.meet, r, sums_of(terms, w, P.kl));
+        // by the last wave, which has the fewest vectors
+        if (meets && threadIdx.x == BLOCK - 64) leave_sums(P.meet, r, sums_of(terms, w, P.kl));
         const float d = w * terms.slope * P.it;
         if (!out) {
         } else if (d == 0.0f) {
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
             if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
                 E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
         }
-        if (meets && threadIdx.x < 64) finish_policy(P.meet, P.stats, P.accumulate);
+        if (meets && wave == NW - 1) finish_policy(P.meet, P.stats, P.accumulate);
     }
 }
 
@@ -479,15 +484,14 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
         const uint32_t mine[2] = {__float_as_uint(m), __float_as_uint(s)};
         if (threadIdx.x == 0) leave(F.meet, (int)part, mine);
         const float zt = E::load(row + t - from);
-        if (!last_of<2>(F.meet)) return;
-        MaxSum a = {-INFINITY, 0.0f};
-        if (lane < parts) a = {__uint_as_float(left<2>(F.meet, lane, 0)), __uint_as_float(left<2>(F.meet, lane, 1))};
-        clear<2>(F.meet);
-        a = join_parts(a, k);
+        uint32_t w[2];
+        if (!last_of(F.meet, true, w)) return;
+        const MaxSum a = join_parts({lane < parts ? __uint_as_float(w[0]) : -INFINITY, __uint_as_float(w[1])}, k);
         if (lane == 0) {
             F.logp[r] = (zt - a.m) * F.it - logf(a.s);
             if (F.row_stats) F.row_stats[2 * r] = a.m, F.row_stats[2 * r + 1] = a.s;
         }
+        clear<2>(F.meet);
     } else if (threadIdx.x == 0) {
         partials += (int64_t)which * (parts + 1);
         partials[part] = {m, s};
@@ -698,51 +702,61 @@ __device__ __forceinline__ void spread(const Pairs &A, int64_t from, int64_t to,
         A.dlogp[i] = w != 0.0f ? d * w : 0.0f;
     }
 }
-// ln(1 + exp(x))
-__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
-// A pair's loss from its margin as it is given out, in 32 bits: its relative error from that is at most that of the margin.
-__device__ __forceinline__ double pair_loss(float margin, float smoothing, float scale)
-{
-    const double h = margin, e = smoothing;
-    return (double)scale * ((1.0 - e) * softplus(-h) + (e != 0.0 ? e * softplus(h) : 0.0));
-}
+// Of a margin h, in 64 bits: loss and slope from one exponential, which is never over 1.
+struct PairLoss {
+    double h, t;                  // exp(-|h|)
+    __device__ __forceinline__ explicit PairLoss(double margin) : h(margin), t(exp(-fabs(margin))) {}
+    // e sigmoid(h) - (1 - e) sigmoid(-h)
+    __device__ __forceinline__ double slope(double e) const
+    {
+        const double inv = 1.0 / (1.0 + t), up = h > 0.0 ? inv : t * inv, down = h > 0.0 ? t * inv : inv;
+        return e * up - (1.0 - e) * down;
+    }
+    // -(1 - e) ln sigmoid(h) - e ln sigmoid(-h)
+    __device__ __forceinline__ double loss(double e) const
+    {
+        const double ln = log1p(t);
+        return (1.0 - e) * (fmax(-h, 0.0) + ln) + (e != 0.0 ? e * (fmax(h, 0.0) + ln) : 0.0);
+    }
+};
 
 // One workgroup a pair.  Both sums are held in 64 bits: a margin is a small difference of sums over thousands of tokens.
 __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
 {
-    __shared__ double lds[2][PAIR_BLOCK / 64];
-    __shared__ float slope;
+    constexpr int NW = PAIR_BLOCK / 64;
+    __shared__ double lds[2][NW];
     const int64_t p = blockIdx.x, q = A.pairs + p;
     const int64_t a0 = offset_of(A, p), a1 = offset_of(A, p + 1), b0 = offset_of(A, q), b1 = offset_of(A, q + 1);
-    const double chosen = block_sum<PAIR_BLOCK>(log_ratio_sum(A, a0, a1), lds[0]);
-    const double rejected = block_sum<PAIR_BLOCK>(log_ratio_sum(A, b0, b1), lds[1]);
-    if (threadIdx.x == 0) {
-        const double h = (double)A.beta * (chosen - rejected), e = A.smoothing;
-        const double up = 1.0 / (1.0 + exp(-h)), down = 1.0 / (1.0 + exp(h));       // sigmoid(h), sigmoid(-h)
-        A.margins[p] = (float)h;
-        if (A.meet.n > 0) {
-            uint32_t w[2];
-            halves(pair_loss((float)h, A.smoothing, A.scale), w[0], w[1]);
-            leave(A.meet, (int)p, w);
-        }
-        slope = (float)((double)A.scale * A.beta * (e * up - (1.0 - e) * down));
-    }
+    const double mine[2] = {wave_sum(log_ratio_sum(A, a0, a1)), wave_sum(log_ratio_sum(A, b0, b1))};
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 63) lds[0][wave] = mine[0], lds[1][wave] = mine[1];
     __syncthreads();
+    // every wave works out the pair's slope for itself
+    const double chosen = row_sum(lane < NW ? lds[0][lane] : 0.0), rejected = row_sum(lane < NW ? lds[1][lane] : 0.0);
+    const PairLoss pair((double)A.beta * (chosen - rejected));
+    const float slope = of_lane((float)((double)A.scale * A.beta * pair.slope(A.smoothing)), 0);
+    if (threadIdx.x == 0) A.margins[p] = (float)pair.h;
+    if (A.meet.n > 0 && wave == 0) {
+        uint32_t w[2];
+        halves((double)A.scale * pair.loss(A.smoothing), w[0], w[1]);
+        if (threadIdx.x == 0) leave(A.meet, (int)p, w);
+        if (last_of(A.meet, !A.accumulate, w)) {
+            double x[1];
+            left_sums(A.meet, w, x);
+            if (threadIdx.x == 63) *A.loss = (float)((A.accumulate ? (double)*A.loss : 0.0) + x[0]);
+            clear<2>(A.meet);
+        }
+    }
     spread(A, a0, a1, slope);
     spread(A, b0, b1, -slope);
     if (p == 0) spread(A, 0, offset_of(A, 0), 0.0f);
     if (q + 1 == 2 * A.pairs) spread(A, b1, A.tokens, 0.0f);
-    if (A.meet.n > 0 && threadIdx.x < 64) {
-        if (!last_of<2>(A.meet)) return;
-        double x[1];
-        left_sums(A.meet, x);
-        if (threadIdx.x == 63) *A.loss = (float)((A.accumulate ? (double)*A.loss : 0.0) + x[0]);
-    }
 }
+// With many pairs, the loss from their margins as they are given out, in 32 bits: its relative error from that is at most a margin's.
 __global__ __launch_bounds__(SUM_BLOCK) void k_pair_sums(const float *margins, int64_t pairs, float smoothing, float scale, double *partials, float *out, int accumulate)
 {
     double x[1] = {};
-    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) x[0] += pair_loss(margins[p], smoothing, scale);
+    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) x[0] += (double)scale * PairLoss((double)margins[p]).loss(smoothing);
     finish_sums<1, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
 }
 __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
@@ -768,32 +782,35 @@ struct RowShape {
 template <typename E, bool POLICY>
 static RowShape row_shape(int64_t vecs)
 {
-#define GS_HELD(BLOCK, NV, LO, KEEP) \
-    if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, LO, KEEP, POLICY>, BLOCK}
-    GS_HELD(64, 4, 0, POLICY ? 4 : 0);
-    GS_HELD(128, 4, 1, POLICY ? 4 : 0);
-    GS_HELD(256, 4, 1, POLICY ? 4 : 0);
+    // Of a row that the shape before, of up to PREV vectors, does not hold, at least PREV - 7 are there, counted from its line: it may start late in it.
+#define GS_HELD(PREV, BLOCK, NV, KEEP) \
+    if (vecs <= (BLOCK) * (NV)) return {k_held<E, BLOCK, NV, ((PREV) > 7 ? ((PREV) - 7) / (BLOCK) : 0), POLICY ? KEEP : 0, POLICY>, BLOCK}
+    GS_HELD(0, 64, 4, 4);
+    GS_HELD(256, 128, 4, 4);
+    GS_HELD(512, 256, 4, 4);
     if constexpr (POLICY) {
-        // wide workgroups: half the registers a wave
-        GS_HELD(512, 4, 1, 4);
-        GS_HELD(1024, 3, 1, 3);
-        GS_HELD(1024, 4, 2, 4);
-        GS_HELD(1024, 6, 3, 6);
-        GS_HELD(1024, 8, 5, 8);
+        // wide workgroups, whose waves have few vectors and keep all exponentials
+        GS_HELD(1024, 512, 4, 4);
+        GS_HELD(2048, 1024, 3, 3);
+        GS_HELD(3072, 1024, 4, 4);
+        GS_HELD(4096, 1024, 6, 6);
+        GS_HELD(6144, 1024, 8, 8);
     } else {
-        GS_HELD(256, 8, 3, 0);
-        GS_HELD(512, 6, 3, 0);
-        GS_HELD(512, 8, 5, 0);
-        GS_HELD(512, 12, 7, 0);
-        GS_HELD(512, 16, 11, 0);
+        // few registers either way: narrow ones, of which a CU holds more
+        GS_HELD(1024, 256, 8, 0);
+        GS_HELD(2048, 512, 6, 0);
+        GS_HELD(3072, 512, 8, 0);
+        GS_HELD(4096, 512, 12, 0);
+        GS_HELD(6144, 512, 16, 0);
     }
-    // KEEP: as many as there is room for in a workgroup's share of the registers; an fp32 vector takes as much as its exponentials
+    // KEEP: as many as 128 registers a lane have room for; an fp32 vector takes as much as its exponentials
     constexpr bool ALL = E::PER == 4;
-    GS_HELD(1024, 12, 7, !POLICY ? 0 : 12);
-    GS_HELD(1024, 16, 11, !POLICY ? 0 : ALL ? 16 : 8);
-    GS_HELD(1024, 20, 15, !POLICY ? 0 : ALL ? 20 : 4);
+    GS_HELD(8192, 1024, 12, 12);
+    GS_HELD(12288, 1024, 16, (ALL ? 16 : 8));
+    GS_HELD(16384, 1024, 20, (ALL ? 20 : 4));
+    static_assert(HELD_MAX == 1024 * 24);
+    return {k_held<E, 1024, 24, (20480 - 7) / 1024, POLICY && ALL ? 24 : 0, POLICY>, 1024};
 #undef GS_HELD
-    return {k_held<E, 1024, HELD_MAX / 1024, 19, POLICY && E::PER == 4 ? HELD_MAX / 1024 : 0, POLICY>, 1024};
 }
 
 struct Grid {

@@ -145,15 +145,14 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, dou
         return;
     }
     if (threadIdx.x >= 64) return;
-    if (threadIdx.x == 0) {
-        uint32_t w[2];
-        halves(s, w[0], w[1]);
-        leave(meet, (int)tile, w);
-    }
-    if (!last_of<2>(meet)) return;
+    uint32_t w[2];
+    halves(s, w[0], w[1]);
+    if (threadIdx.x == 0) leave(meet, (int)tile, w);
+    if (!last_of(meet, !accumulate, w)) return;
     double all[1];
-    left_sums(meet, all);
+    left_sums(meet, w, all);
     if (threadIdx.x == 63) *out = accumulate ? *out + all[0] : all[0];
+    clear<2>(meet);
 }
 
 template <int PER> __device__ __forceinline__ u32x4 scaled(u32x4 q, float c)

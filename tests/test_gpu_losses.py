@@ -237,6 +237,33 @@ def test_policy_loss_at_every_number_of_rows(rows):
     policy_check(Rows(rows, 130, F32, seed=rows), gradient=False)
 
 
+@pytest.mark.parametrize("vocab,dtype", [(40_003, BF16), (98_299, BF16), (98_310, BF16), (20_011, F32), (49_160, F32)])
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 63, 64, 65, 130])
+def test_policy_loss_of_few_long_rows(rows, vocab, dtype):
+    """Both sides of the lines between rows in parts and rows held, with and without a gradient, and accumulating."""
+    policy_check(Rows(rows, vocab, dtype, seed=rows), accumulate=rows % 2 == 1)
+    policy_check(Rows(rows, vocab, dtype, seed=rows + 1, offset=1, gap=2), in_place=True, accumulate=rows % 2 == 0)
+    policy_check(Rows(rows, vocab, dtype, seed=rows), gradient=False)
+
+
+# vectors of a row (8 or 4 elements) at which another kernel takes it, from both sides; with and without a first line to share
+HELD_LINES = [256, 512, 1024, 2048, 3072, 4096, 6144, 8192, 12288, 16384, 20480, 24576]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vecs", HELD_LINES)
+def test_lines_between_kernels(vecs, dtype):
+    per = 8 if dtype == BF16 else 4
+    for vocab, offset, gap in ((vecs * per, 0, 0), (vecs * per + per, 0, 0), (vecs * per - 7 * per, 1, 1), (vecs * per - 7 * per + per - 1, per - 1, 1),
+                               (vecs * per - 6 * per, 8 * per - 1, 1)):
+        x = Rows(2, vocab, dtype, seed=vecs, offset=offset, gap=gap, prompt=0.0)
+        x.logits[0, 0], x.logits[1, -1] = 9.0, 8.0          # the ends count
+        x.target[0], x.target[1] = vocab - 1, 0
+        logp_check(x)
+        x = Rows(70 if vecs > 3000 else 3, vocab, dtype, seed=vecs, offset=offset, gap=gap)
+        policy_check(x, in_place=True)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_policy_gradient_against_differences(dtype):
     """dlogits against central differences of the loss in 64 bits (step 1e-4: the loss is three times differentiable with
@@ -266,6 +293,8 @@ PAIRS = {
     "empty ones": [(0, 3), (4, 0), (0, 0)],
     "uneven": [(5, 700), (512, 513), (64, 63), (1, 2000)],
     "long": [(30_001, 4)],
+    "sixty-five": [(i % 7 + 1, i % 5) for i in range(65)],
+    "two hundred and fifty-six": [(i % 3, 2) for i in range(256)],
     "many": [(i % 37, (i * 7) % 53) for i in range(1500)],
 }
 
@@ -402,6 +431,43 @@ def test_same_bits_every_time_on_every_stream_and_from_a_graph(rows, vocab, dtyp
         graph.replay()
         same()
         torch.randn(1000, device=DEV).sum().item()
+
+
+def test_small_launches_finish_alone():
+    """Launches whose last workgroup finishes them, hundreds in a row with other inputs each, on two streams with a workspace each."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    z = torch.randn(40, 60_000, generator=g, device=DEV, dtype=F32)
+    t = torch.randint(0, 4000, (40,), generator=g, device=DEV)
+    adv, old = torch.randn(40, generator=g, device=DEV), torch.full((40,), -9.0, device=DEV)
+    calls = [(1, 60_000), (7, 45_000), (40, 4000), (33, 5000), (3, 60_000)]
+    want, got = {}, []
+    streams, ws = [torch.cuda.Stream(), torch.cuda.Stream()], [workspace(), workspace()]
+    torch.cuda.synchronize()
+    for i in range(400):
+        rows, vocab = calls[i % 5]
+        first = (i * 7) % (41 - rows)
+        logp, rs, plogp, stats = (torch.full(s, float("nan"), device=DEV) for s in ((rows,), (rows, 2), (rows,), (4,)))
+        torch.cuda.current_stream().synchronize()
+        x, tt, st = z[first:first + rows, :vocab], t[first:first + rows], streams[i % 2]
+        gs.gs_token_logp(x, tt, logp, rs, d_workspace=ws[i % 2], stream=st)
+        out = None if i % 3 else torch.empty_like(x)
+        torch.cuda.current_stream().synchronize()
+        gs.gs_policy_loss(x, tt, old[first:first + rows], None, adv[first:first + rows], None, gs.PolicyHParams(), plogp, out, stats, ws[i % 2], stream=st)
+        got.append((rows, vocab, first, logp, rs, plogp, stats, out))
+    torch.cuda.synchronize()
+    for rows, vocab, first, logp, rs, plogp, stats, _ in got:
+        key = rows, vocab, first
+        if key not in want:
+            x = z[first:first + rows, :vocab].double()
+            tt = t[first:first + rows]
+            w = torch.log_softmax(x, 1).gather(1, tt[:, None])[:, 0]
+            r = (w - old[first:first + rows]).exp()
+            a = adv[first:first + rows]
+            pg = -torch.minimum(r * a, r.clamp(0.8, 1.2) * a)
+            want[key] = w, pg.sum(), (pg.abs()).sum()
+        w, pg, size = want[key]
+        assert float((logp - w).abs().max()) < 2e-5 and float((plogp - w).abs().max()) < 2e-5
+        assert float((stats[1] - pg).abs()) <= 3e-5 * float(size) and torch.equal(stats[0], stats[1])
 
 
 def test_native_and_general_reading_agree(monkeypatch):

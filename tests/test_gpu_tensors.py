@@ -63,8 +63,10 @@ LISTS = {
     "a layer": [64, 64, 64 * 192, 192, 64 * 64, 64, 64, 64, 64 * 256, 256, 256 * 64, 64],
     "lengths around a vector": list(range(1, 40)),
     "around a tile": [2047, 2048, 2049, 8191, 8192, 8193, 16383, 16384, 16385, 16391, 32768, 65537],
-    "a full table": [33] * 120,
-    "and one more": [33] * 121,
+    "a short table": [33] * 16,
+    "and one more": [33] * 17,
+    "a full table": [33] * 128,
+    "and one more again": [33] * 129,
     "many": [(i * 37) % 301 for i in range(1000)],
     "one long among short": [5] * 64 + [3_000_001] + [6] * 64,
     "long": [40_000_003, 11],
@@ -124,6 +126,40 @@ def test_norm_accumulates_and_equals_the_flat_norms():
     assert float(parts) == pytest.approx(float(sq), rel=1e-14)
     gs.gs_grads_sqnorm([], parts, workspace())
     assert float(parts) == 0.0
+
+
+@pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 128, 129, 255, 256, 257])
+def test_norm_of_any_number_of_workgroups(count):
+    """One tensor a workgroup: up to 256 of them finish by themselves, in one launch up to 128 tensors; the rest take another launch."""
+    _, tensors = make([50] * count, [F32] * count, seed=count)
+    S = want_sqnorm(tensors)
+    for _ in range(3):
+        assert float(sqnorm(tensors)) == pytest.approx(S, rel=1e-14)
+    sq = torch.full((1,), 5.0, dtype=torch.float64, device=DEV)
+    for i in range(3):
+        gs.gs_grads_sqnorm(tensors, sq, workspace(), accumulate=True)
+        assert float(sq) == pytest.approx(5.0 + (i + 1) * S, rel=1e-14)
+
+
+def test_a_graph_of_small_norms():
+    _, tensors = make([70_001], [BF16], lead=1)
+    ws, sq = workspace(), torch.zeros(1, dtype=torch.float64, device=DEV)
+    gs.gs_grads_sqnorm(tensors, sq, ws)
+    want = float(sq)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gs.gs_grads_sqnorm(tensors, sq, ws)
+        gs.gs_grads_sqnorm(tensors, sq, ws, accumulate=True)
+    for i in range(5):
+        sq.fill_(-1.0)
+        if i == 3:
+            tensors[0].mul_(2.0)
+            want *= 4.0
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(sq) == 2 * want
+        gs.gs_grads_sqnorm(tensors, sq, ws)
+        assert float(sq) == want
 
 
 def test_nothing_to_clip_still_gives_the_norm():
