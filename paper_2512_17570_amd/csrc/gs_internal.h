@@ -123,8 +123,6 @@ struct AccumAddArgs {
 hipError_t launch_accum_adamw(const StepArgs &A, hipStream_t stream);
 hipError_t launch_accum_adamw_spec(const StepArgs &A, double *partials, size_t workspace_bytes, double *d_out,
                                    int accumulate, hipStream_t stream);
-// adds up `nparts` partials in a fixed order; cap: of a workspace's doubles, all but the folding slices that follow them
-hipError_t launch_fold(double *partials, int64_t cap, int nparts, double *d_out, int accumulate, hipStream_t stream);
 hipError_t launch_grad_sqnorm(const SqnormArgs &A, size_t workspace_bytes, double *d_out, int accumulate,
                               hipStream_t stream);
 

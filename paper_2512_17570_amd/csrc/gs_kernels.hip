@@ -926,7 +926,7 @@ __global__ __launch_bounds__(GS_FINAL_BLOCK) void k_sqnorm_finalize(const double
     if (threadIdx.x == 0) *out = accumulate ? (*out + t) : t;
 }
 
-hipError_t launch_fold(double *partials, int64_t cap, int nparts, double *d_out, int accumulate, hipStream_t stream)
+static hipError_t launch_fold(double *partials, int64_t cap, int nparts, double *d_out, int accumulate, hipStream_t stream)
 {
     if (nparts > GS_FINAL_DIRECT_MAX) {
         double *slices = partials + cap;          // the last GS_FINAL_SLICES doubles of the workspace

@@ -163,7 +163,6 @@ struct Logits {
     int64_t stride;
     const int64_t *targets;
     int vocab;
-    bool few;                     // rows: what they take is a chain of latencies
 };
 __device__ __forceinline__ int target_of(const Logits &L, int64_t r)
 {
@@ -298,8 +297,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
         }
         if (out) zero_row<E, BLOCK>(out, L.vocab);
     };
-    // With few rows a workgroup does not wait to learn whether its row counts before it asks for it.
-    if (!L.few && (t < 0 || w == 0.0f)) return no_token();
+    if (t < 0 || w == 0.0f) return no_token();
     Token token = {};
     if constexpr (POLICY) token = token_of(P, r);
     const T *row = static_cast<const T *>(L.x) + r * L.stride;
@@ -324,7 +322,6 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     else load(std::false_type{});
     const int single = (int)threadIdx.x < c.singles ? c.single<PER>(threadIdx.x) : -1;
     const float zs = single >= 0 ? E::load(row + single) : -INFINITY;
-    if (L.few && (t < 0 || w == 0.0f)) return no_token();
     const float zt = E::load(row + t);
     auto used = [&](int j) { return j < LO || j * BLOCK + wave * 64 < end; };      // by any lane of the wave
 
@@ -402,7 +399,6 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
 constexpr int PART_BLOCK = 256;
 constexpr int PART_MIN = 8192;
 constexpr int PARTS = 64;
-constexpr int64_t FEW_ROWS = 512;
 constexpr int HELD_MAX = 24 * 1024;          // vectors of the longest row that is held
 
 struct MaxSum {
@@ -628,37 +624,32 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
 }
 
 // ---- sums over tokens -------------------------------------------------------------------------
-// Workgroups leave N sums each, one workgroup folds them in a fixed order; a single one finishes by itself.
 constexpr int SUM_BLOCK = 256;
-constexpr int SUM_MAX_BLOCKS = 512;
-template <int N, int BLOCK>
-__device__ __forceinline__ void finish_sums(const double (&x)[N], double *partials, float *out, int accumulate, bool last)
+// N sums of every workgroup, added up by the last of them
+template <int N>
+__device__ __forceinline__ void finish_sums(double (&x)[N], const Meeting &M, float *out, int accumulate)
 {
-    __shared__ double lds[N][BLOCK / 64];
+    __shared__ double lds[N][SUM_BLOCK / 64];
+    uint32_t w[2 * N];
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-        const double t = block_sum<BLOCK>(x[q], lds[q]);
-        if (threadIdx.x == 0) {
-            if (last) out[q] = (float)((accumulate ? (double)out[q] : 0.0) + t);
-            else partials[(int64_t)blockIdx.x * N + q] = t;
-        }
+        x[q] = block_sum<SUM_BLOCK>(x[q], lds[q]);
+        halves(x[q], w[2 * q], w[2 * q + 1]);
     }
-}
-template <int N>
-__global__ __launch_bounds__(SUM_BLOCK) void k_fold_sums(const double *partials, int count, float *out, int accumulate)
-{
-    double x[N] = {};
-    for (int i = threadIdx.x; i < count; i += SUM_BLOCK)
+    if (threadIdx.x >= 64) return;
+    if (threadIdx.x == 0) leave(M, (int)blockIdx.x, w);
+    if (!last_of(M, !accumulate, w)) return;
+    left_sums(M, w, x);
+    if (threadIdx.x == 63)
 #pragma unroll
-        for (int q = 0; q < N; ++q) x[q] += partials[(int64_t)i * N + q];
-    finish_sums<N, SUM_BLOCK>(x, nullptr, out, accumulate, true);
+        for (int q = 0; q < N; ++q) out[q] = (float)((accumulate ? (double)out[q] : 0.0) + x[q]);
+    clear<2 * N>(M);
 }
 
-__global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *targets, int vocab, int64_t rows, Policy P, const float *logp, double *partials,
-                                                           float *out, int accumulate)
+__global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *targets, int vocab, int64_t rows, Policy P, const float *logp)
 {
     double x[4] = {};
-    for (int64_t r = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; r < rows; r += (int64_t)gridDim.x * SUM_BLOCK) {
+    for (int64_t r = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; r < rows; r += (int64_t)P.meet.n * SUM_BLOCK) {
         const float w = weight_of(P.weights, r);
         const int64_t t = targets[r];
         if (t < 0 || t >= vocab || w == 0.0f) continue;
@@ -666,7 +657,7 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *target
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] += e.x[q];
     }
-    finish_sums<4, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
+    finish_sums(x, P.meet, P.stats, P.accumulate);
 }
 
 // ---- preference loss --------------------------------------------------------------------------
@@ -753,11 +744,11 @@ __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
     if (q + 1 == 2 * A.pairs) spread(A, b1, A.tokens, 0.0f);
 }
 // With many pairs, the loss from their margins as they are given out, in 32 bits: its relative error from that is at most a margin's.
-__global__ __launch_bounds__(SUM_BLOCK) void k_pair_sums(const float *margins, int64_t pairs, float smoothing, float scale, double *partials, float *out, int accumulate)
+__global__ __launch_bounds__(SUM_BLOCK) void k_pair_sums(const float *margins, int64_t pairs, float smoothing, float scale, Meeting meet, float *out, int accumulate)
 {
     double x[1] = {};
-    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)gridDim.x * SUM_BLOCK) x[0] += (double)scale * PairLoss((double)margins[p]).loss(smoothing);
-    finish_sums<1, SUM_BLOCK>(x, partials, out, accumulate, gridDim.x == 1);
+    for (int64_t p = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; p < pairs; p += (int64_t)meet.n * SUM_BLOCK) x[0] += (double)scale * PairLoss((double)margins[p]).loss(smoothing);
+    finish_sums(x, meet, out, accumulate);
 }
 __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
 {
@@ -765,10 +756,12 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
 }
 
 // ---- launchers --------------------------------------------------------------------------------
-static int sum_blocks(int64_t n)
+static Meeting meeting(void *ws, int n) { return {static_cast<uint64_t *>(ws), next_tag(), n}; }
+// of the workgroups that go through n tokens or pairs
+static Meeting sums_meeting(int64_t n, void *ws)
 {
-    const int64_t b = (n + 4 * SUM_BLOCK - 1) / (4 * SUM_BLOCK);
-    return (int)(b < 1 ? 1 : b > SUM_MAX_BLOCKS ? SUM_MAX_BLOCKS : b);
+    const int64_t b = (n + SUM_BLOCK - 1) / SUM_BLOCK;
+    return meeting(ws, (int)(b < 1 ? 1 : b > MEET_MAX ? MEET_MAX : b));
 }
 
 static constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
@@ -874,7 +867,7 @@ static hipError_t launch_in_parts(const gs_logits &X, const Logits &L, const Pol
     for (int64_t r = 0; r < X.rows; r += g.rows) {
         const int rows = (int)(X.rows - r < g.rows ? X.rows - r : g.rows);
         if (!POLICY) {
-            const Finish F = {{reinterpret_cast<uint64_t *>(partials), next_tag(), g.parts}, P.it, logp, row_stats};
+            const Finish F = {meeting(partials, g.parts), P.it, logp, row_stats};
             k_part<E, true><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, nullptr, nullptr, F);
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
             continue;
@@ -971,7 +964,7 @@ static bool good_workspace(const void *ws, size_t bytes) { return ws && bytes >=
 
 static Logits logits_of(const gs_logits &x, const int64_t *targets)
 {
-    return {x.data, x.rows > 1 ? x.row_stride : x.vocab, targets, (int)x.vocab, x.rows <= FEW_ROWS};
+    return {x.data, x.rows > 1 ? x.row_stride : x.vocab, targets, (int)x.vocab};
 }
 static Policy scaled_by(float temperature)
 {
@@ -1067,14 +1060,12 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     P.accumulate = accumulate;
     // with few rows the last of them adds up their sums; the workspace's end is theirs, its start holds parts
     const bool meets = rows > 0 && rows <= MEET_MAX && (dlogits || !in_parts(*logits, true));
-    if (meets) P.meet = {reinterpret_cast<uint64_t *>(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_MAX * 64), next_tag(), (int)rows};
+    if (meets) P.meet = meeting(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_MAX * 64, (int)rows);
     hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, d_workspace, st);
     if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
     if (meets) return GS_OK;
-    const int blocks = sum_blocks(rows);
-    double *partials = static_cast<double *>(d_workspace);
-    k_policy_sums<<<blocks, SUM_BLOCK, 0, st>>>(targets, (int)logits->vocab, rows, P, logp, partials, d_stats, accumulate);
-    if (blocks > 1) k_fold_sums<4><<<1, SUM_BLOCK, 0, st>>>(partials, blocks, d_stats, accumulate);
+    P.meet = sums_meeting(rows, d_workspace);
+    k_policy_sums<<<P.meet.n, SUM_BLOCK, 0, st>>>(targets, (int)logits->vocab, rows, P, logp);
     e = hipGetLastError();
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_policy_loss launch");
 }
@@ -1099,16 +1090,14 @@ gs_status gs_preference_loss(const float *logp, const float *ref_logp, const flo
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (pairs) {
         Pairs A = {logp, ref_logp, weights, offsets, tokens, pairs, hp->beta, hp->label_smoothing, hp->scale, margins, dlogp, {}, d_loss, accumulate};
-        if (pairs <= MEET_MAX) A.meet = {static_cast<uint64_t *>(d_workspace), next_tag(), (int)pairs};
+        if (pairs <= MEET_MAX) A.meet = meeting(d_workspace, (int)pairs);
         k_pairs<<<(int)pairs, PAIR_BLOCK, 0, st>>>(A);
     } else if (tokens) {
-        k_zero<<<sum_blocks(tokens), SUM_BLOCK, 0, st>>>(dlogp, tokens);
+        k_zero<<<(int)(tokens > MEET_MAX * SUM_BLOCK ? MEET_MAX : (tokens + SUM_BLOCK - 1) / SUM_BLOCK), SUM_BLOCK, 0, st>>>(dlogp, tokens);
     }
     if (pairs > MEET_MAX || (pairs == 0 && !accumulate)) {
-        const int blocks = sum_blocks(pairs);
-        double *partials = static_cast<double *>(d_workspace);
-        k_pair_sums<<<blocks, SUM_BLOCK, 0, st>>>(margins, pairs, hp->label_smoothing, hp->scale, partials, d_loss, accumulate);
-        if (blocks > 1) k_fold_sums<1><<<1, SUM_BLOCK, 0, st>>>(partials, blocks, d_loss, accumulate);
+        const Meeting meet = sums_meeting(pairs, d_workspace);
+        k_pair_sums<<<meet.n, SUM_BLOCK, 0, st>>>(margins, pairs, hp->label_smoothing, hp->scale, meet, d_loss, accumulate);
     }
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_preference_loss launch");

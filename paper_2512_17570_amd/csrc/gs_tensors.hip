@@ -155,6 +155,25 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, dou
     clear<2>(meet);
 }
 
+// The partials of many tiles, a run of FOLD_RUN of them a workgroup, or what that comes to with FOLD_MAX of them.
+constexpr int FOLD_BLOCK = 1024, FOLD_RUN = 4096, FOLD_MAX = 64;
+__global__ __launch_bounds__(FOLD_BLOCK) void k_tensors_fold(const double *partials, int count, Meeting meet, double *out, int accumulate)
+{
+    __shared__ double lds[FOLD_BLOCK / 64];
+    double x = 0.0;
+    for (int i = (int)blockIdx.x * FOLD_BLOCK + (int)threadIdx.x; i < count; i += meet.n * FOLD_BLOCK) x += partials[i];
+    const double s = block_sum<FOLD_BLOCK>(x, lds);
+    if (threadIdx.x >= 64) return;
+    uint32_t w[2];
+    halves(s, w[0], w[1]);
+    if (threadIdx.x == 0) leave(meet, (int)blockIdx.x, w);
+    if (!last_of(meet, !accumulate, w)) return;
+    double all[1];
+    left_sums(meet, w, all);
+    if (threadIdx.x == 63) *out = accumulate ? *out + all[0] : all[0];
+    clear<2>(meet);
+}
+
 template <int PER> __device__ __forceinline__ u32x4 scaled(u32x4 q, float c)
 {
 #pragma unroll
@@ -340,7 +359,12 @@ static hipError_t norm(const gs_tensor *tensors, int64_t count, double *d_sqnorm
         return hipGetLastError();
     });
     if (e != hipSuccess || meet.n || (done == 0 && accumulate)) return e;
-    return launch_fold(partials, GS_SQNORM_MAX_BLOCKS, (int)done, d_sqnorm, accumulate, stream);
+    const int64_t blocks = (done + FOLD_RUN - 1) / FOLD_RUN;
+    // its slots lie behind the partials
+    meet = {static_cast<uint64_t *>(ws) + GS_SQNORM_MAX_BLOCKS, next_tag(), (int)(blocks < 1 ? 1 : blocks > FOLD_MAX ? FOLD_MAX : blocks)};
+    static_assert(2 * FOLD_MAX <= GS_FINAL_SLICES);
+    k_tensors_fold<<<meet.n, FOLD_BLOCK, 0, stream>>>(partials, (int)done, meet, d_sqnorm, accumulate);
+    return hipGetLastError();
 }
 
 template <int N>
