@@ -629,14 +629,19 @@ constexpr int SUM_BLOCK = 256;
 template <int N>
 __device__ __forceinline__ void finish_sums(double (&x)[N], const Meeting &M, float *out, int accumulate)
 {
-    __shared__ double lds[N][SUM_BLOCK / 64];
-    uint32_t w[2 * N];
+    constexpr int NW = SUM_BLOCK / 64;
+    __shared__ double lds[N][NW];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-        x[q] = block_sum<SUM_BLOCK>(x[q], lds[q]);
-        halves(x[q], w[2 * q], w[2 * q + 1]);
+        x[q] = wave_sum(x[q]);
+        if (lane == 63) lds[q][wave] = x[q];
     }
-    if (threadIdx.x >= 64) return;
+    __syncthreads();
+    if (wave > 0) return;
+    uint32_t w[2 * N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) halves(row_sum(lane < NW ? lds[q][lane] : 0.0), w[2 * q], w[2 * q + 1]);
     if (threadIdx.x == 0) leave(M, (int)blockIdx.x, w);
     if (!last_of(M, !accumulate, w)) return;
     left_sums(M, w, x);
@@ -650,12 +655,14 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_policy_sums(const int64_t *target
 {
     double x[4] = {};
     for (int64_t r = (int64_t)blockIdx.x * SUM_BLOCK + threadIdx.x; r < rows; r += (int64_t)P.meet.n * SUM_BLOCK) {
-        const float w = weight_of(P.weights, r);
+        // all loads together; what a token without weight holds is not added
+        const float w = weight_of(P.weights, r), lp = logp[r];
         const int64_t t = targets[r];
-        if (t < 0 || t >= vocab || w == 0.0f) continue;
-        const Sums e = sums_of(policy_terms(logp[r], token_of(P, r), P), w, P.kl);
+        const Token token = token_of(P, r);
+        const bool counts = t >= 0 && t < vocab && w != 0.0f;
+        const Sums e = sums_of(policy_terms(lp, token, P), w, P.kl);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] += e.x[q];
+        for (int q = 0; q < 4; ++q) x[q] += counts ? e.x[q] : 0.0;
     }
     finish_sums(x, P.meet, P.stats, P.accumulate);
 }
@@ -848,7 +855,7 @@ template <typename E, bool FROM_PARTS>
 static hipError_t launch_grad(GradArgs A, int64_t rows, hipStream_t stream)
 {
     A.runs = grad_runs<E>(A.L.vocab);
-    const int64_t most = kMaxItems / GRAD_BLOCK / A.runs;               // 15 rows of 2^30 elements
+    const int64_t most = kMaxItems / GRAD_BLOCK / A.runs;               // 31 rows of 2^30 fp32 elements
     const int64_t first = A.row0;
     for (int64_t done = 0; done < rows; done += A.rows) {
         A.rows = rows - done < most ? rows - done : most;

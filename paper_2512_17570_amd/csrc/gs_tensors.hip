@@ -312,24 +312,31 @@ static bool good_tensors(const gs_tensor *tensors, int64_t count, bool outs)
     return true;
 }
 
-// Every output against every other array but its own input.  Sorted by address, an overlap shows between neighbours: each
-// range is held against the furthest end so far, of the outputs and of all.
+// Every output against every other array but its own input: sorted by address, an overlap shows against the furthest end so far, of
+// the outputs and of all.
 struct Range {
     uintptr_t lo, hi;
     bool out;
 };
-static gs_status outputs_apart(const gs_tensor *tensors, int64_t count)
+static Range range_of(const void *p, int64_t bytes, bool out)
 {
-    Range few[64], *r = few;
-    if (count > 32 && !(r = static_cast<Range *>(malloc(sizeof(Range) * 2 * (size_t)count)))) return GS_ERR_NOMEM;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, a + (uintptr_t)bytes, out};
+}
+static gs_status outputs_apart(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, const float *d_norm)
+{
+    Range few[66], *r = few;
+    if (count > 32 && !(r = static_cast<Range *>(malloc(sizeof(Range) * (2 * (size_t)count + 2))))) return GS_ERR_NOMEM;
     size_t n = 0;
     for (int64_t i = 0; i < count; ++i) {
         const gs_tensor &t = tensors[i];
         if (t.numel == 0) continue;
-        const uintptr_t bytes = (uintptr_t)(t.numel * size_of(t)), in = reinterpret_cast<uintptr_t>(t.data), out = reinterpret_cast<uintptr_t>(t.out);
-        if (out && out != in) r[n++] = {in, in + bytes, false};
-        r[n++] = {out ? out : in, (out ? out : in) + bytes, true};
+        const int64_t bytes = t.numel * size_of(t);
+        if (t.out && t.out != t.data) r[n++] = range_of(t.data, bytes, false);
+        r[n++] = range_of(t.out ? t.out : t.data, bytes, true);
     }
+    r[n++] = range_of(d_sqnorm, 8, false);
+    if (d_norm) r[n++] = range_of(d_norm, 4, true);
     auto less = [](const Range &a, const Range &b) { return a.lo < b.lo; };
     if (!std::is_sorted(r, r + n, less)) std::sort(r, r + n, less);
     uintptr_t any_end = 0, out_end = 0;
@@ -341,6 +348,14 @@ static gs_status outputs_apart(const gs_tensor *tensors, int64_t count)
     }
     if (r != few) free(r);
     return good ? GS_OK : GS_ERR_INVALID_ARG;
+}
+static bool touches(const gs_tensor *tensors, int64_t count, const Range &o)
+{
+    for (int64_t i = 0; i < count; ++i) {
+        const Range t = range_of(tensors[i].data, tensors[i].numel * size_of(tensors[i]), false);
+        if (t.lo < o.hi && o.lo < t.hi) return true;
+    }
+    return false;
 }
 
 template <int N>
@@ -397,6 +412,8 @@ gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqn
     if (!good_tensors(tensors, count, false)) return GS_ERR_INVALID_ARG;
     if (!d_sqnorm || (reinterpret_cast<uintptr_t>(d_sqnorm) & 7u)) return GS_ERR_INVALID_ARG;
     if (!d_workspace || workspace_bytes < gs_sqnorm_workspace_bytes() || (reinterpret_cast<uintptr_t>(d_workspace) & 7u)) return GS_ERR_WORKSPACE;
+    const Range sq = range_of(d_sqnorm, 8, true), ws = range_of(d_workspace, (int64_t)workspace_bytes, true);
+    if (touches(tensors, count, sq) || touches(tensors, count, ws) || (sq.lo < ws.hi && ws.lo < sq.hi)) return GS_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = count <= TABLE_SMALL ? norm<TABLE_SMALL>(tensors, count, d_sqnorm, accumulate, d_workspace, st)
                                         : norm<TABLE>(tensors, count, d_sqnorm, accumulate, d_workspace, st);
@@ -408,7 +425,7 @@ gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d
     if (!good_tensors(tensors, count, true)) return GS_ERR_INVALID_ARG;
     if (!d_sqnorm || (reinterpret_cast<uintptr_t>(d_sqnorm) & 7u) || (reinterpret_cast<uintptr_t>(d_norm) & 3u)) return GS_ERR_INVALID_ARG;
     if (!(max_norm > 0.0f)) return GS_ERR_INVALID_ARG;
-    if (gs_status s = outputs_apart(tensors, count); s != GS_OK) return s;
+    if (gs_status s = outputs_apart(tensors, count, d_sqnorm, d_norm); s != GS_OK) return s;
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = count <= TABLE_SMALL ? clip<TABLE_SMALL>(tensors, count, d_sqnorm, max_norm, d_norm, st)
                                         : clip<TABLE>(tensors, count, d_sqnorm, max_norm, d_norm, st);

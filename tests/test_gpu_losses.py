@@ -246,6 +246,34 @@ def test_policy_loss_of_few_long_rows(rows, vocab, dtype):
     policy_check(Rows(rows, vocab, dtype, seed=rows), gradient=False)
 
 
+def test_no_rows():
+    """An empty batch: sums of 0, or what was there; nothing else is touched."""
+    z, t, none = torch.empty(0, 60_000, dtype=BF16, device=DEV), torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(0, device=DEV)
+    stats = torch.full((4,), 7.0, device=DEV)
+    gs.gs_policy_loss(z, t, none, None, none, None, gs.PolicyHParams(), none, z, stats, workspace(), accumulate=True)
+    assert stats.tolist() == [7.0] * 4
+    gs.gs_policy_loss(z, t, none, None, none, None, gs.PolicyHParams(), none, z, stats, workspace())
+    assert stats.tolist() == [0.0] * 4
+    gs.gs_token_logp(z, t, none, d_workspace=workspace())
+    gs.gs_token_logp_grad(z, t, none.view(0, 2), none, z)
+
+
+def test_no_row_counts():
+    """A batch of prompts, and one of weights of 0."""
+    for rows in (1, 70, 300):
+        x = Rows(rows, 9000, BF16, seed=rows, prompt=1.1)
+        x.logits.fill_(float("nan"))
+        _, out = x.like(0, 0)
+        logp, stats = torch.full((rows,), 3.0, device=DEV), torch.full((4,), 3.0, device=DEV)
+        nan = torch.full((rows,), float("nan"), device=DEV)
+        gs.gs_policy_loss(x.logits, t_dev(x), nan, nan, nan, None, gs.PolicyHParams(kl_coef=0.1), logp, out, stats, workspace())
+        assert not logp.any() and not out.any() and not stats.any()
+        x.target.fill_(5)
+        out.fill_(1.0)
+        gs.gs_policy_loss(x.logits, t_dev(x), nan, nan, nan, torch.zeros(rows, device=DEV), gs.PolicyHParams(), logp.fill_(2.0), out, stats.fill_(2.0), workspace())
+        assert not logp.any() and not out.any() and not stats.any()
+
+
 # vectors of a row (8 or 4 elements) at which another kernel takes it, from both sides; with and without a first line to share
 HELD_LINES = [256, 512, 1024, 2048, 3072, 4096, 6144, 8192, 12288, 16384, 20480, 24576]
 

@@ -117,6 +117,8 @@ def test_grads_sqnorm():
         assert call(*tensors(GOOD), **kw) == BAD
     for kw in ({"ws": 0}, {"ws": A[6] + 4}, {"b": WS - 1}):
         assert call(*tensors(GOOD), **kw) == WORK
+    for kw in ({"sq": A[0] + 392}, {"ws": A[0] + 8}, {"sq": A[6] + 64}, {"ws": A[0] - WS + 8}):
+        assert call(*tensors(GOOD), **kw) == BAD, kw
     assert call(None, 0, acc=1) == gs.GS_OK and call(*tensors((None, None, 0, gs.GS_BF16)), acc=1) == gs.GS_OK
 
 
@@ -124,7 +126,8 @@ def test_grads_clip():
     call = lambda t, n, sq=A[5], most=1.0, norm=A[6]: gs._lib.gs_grads_clip(t, n, sq, most, norm, None)  # noqa: E731
     for t in WRONG_TENSORS:
         assert call(*tensors(GOOD, t)) == BAD, t
-    for kw in ({"sq": 0}, {"sq": A[5] + 4}, {"norm": A[6] + 2}, {"most": 0.0}, {"most": -1.0}, {"most": NAN}):
+    for kw in ({"sq": 0}, {"sq": A[5] + 4}, {"norm": A[6] + 2}, {"most": 0.0}, {"most": -1.0}, {"most": NAN},
+               {"sq": A[0] + 392}, {"norm": A[0] + 396}, {"norm": A[5] + 4}):
         assert call(*tensors(GOOD), **kw) == BAD, kw
     overlaps = [
         [GOOD, GOOD],                                                               # twice
