@@ -2,8 +2,14 @@
 // their gradient, the clipped policy loss with a KL term, and the preference loss over pairs of sequences.
 //
 // All the work is one or two passes over rows of logits (2 or 4 bytes an element, one row a token, up to a few hundred
-// thousand elements a row): read, and for a gradient written once, with two exponentials an element and no product of
+// thousand elements a row): read, and for a gradient written once, with one or two exponentials an element and no product of
 // matrices, so HBM is the bound and there is no MFMA here.
+//   * a row of up to 196608 bf16 (98304 fp32) elements is read once: it stays in its workgroup's registers (k_held)
+//   * longer rows, and rows of which there are too few to fill the chip, go in parts (k_part), and a gradient reads them again (k_grad)
+//   * the preference loss knows a token's gradient only when both sequences of its pair have been scored, so it reads twice
+// Against what the same card copies (one 16-byte vector a lane, 6.7 TB/s) and only reads (7.1 TB/s): 16384 x 32000 bf16 scored at 7.0
+// TB/s; policy loss with its gradient over 8192 x 131072 at 5.6 and 4095 x 50001 at 5.6 (a copy in the shape of k_held, a row held
+// from its first load to its first store, 6.0 and 6.1); 2048 x 32003 fp32 at 5.5; gradients of known rows 6.2 to 6.5.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -226,7 +232,11 @@ __device__ __forceinline__ void grad_singly(const typename E::T *row, typename E
 //
 // A wave takes its exponentials from a maximum of its own, as soon as its vectors are there, and waits for the others once, for the
 // row's maximum and sum; its gradient is then f exp2((m_wave - m) k) times those exponentials.  Of the first KEEP vectors the
-// exponentials stay (four bytes an element), of the others the logits (two in bf16), and the exponential is taken again.
+// exponentials stay (four bytes an element), of the others the logits (two in bf16), and the exponential is taken again: 8192 x 131072,
+// of 16 vectors none / 5 / 9 kept 0.85/0.78/0.76 ms (with a maximum of the whole row first, and all taken again, 0.89).
+// A longer row leaves room for one workgroup on a CU, whose reading and writing then take turns; other CUs' fill the gaps.  Loads and
+// stores carry the non-temporal hint: written through as well, or without the hint, they lose 1-3 and 2-8 %, loads without it 12 % where
+// nothing is written.  Vectors are counted from a line's start: with rows that start anywhere (50001) 0.143 ms against 0.151.
 template <int CTRL, int ROWS = 0xf>
 __device__ __forceinline__ float from_dpp(float x, float none)
 {
@@ -412,13 +422,14 @@ __device__ __forceinline__ MaxSum join_parts(MaxSum a, float k)
     return {m, wave_join<false>(a.s * __builtin_amdgcn_exp2f((a.m - base) * k))};
 }
 
-// The part's maximum and its sum of exp2(k (z - maximum)).  Read again afterwards, so the lines stay in the caches.  A row has one
+// The part's maximum and its sum of exp2(k (z - maximum)).  Lines that are read again afterwards stay in the caches.  A row has one
 // entry more than parts: the token's own logit, which a gradient written in place would not leave for the others to read.
 //   FINISH: the last of a row's workgroups also joins them, for a log-probability with no gradient after it
 struct Finish {
     Meeting meet;
     float it;
     float *logp, *row_stats;
+    bool once;                    // more than the caches hold, and not read again
 };
 template <typename E, bool FINISH>
 __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int parts, int len, float k, const float *weights, MaxSum *partials, Finish F)
@@ -443,12 +454,16 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
     float m = -INFINITY, s = 0.0f;
     for (int i0 = 0; i0 == 0 || i0 < c.vecs; i0 += NV * PART_BLOCK) {
         u32x4 q[NV];
+        auto load = [&](auto keep) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = i0 + j * PART_BLOCK + (int)threadIdx.x;
-            q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
-            if (i < c.vecs) q[j] = v[i];
-        }
+            for (int j = 0; j < NV; ++j) {
+                const int i = i0 + j * PART_BLOCK + (int)threadIdx.x;
+                q[j] = u32x4{E::LOWEST, E::LOWEST, E::LOWEST, E::LOWEST};
+                if (i < c.vecs) q[j] = decltype(keep)::value ? v[i] : __builtin_nontemporal_load(v + i);
+            }
+        };
+        if (FINISH && F.once) load(std::false_type{});
+        else load(std::true_type{});
         typename E::Max most;
 #pragma unroll
         for (int j = 0; j < NV; ++j) most.add(q[j]);
@@ -520,7 +535,9 @@ __global__ __launch_bounds__(PART_BLOCK) void k_join(Logits L, int64_t row0, int
 
 // ---- gradient of rows whose maximum and sum are known -------------------------------------------
 // A workgroup takes a run of GRAD_VECS vectors of a row, counted from the start of the row's first line; the first one has the single elements
-// too.  PARTS: maximum and sum come from a row's parts, and its policy loss is worked out here; else they and the loss's gradient in logp
+// too.  Two vectors a lane, written through: 8192 x 131072 bf16 0.683 ms (6.3 TB/s) against 0.718 without, 0.718 with one and 0.740 with
+// four; rows of 2000 0.59 against 1.09 with one.
+// FROM_PARTS: maximum and sum come from a row's parts, and its policy loss is worked out here; else they and the loss's gradient in logp
 // are given, and the rows are taken from the last one on: the end of what was read before is still in the memory-side cache.
 constexpr int GRAD_BLOCK = 256;
 constexpr int GRAD_NV = 2;
@@ -718,7 +735,8 @@ struct PairLoss {
     }
 };
 
-// One workgroup a pair.  Both sums are held in 64 bits: a margin is a small difference of sums over thousands of tokens.
+// One workgroup a pair: 4 to 6 us whatever the pairs, a chain of loads, a reduction and two functions in 64 bits.  Both sums are held
+// in 64 bits: a margin is a small difference of sums over thousands of tokens.
 __global__ __launch_bounds__(PAIR_BLOCK) void k_pairs(Pairs A)
 {
     constexpr int NW = PAIR_BLOCK / 64;
@@ -874,7 +892,8 @@ static hipError_t launch_in_parts(const gs_logits &X, const Logits &L, const Pol
     for (int64_t r = 0; r < X.rows; r += g.rows) {
         const int rows = (int)(X.rows - r < g.rows ? X.rows - r : g.rows);
         if (!POLICY) {
-            const Finish F = {meeting(partials, g.parts), P.it, logp, row_stats};
+            const bool once = !row_stats && X.rows * X.vocab * (int64_t)sizeof(typename E::T) > GS_KEEP_BYTES;
+            const Finish F = {meeting(partials, g.parts), P.it, logp, row_stats, once};
             k_part<E, true><<<(uint32_t)rows * g.parts, PART_BLOCK, 0, stream>>>(L, r, g.parts, g.len, P.k, nullptr, nullptr, F);
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
             continue;

@@ -4,6 +4,10 @@
 // One pass that reads every element (the norm) and one that reads and writes it (the clip): HBM-bound.  A launch takes a
 // table of tensors in its arguments, so nothing is copied to the device first and nothing is kept from call to call; its workgroups
 // are tiles of one tensor each, and find which by a look at the first tile of every tensor.
+//   Measured: 805 M fp32 gradients in 12 tensors, norm 0.468 ms (6.9 TB/s), clip into other buffers 1.00 ms (6.4); 201 M in 48 tensors of
+// both types 65 and 118 us (6.2, 6.8: the end of what the norm read is still in the memory-side cache, 183 us together against 189 in the
+// norm's own order); 48 tensors of 2048 to 8192 bf16 elements 5.0 and 3.6 us on the GPU, 12.3 us a pass.  A plain copy reaches 6.7 TB/s on the same
+// card, reading 7.1.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -240,7 +244,9 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_clip(Table<N> t, const
 }
 
 // ---- launchers --------------------------------------------------------------------------------
-constexpr int NORM_NV = 4, CLIP_NV = 2;              // vectors of a lane
+// Vectors of a lane.  Clip of 805 M fp32 with 1 / 2 / 4 / 8 of them 1.13/0.99/1.10/1.18 ms, with two of them not written through 1.05, with
+// fewer workgroups on a CU more; norm of 201 M in 48 tensors 99/66/62/64 us.
+constexpr int NORM_NV = 4, CLIP_NV = 2;
 static int64_t size_of(const gs_tensor &t) { return t.dtype == GS_BF16 ? 2 : 4; }
 // tiles of a tensor: its vectors counted from the start of the first one's line
 static uint32_t tiles_of(const gs_tensor &t, int64_t tile_vecs)
