@@ -102,19 +102,27 @@ struct Meeting {
 };
 constexpr int MEET_MAX = 256;     // every workgroup reads the slots of all
 
-// by one lane of the wave that looks afterwards
+// by lane 0 of the wave that looks afterwards; alone, there is nothing to leave
 template <int W>
 __device__ __forceinline__ void leave(const Meeting &M, int me, const uint32_t (&w)[W])
 {
+    if (M.n == 1) return;
 #pragma unroll
     for (int i = 0; i < W; ++i)
         __hip_atomic_store(M.slots + (int64_t)me * W + i, (uint64_t)M.tag << 32 | w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// By the whole wave: true in the workgroup that finishes, with the words of slot `lane` in w; left_words() has those of later slots.
-// Up to 64 slots and with `again` (a result may be written twice) every one that sees all may, since it has all it needs.
+// By the whole wave, whose lane 0 has in w what it has left: true in the workgroup that finishes, with the words of slot `lane` in w;
+// left_words() has those of later slots.  Up to 64 slots and with `again` (a result may be written twice) every one that sees all may, since it
+// has all it needs.
 template <int W>
 __device__ __forceinline__ bool last_of(const Meeting &M, bool again, uint32_t (&w)[W])
 {
+    if (M.n == 1) {
+        if ((threadIdx.x & 63) != 0)
+#pragma unroll
+            for (int q = 0; q < W; ++q) w[q] = 0;
+        return true;
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int lane = threadIdx.x & 63;
     bool here = true;
@@ -146,6 +154,7 @@ __device__ __forceinline__ void left_words(const Meeting &M, int i, uint32_t (&w
 template <int W>
 __device__ __forceinline__ void clear(const Meeting &M)
 {
+    if (M.n == 1) return;
     for (int i = threadIdx.x & 63; i < M.n * W; i += 64) __hip_atomic_store(M.slots + i, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 // W / 2 doubles a slot, summed over all of them in a fixed order, in the wave's last lane

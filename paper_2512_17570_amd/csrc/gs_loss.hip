@@ -185,24 +185,31 @@ __device__ __forceinline__ Sums sums_of(const Terms &e, float w, float kl_coef)
     const double pg = (double)w * e.pg, kl = (double)w * e.kl;
     return {{kl_coef != 0.0f ? pg + kl_coef * kl : pg, pg, kl, e.clipped ? (double)w : 0.0}};
 }
-__device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Sums &s)
+// One row's, by a wave: left in 32 bits, since every workgroup looks at all that are there, and halves of them would be as many words again.
+__device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Sums &s, uint32_t (&w)[4])
 {
-    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) halves(s.x[i], w[2 * i], w[2 * i + 1]);
-    leave(M, (int)r, w);
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint((float)s.x[i]);
+    if ((threadIdx.x & 63) == 0) leave(M, (int)r, w);
 }
-// by the wave whose lane has left a row's sums
-__device__ __forceinline__ void finish_policy(const Meeting &M, float *out, int accumulate)
+__device__ __forceinline__ void finish_policy(const Meeting &M, uint32_t (&w)[4], float *out, int accumulate)
 {
-    uint32_t w[8];
     if (!last_of(M, !accumulate, w)) return;
     double x[4];
-    left_sums(M, w, x);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = __uint_as_float(w[q]);          // 0 without a slot
+#pragma unroll 1
+    for (int i = (threadIdx.x & 63) + 64; i < M.n; i += 64) {
+        left_words(M, i, w);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] += __uint_as_float(w[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = wave_sum(x[q]);
     if ((threadIdx.x & 63) == 63)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = (float)((accumulate ? (double)out[i] : 0.0) + x[i]);
-    clear<8>(M);
+        for (int q = 0; q < 4; ++q) out[q] = (float)((accumulate ? (double)out[q] : 0.0) + x[q]);
+    clear<4>(M);
 }
 
 // +0 over a row
@@ -302,8 +309,9 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
             if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
         }
         if (meets && threadIdx.x >= BLOCK - 64) {
-            if (threadIdx.x == BLOCK - 64) leave_sums(P.meet, r, Sums{});
-            finish_policy(P.meet, P.stats, P.accumulate);
+            uint32_t words[4];
+            leave_sums(P.meet, r, Sums{}, words);
+            finish_policy(P.meet, words, P.stats, P.accumulate);
         }
         if (out) zero_row<E, BLOCK>(out, L.vocab);
     };
@@ -372,7 +380,8 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     if constexpr (POLICY) {
         const Terms terms = policy_terms(lp, token, P);
         // by the last wave, which has the fewest vectors
-        if (meets && threadIdx.x == BLOCK - 64) leave_sums(P.meet, r, sums_of(terms, w, P.kl));
+        uint32_t words[4] = {};
+        if (meets && wave == NW - 1) leave_sums(P.meet, r, sums_of(terms, w, P.kl), words);
         const float d = w * terms.slope * P.it;
         if (!out) {
         } else if (d == 0.0f) {
@@ -399,7 +408,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
             if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
                 E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
         }
-        if (meets && wave == NW - 1) finish_policy(P.meet, P.stats, P.accumulate);
+        if (meets && wave == NW - 1) finish_policy(P.meet, words, P.stats, P.accumulate);
     }
 }
 
@@ -492,10 +501,9 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
     if constexpr (FINISH) {
         if (threadIdx.x >= 64) return;
         F.meet.slots += (int64_t)which * parts * 2;
-        const uint32_t mine[2] = {__float_as_uint(m), __float_as_uint(s)};
-        if (threadIdx.x == 0) leave(F.meet, (int)part, mine);
+        uint32_t w[2] = {__float_as_uint(m), __float_as_uint(s)};
+        if (threadIdx.x == 0) leave(F.meet, (int)part, w);
         const float zt = E::load(row + t - from);
-        uint32_t w[2];
         if (!last_of(F.meet, true, w)) return;
         const MaxSum a = join_parts({lane < parts ? __uint_as_float(w[0]) : -INFINITY, __uint_as_float(w[1])}, k);
         if (lane == 0) {
@@ -582,8 +590,9 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
         if (run == 0 && threadIdx.x < 64) {
             if (threadIdx.x == 0) A.logp[r] = lp;
             if (A.P.meet.n > 0) {
-                if (threadIdx.x == 0) leave_sums(A.P.meet, r, sums);
-                finish_policy(A.P.meet, A.P.stats, A.P.accumulate);
+                uint32_t words[4];
+                leave_sums(A.P.meet, r, sums, words);
+                finish_policy(A.P.meet, words, A.P.stats, A.P.accumulate);
             }
         }
     } else if (t >= 0) {
@@ -641,7 +650,7 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
 }
 
 // ---- sums over tokens -------------------------------------------------------------------------
-constexpr int SUM_BLOCK = 256;
+constexpr int SUM_BLOCK = 512;
 // N sums of every workgroup, added up by the last of them
 template <int N>
 __device__ __forceinline__ void finish_sums(double (&x)[N], const Meeting &M, float *out, int accumulate)
@@ -781,12 +790,15 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
 }
 
 // ---- launchers --------------------------------------------------------------------------------
+// Workgroups that meet with more work behind them than a sum: policy loss, 128 / 200 / 256 rows of 8000 7.0/8.9/9.4 us, with a launch of
+// its own for the sums 8.3; 128 / 256 pairs 5.4/6.9 against 6.6.
+constexpr int MEET_FEW = 128;
 static Meeting meeting(void *ws, int n) { return {static_cast<uint64_t *>(ws), next_tag(), n}; }
 // of the workgroups that go through n tokens or pairs
 static Meeting sums_meeting(int64_t n, void *ws)
 {
     const int64_t b = (n + SUM_BLOCK - 1) / SUM_BLOCK;
-    return meeting(ws, (int)(b < 1 ? 1 : b > MEET_MAX ? MEET_MAX : b));
+    return meeting(ws, (int)(b < 1 ? 1 : b > MEET_FEW ? MEET_FEW : b));
 }
 
 static constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
@@ -1085,8 +1097,8 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     P.stats = d_stats;
     P.accumulate = accumulate;
     // with few rows the last of them adds up their sums; the workspace's end is theirs, its start holds parts
-    const bool meets = rows > 0 && rows <= MEET_MAX && (dlogits || !in_parts(*logits, true));
-    if (meets) P.meet = meeting(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_MAX * 64, (int)rows);
+    const bool meets = rows > 0 && rows <= MEET_FEW && (dlogits || !in_parts(*logits, true));
+    if (meets) P.meet = meeting(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_FEW * 32, (int)rows);
     hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, d_workspace, st);
     if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
     if (meets) return GS_OK;
@@ -1116,12 +1128,12 @@ gs_status gs_preference_loss(const float *logp, const float *ref_logp, const flo
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (pairs) {
         Pairs A = {logp, ref_logp, weights, offsets, tokens, pairs, hp->beta, hp->label_smoothing, hp->scale, margins, dlogp, {}, d_loss, accumulate};
-        if (pairs <= MEET_MAX) A.meet = meeting(d_workspace, (int)pairs);
+        if (pairs <= MEET_FEW) A.meet = meeting(d_workspace, (int)pairs);
         k_pairs<<<(int)pairs, PAIR_BLOCK, 0, st>>>(A);
     } else if (tokens) {
-        k_zero<<<(int)(tokens > MEET_MAX * SUM_BLOCK ? MEET_MAX : (tokens + SUM_BLOCK - 1) / SUM_BLOCK), SUM_BLOCK, 0, st>>>(dlogp, tokens);
+        k_zero<<<(int)(tokens > 256 * SUM_BLOCK ? 256 : (tokens + SUM_BLOCK - 1) / SUM_BLOCK), SUM_BLOCK, 0, st>>>(dlogp, tokens);
     }
-    if (pairs > MEET_MAX || (pairs == 0 && !accumulate)) {
+    if (pairs > MEET_FEW || (pairs == 0 && !accumulate)) {
         const Meeting meet = sums_meeting(pairs, d_workspace);
         k_pair_sums<<<meet.n, SUM_BLOCK, 0, st>>>(margins, pairs, hp->label_smoothing, hp->scale, meet, d_loss, accumulate);
     }
