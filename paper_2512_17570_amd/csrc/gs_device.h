@@ -89,7 +89,7 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
 // Of a small launch a second one, for what its workgroups leave, is the larger part: 3.7 us of a stream's time each, whatever they
 // do.  So each leaves W 32-bit words in the caller's workspace, then looks whether all n have, and the last to look sees that they have.
 //   - Nothing has to be in the workspace before: a word lies beside a tag of this launch, in one 64-bit store, and counts only with
-//     it.  Tags are the upper halves of signalling NaNs, which no sum that was left there before has.
+//     it.  Tags are the upper halves of signalling NaNs, which no sum in 64 bits has; who leaves other words there sees to it.
 //   - Two may see all n: the one that takes the tag out of the first slot finishes; or both do, with the same result.
 //   - Whoever finishes clears the slots, so a graph, whose launches have the same tag every time, finds none of its own.
 //   - Nobody waits for another workgroup.

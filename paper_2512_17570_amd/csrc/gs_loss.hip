@@ -513,7 +513,7 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
         clear<2>(F.meet);
     } else if (threadIdx.x == 0) {
         partials += (int64_t)which * (parts + 1);
-        partials[part] = {m, s};
+        partials[part] = {m, s == s ? s : NAN};              // a NaN of a logit's bits could be taken for a tag
         if (t >= from && t < from + n) partials[parts].m = E::load(row + t - from);
     }
 }

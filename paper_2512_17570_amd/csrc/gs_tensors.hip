@@ -249,9 +249,9 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_clip(Table<N> t, const
 constexpr int NORM_NV = 4, CLIP_NV = 2;
 static int64_t size_of(const gs_tensor &t) { return t.dtype == GS_BF16 ? 2 : 4; }
 // tiles of a tensor: its vectors counted from the start of the first one's line
-static uint32_t tiles_of(const gs_tensor &t, int64_t tile_vecs)
+static uint64_t tiles_of(const gs_tensor &t, int64_t tile_vecs)
 {
-    return (uint32_t)((t.numel / (16 / size_of(t)) + 7) / tile_vecs + 1);
+    return (uint64_t)((t.numel / (16 / size_of(t)) + 7) / tile_vecs + 1);
 }
 static uint64_t tiles_of(const gs_tensor *t, int64_t count, int64_t tile_vecs)
 {
@@ -293,7 +293,7 @@ static hipError_t for_tables(const gs_tensor *tensors, int64_t count, int nv, in
             at += bytes;
             t.first[t.count] = t.tiles;
             t.e[t.count++] = {x.data, x.out ? x.out : const_cast<void *>(x.data), x.numel * 2 + (x.dtype == GS_BF16)};
-            t.tiles += tiles_of(x, tile_vecs);
+            t.tiles += (uint32_t)tiles_of(x, tile_vecs);
         }
         if (t.count == 0) continue;
         for (int i = t.count; i < N; ++i) t.first[i] = ~0u;

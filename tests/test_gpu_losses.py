@@ -583,3 +583,19 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(ValueError):
         gs.gs_preference_loss(lp, None, None, torch.zeros(2, dtype=torch.int64, device=DEV), gs.PreferenceHParams(),
                               torch.zeros(1, device=DEV), torch.zeros(4, device=DEV), torch.zeros(1, device=DEV), ws)
+
+
+@pytest.mark.parametrize("bits", [0x7FF00001, 0x7FF00123, 0x7FF7FFFF, 0x7F800001, 0x7FC00000])
+def test_what_a_call_leaves_in_the_workspace_is_no_tag(bits):
+    """Upper halves of 64-bit words between 0x7ff00001 and 0x7ff7ffff mark what a launch has left for its last workgroup.  Rows in parts
+    with NaN of such bits among the logits leave none."""
+    z = torch.randn(4, 60_000, device=DEV, dtype=F32)
+    z[:, 100] = torch.tensor(bits, dtype=torch.int32, device=DEV).view(F32)
+    t, one, logp, stats = torch.zeros(4, dtype=torch.int64, device=DEV), torch.ones(4, device=DEV), torch.zeros(4, device=DEV), torch.zeros(4, device=DEV)
+    for out in (None, torch.empty_like(z)):
+        ws = torch.zeros(WS, dtype=torch.uint8, device=DEV)
+        gs.gs_policy_loss(z, t, one, None, one, None, gs.PolicyHParams(), logp, out, stats, ws)
+        gs.gs_token_logp(z, t, logp, None, d_workspace=ws)
+        upper = ws.view(torch.int32)[1::2]
+        assert not bool(((upper >= 0x7FF00001) & (upper <= 0x7FF7FFFF)).any())
+        assert bool(logp.isnan().all()) and bool(stats[:2].isnan().all())
