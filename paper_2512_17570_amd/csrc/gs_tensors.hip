@@ -6,13 +6,14 @@
 // are tiles of one tensor each, and find which by a look at the first tile of every tensor.
 //   Measured: 805 M fp32 gradients in 12 tensors, norm 0.468 ms (6.9 TB/s), clip into other buffers 1.00 ms (6.4); 201 M in 48 tensors of
 // both types 65 and 118 us (6.2, 6.8: the end of what the norm read is still in the memory-side cache, 183 us together against 189 in the
-// norm's own order); 48 tensors of 2048 to 8192 bf16 elements 5.0 and 3.6 us on the GPU, 12.3 us a pass.  A plain copy reaches 6.7 TB/s on the same
-// card, reading 7.1.
+// norm's own order); 48 tensors of 2048 to 8192 bf16 elements 5.0 and 3.6 us on the GPU, 9 to 12 us a pass, as fast as the host calls.  A plain
+// copy reaches 6.7 TB/s on the same card, reading 7.1.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdlib>
 #include <cstring>
+#include <type_traits>
 
 #include "gs_device.h"
 #include "gs_internal.h"
@@ -24,8 +25,11 @@ namespace gs {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TENSOR_BLOCK = 256;
-constexpr int TABLE = 128;             // tensors of one launch: 3600 of the 4096 bytes that a launch's arguments may have
-constexpr int TABLE_SMALL = 16;
+// Tensors of one launch, in the 4096 bytes that its arguments may have: a short list, which is quick to go through, a long one, and a long
+// one of tensors that stay where they are.  With 128 at most, as addresses and lengths of 64 bits each would have it, norm and clip of 144 tensors
+// of 100 to 40 000 elements take 21.5 us against 15, of 448 of 4096 elements 47 against 35; with 1.7 MB a tensor level, 1 to 3 % ahead.
+constexpr int TABLE_SMALL = 16, TABLE = 160, TABLE_IN_PLACE = 240;
+constexpr int64_t PIECE = (int64_t)1 << 31;     // longer tensors go as pieces of so many elements, whose number takes 32 bits
 
 struct Entry {
     const void *in;
@@ -34,20 +38,50 @@ struct Entry {
     int32_t dtype;
     uint32_t first;                    // its first tile, of this launch's
 };
+__device__ __forceinline__ void *address(uint32_t lo, uint32_t hi)
+{
+    return (void *)(__attribute__((address_space(1))) void *)((uint64_t)hi << 32 | lo);       // device memory, not what may be LDS
+}
+// An address of either type is even: the type takes its lowest bit.
+struct Whereabouts {
+    uint32_t lo, hi, numel;
+    static Whereabouts of(const gs_tensor &x)
+    {
+        const uint64_t a = reinterpret_cast<uintptr_t>(x.data) | (x.dtype == GS_BF16 ? 1 : 0);
+        return {(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)x.numel};
+    }
+    __device__ __forceinline__ Entry entry(uint32_t first) const
+    {
+        void *p = address(lo & ~1u, hi);
+        return {p, p, (int64_t)numel, lo & 1 ? GS_BF16 : GS_F32, first};
+    }
+};
+struct WithOut {
+    Whereabouts in;
+    uint32_t lo, hi;
+    static WithOut of(const gs_tensor &x)
+    {
+        const uint64_t a = reinterpret_cast<uintptr_t>(x.out ? x.out : x.data);
+        return {Whereabouts::of(x), (uint32_t)a, (uint32_t)(a >> 32)};
+    }
+    __device__ __forceinline__ Entry entry(uint32_t first) const
+    {
+        Entry e = in.entry(first);
+        e.out = address(lo, hi);
+        return e;
+    }
+};
 // First tiles beside each other, so that looking for a tile's tensor takes few lines of memory; ~0 behind the last tensor.
 template <int N> struct Table {
-    uint32_t first[N];
+    typedef std::conditional_t<N == TABLE_IN_PLACE, Whereabouts, WithOut> S;
+    alignas(16) uint32_t first[N];
     uint32_t tiles, keep_tile;         // norm: tiles from this one on are left in the memory-side cache, for the clip
     int32_t count, runs;               // runs: of NV vectors a lane, one after another in a tile
-    struct {
-        const void *in;
-        void *out;
-        int64_t numel_bf16;            // elements, twice, and 1 for bf16
-    } e[N];
+    S e[N];
 };
 
 // The tensor that a tile belongs to: the last one whose first tile is not behind it.  A short list is gone through by the scalar unit, of
-// a long one every lane looks at two.
+// a long one every lane looks at four, in one load: with a load each, clip of 144 tensors of 1.7 MB 207 us against 200.
 template <int N>
 __device__ __forceinline__ Entry entry_of(const Table<N> &t, uint32_t tile)
 {
@@ -56,13 +90,15 @@ __device__ __forceinline__ Entry entry_of(const Table<N> &t, uint32_t tile)
 #pragma unroll
         for (int i = 1; i < N; ++i) n += t.first[i] <= tile ? 1 : 0;
     } else {
-        static_assert(N == 128, "two for each lane");
+        static_assert(N % 4 == 0 && N <= 256);
         const int lane = threadIdx.x & 63;
-        n = __popcll(__ballot(t.first[lane] <= tile)) + __popcll(__ballot(t.first[lane + 64] <= tile)) - 1;
-        n = __builtin_amdgcn_readfirstlane(n);
+        u32x4 f = {~0u, ~0u, ~0u, ~0u};
+        if (lane < N / 4) f = reinterpret_cast<const u32x4 *>(t.first)[lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += __popcll(__ballot(f[i] <= tile));
+        n = __builtin_amdgcn_readfirstlane(n - 1);
     }
-    const auto &e = t.e[n];
-    return {e.in, e.out, e.numel_bf16 >> 1, e.numel_bf16 & 1 ? GS_BF16 : GS_F32, t.first[n]};
+    return t.e[n].entry(t.first[n]);
 }
 
 // A tile's part of a tensor: the vectors [at, end) behind `head` single elements, counted from the start of the first one's 128-byte line
@@ -134,8 +170,9 @@ __device__ __forceinline__ double tile_squares(const Entry &e, uint32_t tile, in
     return x + y;
 }
 
+// before: tiles of the launches in front of this one, which meet with its own.
 template <int N, int NV>
-__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, double *partials, Meeting meet, double *out, int accumulate)
+__global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, double *partials, Meeting meet, int before, double *out, int accumulate)
 {
     __shared__ double lds[TENSOR_BLOCK / 64];
     const uint32_t tile = blockIdx.x;
@@ -151,7 +188,7 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_sqnorm(Table<N> t, dou
     if (threadIdx.x >= 64) return;
     uint32_t w[2];
     halves(s, w[0], w[1]);
-    if (threadIdx.x == 0) leave(meet, (int)tile, w);
+    if (threadIdx.x == 0) leave(meet, before + (int)tile, w);
     if (!last_of(meet, !accumulate, w)) return;
     double all[1];
     left_sums(meet, w, all);
@@ -248,32 +285,34 @@ __global__ __launch_bounds__(TENSOR_BLOCK) void k_tensors_clip(Table<N> t, const
 // fewer workgroups on a CU more; norm of 201 M in 48 tensors 99/66/62/64 us.
 constexpr int NORM_NV = 4, CLIP_NV = 2;
 static int64_t size_of(const gs_tensor &t) { return t.dtype == GS_BF16 ? 2 : 4; }
-// tiles of a tensor: its vectors counted from the start of the first one's line
-static uint64_t tiles_of(const gs_tensor &t, int64_t tile_vecs)
-{
-    return (uint64_t)((t.numel / (16 / size_of(t)) + 7) / tile_vecs + 1);
-}
-static uint64_t tiles_of(const gs_tensor *t, int64_t count, int64_t tile_vecs)
+// tiles of 2^shift vectors in a tensor: its vectors counted from the start of the first one's line
+static uint64_t tiles_of(const gs_tensor &t, int shift) { return (uint64_t)(((t.numel >> (t.dtype == GS_BF16 ? 3 : 2)) + 7) >> shift) + 1; }
+static uint64_t tiles_of(const gs_tensor *t, int64_t count, int shift)
 {
     uint64_t n = 0;
-    for (int64_t i = 0; i < count; ++i) n += t[i].numel ? tiles_of(t[i], tile_vecs) : 0;
+    for (int64_t i = 0; i < count; ++i) n += t[i].numel ? tiles_of(t[i], shift) : 0;
     return n;
 }
 
-// Runs of a tile so that there are no more than `most` tiles.
-static int runs_for(const gs_tensor *t, int64_t count, int nv, uint64_t most)
+// Tiles of a list: 2^shift vectors each, in runs of NV a lane, so many that there are no more of them than `most`.
+struct Tiles {
+    uint64_t count;
+    int shift, runs;
+};
+template <int NV>
+static Tiles tiles_for(const gs_tensor *t, int64_t count, uint64_t most)
 {
-    int runs = 1;
-    while (tiles_of(t, count, (int64_t)TENSOR_BLOCK * nv * runs) > most) runs *= 2;
-    return runs;
+    static_assert((TENSOR_BLOCK * NV & (TENSOR_BLOCK * NV - 1)) == 0);
+    Tiles r = {0, __builtin_ctz(TENSOR_BLOCK * NV), 1};
+    while ((r.count = tiles_of(t, count, r.shift)) > most) ++r.shift, r.runs *= 2;
+    return r;
 }
 
 // Calls launch(table) for tables of up to N tensors that hold all of them between them; `back`: from the last one on.  Bytes of the list
 // from keep_from on are marked to be kept.
 template <int N, typename F>
-static hipError_t for_tables(const gs_tensor *tensors, int64_t count, int nv, int runs, bool back, int64_t keep_from, F launch)
+static hipError_t for_tables(const gs_tensor *tensors, int64_t count, const Tiles &tiles, bool back, int64_t keep_from, F launch)
 {
-    const int64_t tile_vecs = (int64_t)TENSOR_BLOCK * nv * runs;
     Table<N> t;
     int64_t at = 0;                    // bytes before this tensor
     for (int64_t left = count; left > 0;) {
@@ -282,18 +321,18 @@ static hipError_t for_tables(const gs_tensor *tensors, int64_t count, int nv, in
         for (int n = 0; n < N && (back ? a > 0 : b < count); back ? --a : ++b) n += tensors[back ? a - 1 : b].numel != 0;
         left -= b - a;
         t.count = 0;
-        t.runs = runs;
+        t.runs = tiles.runs;
         t.tiles = 0;
         t.keep_tile = ~0u;
         for (int64_t i = a; i < b; ++i) {
             const gs_tensor &x = tensors[i];
             if (x.numel == 0) continue;
             const int64_t bytes = x.numel * size_of(x);
-            if (t.keep_tile == ~0u && at + bytes > keep_from) t.keep_tile = t.tiles + (uint32_t)(keep_from > at ? (keep_from - at) / (16 * tile_vecs) : 0);
+            if (t.keep_tile == ~0u && at + bytes > keep_from) t.keep_tile = t.tiles + (uint32_t)(keep_from > at ? (keep_from - at) >> (tiles.shift + 4) : 0);
             at += bytes;
             t.first[t.count] = t.tiles;
-            t.e[t.count++] = {x.data, x.out ? x.out : const_cast<void *>(x.data), x.numel * 2 + (x.dtype == GS_BF16)};
-            t.tiles += (uint32_t)tiles_of(x, tile_vecs);
+            t.e[t.count++] = Table<N>::S::of(x);
+            t.tiles += (uint32_t)tiles_of(x, tiles.shift);
         }
         if (t.count == 0) continue;
         for (int i = t.count; i < N; ++i) t.first[i] = ~0u;
@@ -364,18 +403,44 @@ static bool touches(const gs_tensor *tensors, int64_t count, const Range &o)
     return false;
 }
 
+// Long tensors in pieces: another list, in memory of the caller's to free.
+static bool cut_long(const gs_tensor *&tensors, int64_t &count, void *&memory)
+{
+    int64_t n = 0, longest = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        n += tensors[i].numel > PIECE ? (tensors[i].numel + PIECE - 1) / PIECE : 1;
+        longest = std::max(longest, tensors[i].numel);
+    }
+    memory = nullptr;
+    if (longest <= PIECE) return true;
+    gs_tensor *to = static_cast<gs_tensor *>(memory = malloc(sizeof(gs_tensor) * (size_t)n));
+    if (!to) return false;
+    n = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        gs_tensor x = tensors[i];
+        for (int64_t left = x.numel; left > 0; left -= PIECE) {
+            x.numel = std::min(left, PIECE);
+            to[n++] = x;
+            x.data = static_cast<char *>(const_cast<void *>(x.data)) + PIECE * size_of(x);
+            if (x.out) x.out = static_cast<char *>(x.out) + PIECE * size_of(x);
+        }
+    }
+    tensors = to;
+    count = n;
+    return true;
+}
+
 template <int N>
 static hipError_t norm(const gs_tensor *tensors, int64_t count, double *d_sqnorm, int accumulate, void *ws, hipStream_t stream)
 {
-    const int runs = runs_for(tensors, count, NORM_NV, GS_SQNORM_MAX_BLOCKS);
-    const int64_t tiles = (int64_t)tiles_of(tensors, count, (int64_t)TENSOR_BLOCK * NORM_NV * runs);
+    const Tiles tiles = tiles_for<NORM_NV>(tensors, count, GS_SQNORM_MAX_BLOCKS);
     Meeting meet = {};
-    if (tiles > 0 && tiles <= MEET_MAX && count <= N) meet = {static_cast<uint64_t *>(ws), next_tag(), (int)tiles};
+    if (tiles.count > 0 && tiles.count <= MEET_MAX) meet = {static_cast<uint64_t *>(ws), next_tag(), (int)tiles.count};
     int64_t bytes = 0, done = 0;
     for (int64_t i = 0; i < count; ++i) bytes += tensors[i].numel * size_of(tensors[i]);
     double *partials = static_cast<double *>(ws);
-    hipError_t e = for_tables<N>(tensors, count, NORM_NV, runs, false, bytes - GS_KEEP_BYTES, [&](const Table<N> &t) {
-        k_tensors_sqnorm<N, NORM_NV><<<t.tiles, TENSOR_BLOCK, 0, stream>>>(t, partials + done, meet, d_sqnorm, accumulate);
+    hipError_t e = for_tables<N>(tensors, count, tiles, false, bytes - GS_KEEP_BYTES, [&](const Table<N> &t) {
+        k_tensors_sqnorm<N, NORM_NV><<<t.tiles, TENSOR_BLOCK, 0, stream>>>(t, partials + done, meet, (int)done, d_sqnorm, accumulate);
         done += t.tiles;
         return hipGetLastError();
     });
@@ -391,8 +456,8 @@ static hipError_t norm(const gs_tensor *tensors, int64_t count, double *d_sqnorm
 template <int N>
 static hipError_t clip(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, float max_norm, float *d_norm, hipStream_t stream)
 {
-    const int runs = runs_for(tensors, count, CLIP_NV, 1u << 23);
-    hipError_t e = for_tables<N>(tensors, count, CLIP_NV, runs, true, INT64_MAX, [&](const Table<N> &t) {
+    const Tiles tiles = tiles_for<CLIP_NV>(tensors, count, 1u << 23);
+    hipError_t e = for_tables<N>(tensors, count, tiles, true, INT64_MAX, [&](const Table<N> &t) {
         k_tensors_clip<N, CLIP_NV><<<t.tiles, TENSOR_BLOCK, 0, stream>>>(t, d_sqnorm, max_norm, d_norm);
         d_norm = nullptr;              // written by the first launch
         return hipGetLastError();
@@ -421,8 +486,10 @@ gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqn
     const Range sq = range_of(d_sqnorm, 8, true), ws = range_of(d_workspace, (int64_t)workspace_bytes, true);
     if (touches(tensors, count, sq) || touches(tensors, count, ws) || (sq.lo < ws.hi && ws.lo < sq.hi)) return GS_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = count <= TABLE_SMALL ? norm<TABLE_SMALL>(tensors, count, d_sqnorm, accumulate, d_workspace, st)
-                                        : norm<TABLE>(tensors, count, d_sqnorm, accumulate, d_workspace, st);
+    void *memory;
+    if (!cut_long(tensors, count, memory)) return GS_ERR_NOMEM;
+    const hipError_t e = (count <= TABLE_SMALL ? norm<TABLE_SMALL> : norm<TABLE_IN_PLACE>)(tensors, count, d_sqnorm, accumulate, d_workspace, st);
+    free(memory);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_grads_sqnorm launch");
 }
 
@@ -433,8 +500,12 @@ gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d
     if (!(max_norm > 0.0f)) return GS_ERR_INVALID_ARG;
     if (gs_status s = outputs_apart(tensors, count, d_sqnorm, d_norm); s != GS_OK) return s;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = count <= TABLE_SMALL ? clip<TABLE_SMALL>(tensors, count, d_sqnorm, max_norm, d_norm, st)
-                                        : clip<TABLE>(tensors, count, d_sqnorm, max_norm, d_norm, st);
+    void *memory;
+    if (!cut_long(tensors, count, memory)) return GS_ERR_NOMEM;
+    bool in_place = true;
+    for (int64_t i = 0; i < count; ++i) in_place = in_place && (!tensors[i].out || tensors[i].out == tensors[i].data);
+    const hipError_t e = (count <= TABLE_SMALL ? clip<TABLE_SMALL> : in_place ? clip<TABLE_IN_PLACE> : clip<TABLE>)(tensors, count, d_sqnorm, max_norm, d_norm, st);
+    free(memory);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_grads_clip launch");
 }
 

@@ -130,7 +130,7 @@ def test_norm_accumulates_and_equals_the_flat_norms():
 
 @pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 128, 129, 255, 256, 257])
 def test_norm_of_any_number_of_workgroups(count):
-    """One tensor a workgroup: up to 256 of them finish by themselves, in one launch up to 128 tensors; the rest take another launch."""
+    """One tensor a workgroup: up to 256 of them finish by themselves, in one launch or two; more take another launch."""
     _, tensors = make([50] * count, [F32] * count, seed=count)
     S = want_sqnorm(tensors)
     for _ in range(3):
@@ -326,3 +326,47 @@ def test_wrong_tensors_are_refused():
             gs.gs_grads_clip([t], sq, bad)
     gs.gs_grads_clip([u[:100], u[100:200]], sq, 1.0, outs=[u[200:300], u[300:400]])        # side by side is fine
     assert ctypes.sizeof(gs.gs_tensor) == 32
+
+
+@pytest.mark.parametrize("count", [15, 16, 17, 159, 160, 161, 239, 240, 241, 320, 321, 480, 481])
+def test_lists_at_the_lines_between_launches(count):
+    """Norm and clip of lists as long as a launch takes, and one tensor longer, with empty tensors among them; all in place, all elsewhere,
+    and one of many elsewhere."""
+    sizes = [(i * 29) % 77 + 1 for i in range(count)]
+    sizes = [n for i, n in enumerate(sizes) for n in ([n, 0] if i % 50 == 7 else [n])]
+    kinds = kinds_of(sizes, "mixed")
+    _, tensors = make(sizes, kinds, seed=count, lead=1)
+    S = want_sqnorm(tensors)
+    sq = sqnorm(tensors)
+    assert float(sq) == pytest.approx(S, rel=1e-14)
+    max_norm = 0.3 * math.sqrt(S)
+    want = [want_clip(t, float(sq), max_norm) for t in tensors]
+    _, into = make(sizes, kinds, seed=9, lead=1)
+    gs.gs_grads_clip(tensors, sq, max_norm, outs=into)
+    assert all(same_bits(a, b) for a, b in zip(into, want))
+    copies = [t.clone() for t in tensors]
+    gs.gs_grads_clip(copies, sq, max_norm)
+    assert all(same_bits(a, b) for a, b in zip(copies, want))
+    into[3].fill_(7.0)
+    gs.gs_grads_clip(tensors, sq, max_norm, outs=[into[3] if i == 3 else None for i in range(len(tensors))])
+    assert all(same_bits(into[3] if i == 3 else t, want[i]) for i, t in enumerate(tensors))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_tensors_longer_than_a_piece(dtype):
+    """More than 2^31 elements, from an odd one on: the norm is its parts', the clip that of short tensors over the same elements."""
+    n = 2 ** 31 + 12_345
+    flat = torch.full((n + 64,), 2.0 ** -10, dtype=dtype, device=DEV)
+    ends = [3, 4, 2 ** 31 + 2, 2 ** 31 + 3, 2 ** 31 + 4, n + 2]
+    flat[torch.tensor(ends, device=DEV)] = torch.tensor([1.0, 2.0, 3.0, 4.0, 5.0, 6.0], device=DEV).to(dtype)
+    flat[2], flat[n + 3] = 9.0, 9.0
+    t = flat[3:n + 3]
+    S = (n - 6) * 2.0 ** -20 + 1 + 4 + 9 + 16 + 25 + 36
+    sq = sqnorm([t])
+    assert float(sq) == pytest.approx(S, rel=1e-12)
+    gs.gs_grads_clip([t], sq, 0.25 * math.sqrt(S))
+    want = want_clip(torch.tensor([2.0 ** -10, 1.0, 2.0, 3.0, 4.0, 5.0, 6.0], device=DEV).to(dtype), float(sq), 0.25 * math.sqrt(S))
+    assert same_bits(flat[torch.tensor(ends, device=DEV)], want[1:]) and float(flat[2]) == float(flat[n + 3]) == 9.0
+    flat[torch.tensor(ends, device=DEV)] = want[0].to(dtype)
+    for a in range(3, n + 3, 1 << 28):
+        assert bool((flat[a:min(a + (1 << 28), n + 3)] == want[0]).all())
