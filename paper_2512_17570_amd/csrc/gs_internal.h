@@ -141,5 +141,17 @@ StepConsts make_consts(const gs_adamw_hparams &hp);
 gs_status hip_fail(hipError_t e, const char *what);
 uint32_t next_tag();      // of a launch whose last workgroup finishes it (gs_device.h)
 
+// What a call reads or writes at an address.  Nothing (no bytes, or a null pointer) overlaps nothing, wherever it lies.
+struct Range {
+    uintptr_t lo, hi;
+    bool out;
+};
+inline Range range_of(const void *p, int64_t bytes, bool out)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, p ? a + (uintptr_t)bytes : a, out};
+}
+inline bool overlap(const Range &a, const Range &b) { return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi; }
+
 }  // namespace gs
 #endif

@@ -955,21 +955,12 @@ static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy 
 }
 
 // ---- checks -----------------------------------------------------------------------------------
-struct Span {
-    uintptr_t lo, hi;
-    bool out;
-};
-static Span span_of(const void *p, int64_t bytes, bool out)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return {a, p ? a + (uintptr_t)bytes : a, out};
-}
-// no output overlaps another array; spans `a` and `b` may, where `skip` says so (an output that is its own input)
-static bool apart(const Span *s, int n, bool skip = false, int a = -1, int b = -1)
+// no output overlaps another array; ranges `a` and `b` may, where `skip` says so (an output that is its own input)
+static bool apart(const Range *s, int n, bool skip = false, int a = -1, int b = -1)
 {
     for (int i = 0; i < n; ++i)
         for (int j = i + 1; j < n; ++j)
-            if ((s[i].out || s[j].out) && !(skip && i == a && j == b) && s[i].lo < s[j].hi && s[j].lo < s[i].hi) return false;
+            if ((s[i].out || s[j].out) && !(skip && i == a && j == b) && overlap(s[i], s[j])) return false;
     return true;
 }
 static bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -1026,9 +1017,9 @@ gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float t
     if (rows && (!good(targets, 8) || !good(logp, 4) || !aligned(row_stats, 4))) return GS_ERR_INVALID_ARG;
     if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
     if (rows == 0) return GS_OK;
-    const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size_of(logits->dtype)), false),
-                      span_of(targets, rows * 8, false), span_of(logp, rows * 4, true), span_of(row_stats, rows * 8, true),
-                      span_of(d_workspace, (int64_t)workspace_bytes, true)};
+    const Range s[] = {range_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size_of(logits->dtype)), false),
+                       range_of(targets, rows * 8, false), range_of(logp, rows * 4, true), range_of(row_stats, rows * 8, true),
+                       range_of(d_workspace, (int64_t)workspace_bytes, true)};
     if (!apart(s, 5)) return GS_ERR_INVALID_ARG;
     hipError_t e = launch_rows<false>(*logits, logits_of(*logits, targets), scaled_by(temperature), logp, row_stats, nullptr, 0, d_workspace,
                                       static_cast<hipStream_t>(stream));
@@ -1043,9 +1034,9 @@ gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, fl
     if (rows == 0) return GS_OK;
     if (!good(targets, 8) || !good(row_stats, 4) || !good(dlogp, 4) || !good_output(*logits, dlogits, dlogits_stride)) return GS_ERR_INVALID_ARG;
     const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
-    const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
-                      span_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), span_of(targets, rows * 8, false),
-                      span_of(row_stats, rows * 8, false), span_of(dlogp, rows * 4, false)};
+    const Range s[] = {range_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
+                       range_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), range_of(targets, rows * 8, false),
+                       range_of(row_stats, rows * 8, false), range_of(dlogp, rows * 4, false)};
     if (!apart(s, 5, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
     GradArgs A = {};
     A.L = logits_of(*logits, targets);
@@ -1078,11 +1069,11 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     if (rows == 0 && accumulate) return GS_OK;
     if (rows) {
         const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
-        const Span s[] = {span_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
-                          span_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), span_of(targets, rows * 8, false),
-                          span_of(old_logp, rows * 4, false), span_of(ref_logp, rows * 4, false), span_of(advantages, rows * 4, false),
-                          span_of(weights, rows * 4, false), span_of(logp, rows * 4, true), span_of(d_stats, 16, true),
-                          span_of(d_workspace, (int64_t)workspace_bytes, true)};
+        const Range s[] = {range_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
+                           range_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), range_of(targets, rows * 8, false),
+                           range_of(old_logp, rows * 4, false), range_of(ref_logp, rows * 4, false), range_of(advantages, rows * 4, false),
+                           range_of(weights, rows * 4, false), range_of(logp, rows * 4, true), range_of(d_stats, 16, true),
+                           range_of(d_workspace, (int64_t)workspace_bytes, true)};
         if (!apart(s, 10, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -1120,9 +1111,9 @@ gs_status gs_preference_loss(const float *logp, const float *ref_logp, const flo
     if (pairs && (!good(offsets, 8) || !good(margins, 4))) return GS_ERR_INVALID_ARG;
     if (!good(d_loss, 4)) return GS_ERR_INVALID_ARG;
     if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
-    const Span s[] = {span_of(logp, tokens * 4, false), span_of(ref_logp, tokens * 4, false), span_of(weights, tokens * 4, false),
-                      span_of(offsets, pairs ? (2 * pairs + 1) * 8 : 0, false), span_of(margins, pairs * 4, true), span_of(dlogp, tokens * 4, true),
-                      span_of(d_loss, 4, true), span_of(d_workspace, (int64_t)workspace_bytes, true)};
+    const Range s[] = {range_of(logp, tokens * 4, false), range_of(ref_logp, tokens * 4, false), range_of(weights, tokens * 4, false),
+                       range_of(offsets, pairs ? (2 * pairs + 1) * 8 : 0, false), range_of(margins, pairs * 4, true), range_of(dlogp, tokens * 4, true),
+                       range_of(d_loss, 4, true), range_of(d_workspace, (int64_t)workspace_bytes, true)};
     if (!apart(s, 8)) return GS_ERR_INVALID_ARG;
     if (pairs == 0 && tokens == 0 && accumulate) return GS_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -359,15 +359,6 @@ static bool good_tensors(const gs_tensor *tensors, int64_t count, bool outs)
 
 // Every output against every other array but its own input: sorted by address, an overlap shows against the furthest end so far, of
 // the outputs and of all.
-struct Range {
-    uintptr_t lo, hi;
-    bool out;
-};
-static Range range_of(const void *p, int64_t bytes, bool out)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return {a, a + (uintptr_t)bytes, out};
-}
 static gs_status outputs_apart(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, const float *d_norm)
 {
     Range few[66], *r = few;
@@ -396,10 +387,8 @@ static gs_status outputs_apart(const gs_tensor *tensors, int64_t count, const do
 }
 static bool touches(const gs_tensor *tensors, int64_t count, const Range &o)
 {
-    for (int64_t i = 0; i < count; ++i) {
-        const Range t = range_of(tensors[i].data, tensors[i].numel * size_of(tensors[i]), false);
-        if (t.lo < o.hi && o.lo < t.hi) return true;
-    }
+    for (int64_t i = 0; i < count; ++i)
+        if (overlap(range_of(tensors[i].data, tensors[i].numel * size_of(tensors[i]), false), o)) return true;
     return false;
 }
 
@@ -484,7 +473,7 @@ gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqn
     if (!d_sqnorm || (reinterpret_cast<uintptr_t>(d_sqnorm) & 7u)) return GS_ERR_INVALID_ARG;
     if (!d_workspace || workspace_bytes < gs_sqnorm_workspace_bytes() || (reinterpret_cast<uintptr_t>(d_workspace) & 7u)) return GS_ERR_WORKSPACE;
     const Range sq = range_of(d_sqnorm, 8, true), ws = range_of(d_workspace, (int64_t)workspace_bytes, true);
-    if (touches(tensors, count, sq) || touches(tensors, count, ws) || (sq.lo < ws.hi && ws.lo < sq.hi)) return GS_ERR_INVALID_ARG;
+    if (touches(tensors, count, sq) || touches(tensors, count, ws) || overlap(sq, ws)) return GS_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     void *memory;
     if (!cut_long(tensors, count, memory)) return GS_ERR_NOMEM;
