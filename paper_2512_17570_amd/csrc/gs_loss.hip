@@ -185,31 +185,37 @@ __device__ __forceinline__ Sums sums_of(const Terms &e, float w, float kl_coef)
     const double pg = (double)w * e.pg, kl = (double)w * e.kl;
     return {{kl_coef != 0.0f ? pg + kl_coef * kl : pg, pg, kl, e.clipped ? (double)w : 0.0}};
 }
-// One row's, by a wave: left in 32 bits, since every workgroup looks at all that are there, and halves of them would be as many words again.
-__device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Sums &s, uint32_t (&w)[4])
+// One row's, by a wave: the policy and the KL term in 64 bits each, as the sums of many rows are held, and a weight as it is.  Their sum with
+// the KL term's factor is made of the sums: every workgroup looks at all words that are there, of which these are five.
+__device__ __forceinline__ void leave_sums(const Meeting &M, int64_t r, const Sums &s, uint32_t (&w)[5])
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint((float)s.x[i]);
+    halves(s.x[1], w[0], w[1]);
+    halves(s.x[2], w[2], w[3]);
+    w[4] = __float_as_uint((float)s.x[3]);
     if ((threadIdx.x & 63) == 0) leave(M, (int)r, w);
 }
-__device__ __forceinline__ void finish_policy(const Meeting &M, uint32_t (&w)[4], float *out, int accumulate)
+__device__ __forceinline__ void finish_policy(const Meeting &M, uint32_t (&w)[5], const Policy &P)
 {
-    if (!last_of(M, !accumulate, w)) return;
-    double x[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = __uint_as_float(w[q]);          // 0 without a slot
+    if (!last_of(M, !P.accumulate, w)) return;
+    double pg = 0.0, kl = 0.0, clipped = 0.0;
+    auto add = [&] {                                       // 0 without a slot
+        pg += __hiloint2double((int)w[1], (int)w[0]);
+        kl += __hiloint2double((int)w[3], (int)w[2]);
+        clipped += __uint_as_float(w[4]);
+    };
+    add();
 #pragma unroll 1
     for (int i = (threadIdx.x & 63) + 64; i < M.n; i += 64) {
         left_words(M, i, w);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] += __uint_as_float(w[q]);
+        add();
     }
+    pg = wave_sum(pg), kl = wave_sum(kl), clipped = wave_sum(clipped);
+    if ((threadIdx.x & 63) == 63) {
+        const double x[4] = {P.kl != 0.0f ? pg + P.kl * kl : pg, pg, kl, clipped};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = wave_sum(x[q]);
-    if ((threadIdx.x & 63) == 63)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) out[q] = (float)((accumulate ? (double)out[q] : 0.0) + x[q]);
-    clear<4>(M);
+        for (int q = 0; q < 4; ++q) P.stats[q] = (float)((P.accumulate ? (double)P.stats[q] : 0.0) + x[q]);
+    }
+    clear<5>(M);
 }
 
 // +0 over a row
@@ -309,9 +315,9 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
             if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
         }
         if (meets && threadIdx.x >= BLOCK - 64) {
-            uint32_t words[4];
+            uint32_t words[5];
             leave_sums(P.meet, r, Sums{}, words);
-            finish_policy(P.meet, words, P.stats, P.accumulate);
+            finish_policy(P.meet, words, P);
         }
         if (out) zero_row<E, BLOCK>(out, L.vocab);
     };
@@ -380,7 +386,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     if constexpr (POLICY) {
         const Terms terms = policy_terms(lp, token, P);
         // by the last wave, which has the fewest vectors
-        uint32_t words[4] = {};
+        uint32_t words[5] = {};
         if (meets && wave == NW - 1) leave_sums(P.meet, r, sums_of(terms, w, P.kl), words);
         const float d = w * terms.slope * P.it;
         if (!out) {
@@ -408,7 +414,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
             if (at >= 0 && at < c.vecs * PER ? (at / PER + skip) % BLOCK == (int)threadIdx.x : single == t)
                 E::store(out + t, d * (1.0f - __builtin_amdgcn_exp2f((zt - m) * P.k) / s));
         }
-        if (meets && wave == NW - 1) finish_policy(P.meet, words, P.stats, P.accumulate);
+        if (meets && wave == NW - 1) finish_policy(P.meet, words, P);
     }
 }
 
@@ -590,9 +596,9 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
         if (run == 0 && threadIdx.x < 64) {
             if (threadIdx.x == 0) A.logp[r] = lp;
             if (A.P.meet.n > 0) {
-                uint32_t words[4];
+                uint32_t words[5];
                 leave_sums(A.P.meet, r, sums, words);
-                finish_policy(A.P.meet, words, A.P.stats, A.P.accumulate);
+                finish_policy(A.P.meet, words, A.P);
             }
         }
     } else if (t >= 0) {
@@ -790,8 +796,9 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
 }
 
 // ---- launchers --------------------------------------------------------------------------------
-// Workgroups that meet with more work behind them than a sum: policy loss, 128 / 200 / 256 rows of 8000 7.0/8.9/9.4 us, with a launch of
-// its own for the sums 8.3; 128 / 256 pairs 5.4/6.9 against 6.6.
+// Workgroups that meet with more work behind them than a sum: each looks at the words of all.  Policy loss, 33 / 64 / 100 / 128 rows of 8000 bf16
+// 5.7/5.6/6.4/6.8 us, with a launch of its own for the sums 6.5/6.7/6.9/7.1; of 32000 7.8/8.1/9.0/9.7 against 8.9/8.8/9.0/9.2, and
+// 32003 fp32 8.3/9.0/10.7/10.5 against 9.1/9.7/9.9/10.2.  128 / 256 pairs 5.4/6.9 against 6.6.
 constexpr int MEET_FEW = 128;
 static Meeting meeting(void *ws, int n) { return {static_cast<uint64_t *>(ws), next_tag(), n}; }
 // of the workgroups that go through n tokens or pairs
@@ -1089,7 +1096,7 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     P.accumulate = accumulate;
     // with few rows the last of them adds up their sums; the workspace's end is theirs, its start holds parts
     const bool meets = rows > 0 && rows <= MEET_FEW && (dlogits || !in_parts(*logits, true));
-    if (meets) P.meet = meeting(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_FEW * 32, (int)rows);
+    if (meets) P.meet = meeting(static_cast<char *>(d_workspace) + (size_t)GS_SQNORM_MAX_BLOCKS * 8 - MEET_FEW * 40, (int)rows);
     hipError_t e = launch_rows<true>(*logits, logits_of(*logits, targets), P, logp, nullptr, dlogits, rows > 1 ? dlogits_stride : logits->vocab, d_workspace, st);
     if (e != hipSuccess) return hip_fail(e, "gs_policy_loss launch");
     if (meets) return GS_OK;
