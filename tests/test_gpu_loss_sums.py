@@ -1,12 +1,14 @@
-"""GPU tests of the losses' sums over tokens: what 64 bits hold and 32 do not, on both sides of the lines between the
+"""GPU tests of the losses' sums over tokens and pairs: what 64 bits hold and 32 do not, on both sides of the lines between the
 launches that add them up."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
+import loss_oracle as O
 from gpu_util import DEV, gs
-from test_gpu_losses import BF16, F32, workspace
+from test_gpu_losses import BF16, F32, f32, within, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +37,58 @@ def test_policy_terms_are_added_in_64_bits(rows, vocab, dtype, gradient, accumul
                       accumulate=accumulate)
     assert not logp.any()
     assert stats.tolist() == [-2.0 ** -46, -2.0 ** -46, 0.0, 0.0]
+
+
+@pytest.mark.parametrize("pairs", [1, 100, 128, 129, 130, 1000, 70_000, 262_000, 262_144, 300_001])
+@pytest.mark.parametrize("low,high", [(15.0, 25.0), (40.0, 60.0), (-1.0, 1.0)])
+def test_preference_loss_of_well_separated_pairs(pairs, low, high):
+    """ln(1 + exp(-h)) turns by h times what h turns by, relatively: from a margin in 64 bits, added in 64 and rounded once."""
+    g = torch.Generator().manual_seed(pairs)
+    h = torch.rand(pairs, generator=g).numpy() * (high - low) + low
+    chosen = -torch.rand(pairs, generator=g).numpy()
+    logp = np.concatenate([chosen, chosen - h]).astype(np.float32)
+    offsets = np.arange(2 * pairs + 1, dtype=np.int64)
+    x = logp.astype(float)
+    h = x[:pairs] - x[pairs:]
+    scale = float(np.float32(1.0 / pairs))
+    want = scale * (np.maximum(-h, 0) + np.log1p(np.exp(-np.abs(h)))).sum()
+    margins, dlogp, loss = (torch.zeros(n, dtype=F32, device=DEV) for n in (pairs, 2 * pairs, 1))
+    gs.gs_preference_loss(f32(logp), None, None, torch.tensor(offsets, device=DEV), gs.PreferenceHParams(beta=1.0, scale=1.0 / pairs), margins, dlogp,
+                          loss, workspace())
+    within(margins, h, 2 * O.U * np.abs(h), "margins")
+    within(loss, np.array([want]), 2 * O.U * want, "loss")
+    up = scale / (1 + np.exp(h))
+    within(dlogp, np.concatenate([-up, up]), np.tile(2 * O.U * up, 2) + O.TINY, "dlogp")
+
+
+def test_preference_loss_of_more_pairs_than_partials():
+    """Every output, sequences of any length, accumulating, the same bits every time."""
+    pairs = 300_001
+    g = torch.Generator().manual_seed(1)
+    offsets = np.concatenate([[0], np.cumsum(torch.randint(0, 5, (2 * pairs,), generator=g).numpy())]).astype(np.int64)
+    tokens = int(offsets[-1])
+    logp = (-torch.rand(tokens, generator=g) * 6).numpy()
+    ref = (logp + torch.randn(tokens, generator=g).numpy() * 0.3).astype(np.float32)
+    w = (torch.rand(tokens, generator=g) < 0.8).float().numpy()
+    w[offsets[5]:offsets[6]] = 0.0
+    hp = gs.PreferenceHParams(beta=0.3, label_smoothing=0.1, scale=1.0 / pairs)
+    e, beta, scale = (float(np.float32(v)) for v in (0.1, 0.3, 1.0 / pairs))
+    r = np.concatenate([[0.0], np.cumsum(np.where(w != 0, w.astype(float) * (logp.astype(float) - ref), 0.0))])
+    sums = r[offsets[1:]] - r[offsets[:-1]]
+    h = beta * (sums[:pairs] - sums[pairs:])
+    want = scale * ((1 - e) * np.log1p(np.exp(-h)) + e * np.log1p(np.exp(h))).sum()
+    slope = scale * beta * (e / (1 + np.exp(-h)) - (1 - e) / (1 + np.exp(h)))
+    d = np.repeat(np.concatenate([slope, -slope]), np.diff(offsets)) * w
+    args = f32(logp), f32(ref), f32(w), torch.tensor(offsets, device=DEV), hp
+    kept = None
+    for first in (0.0, 3.0, 0.0):
+        margins, dlogp, loss = torch.zeros(pairs, device=DEV), torch.full((tokens,), 9.0, device=DEV), torch.full((1,), first, device=DEV)
+        gs.gs_preference_loss(*args, margins, dlogp, loss, workspace(), accumulate=first != 0)
+        # running sums of a million terms of the oracle: 1e-9
+        within(margins, h, 2 * O.U * np.abs(h) + 1e-9, "margins")
+        within(loss, np.array([want + first]), 2 * O.U * (want + first) + 1e-9, "loss")
+        within(dlogp, d, 4 * O.U * np.abs(d) + 1e-9 * scale, "dlogp")
+        if first == 0.0:
+            if kept is not None:
+                assert all(torch.equal(a, b) for a, b in zip(kept, (margins, dlogp, loss)))
+            kept = margins, dlogp, loss
