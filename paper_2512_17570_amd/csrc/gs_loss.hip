@@ -150,8 +150,12 @@ __device__ __forceinline__ Token token_of(const Policy &P, int64_t r)
 __device__ __forceinline__ Terms policy_terms(float logp, const Token &k, const Policy &P)
 {
     Terms t;
-    const float a = k.advantage, ratio = expf(logp - k.old_logp);
-    const float plain = ratio * a, held = fminf(fmaxf(ratio, P.low), P.high) * a;
+    const float a = k.advantage, x = logp - k.old_logp, ratio = expf(x), held = fminf(fmaxf(ratio, P.low), P.high) * a;
+    float plain = ratio * a;
+    if (ratio == INFINITY && x < INFINITY) {      // too large for 32 bits, which its product with no advantage or a tiny one is not
+        const float root = expf(0.25f * fminf(x, 300.0f));
+        plain = a * root * root * root * root;
+    }
     t.clipped = held < plain;     // NaN: the plain product, which then is one
     t.pg = -(t.clipped ? held : plain);
     t.slope = t.clipped ? 0.0f : -plain;

@@ -92,3 +92,37 @@ def test_preference_loss_of_more_pairs_than_partials():
             if kept is not None:
                 assert all(torch.equal(a, b) for a, b in zip(kept, (margins, dlogp, loss)))
             kept = margins, dlogp, loss
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(8, 50, BF16), (8, 4000, F32), (150, 2000, BF16), (8, 70_000, BF16), (200, 100_000, F32)])
+def test_ratios_beyond_32_bits(rows, vocab, dtype):
+    """Tokens that the old policy gave next to nothing: a ratio over the largest 32-bit number times no advantage, or a tiny one, is what the
+    formula has, and the other tokens' loss and gradient are theirs."""
+    g = torch.Generator().manual_seed(rows)
+    z = (torch.randn(rows, vocab, generator=g) * 2).to(dtype).to(DEV)
+    t = torch.randint(0, vocab, (rows,), generator=g)
+    zz = z.double().cpu().numpy()
+    lp, bound, live = O.token_logp(zz, t.numpy(), 1.0)
+    old = (lp - 0.05).astype(np.float32)
+    adv = torch.randn(rows, generator=g).numpy()
+    old[1], adv[1] = -300.0, 0.0
+    old[2], adv[2] = -150.0, -0.0
+    old[3], adv[3] = lp[3] - 89.5, -2e-38
+    old[4], adv[4] = lp[4] - 95.0, -2e-38
+    old[5], adv[5] = lp[5] - 200.0, 1.0                  # clipped
+    old[6], adv[6] = -900.0, 0.0
+    weights = np.full(rows, 1e-3, np.float32)
+    rest = np.arange(rows) != 6                          # over the largest 64-bit number too, times 0
+    held = old.copy()
+    held[5] = lp[5] - 1.0                                # clipped as well: the same terms, with a bound of their size
+    stats, off_stats, d, o = O.policy(lp[rest], bound[rest], live[rest], held[rest].astype(float), None, adv[rest].astype(float),
+                                      weights[rest].astype(float), 0.2, 0.2, 0.0)
+    dlogp, off = np.insert(d, 6, 0.0), np.insert(o, 6, 0.0)
+    want, g_bound = O.dlogits(zz, t.numpy(), 1.0, dlogp, off, dtype == BF16)
+    for gradient in (True, False):
+        out = torch.full_like(z, 7.0) if gradient else None
+        logp, got = torch.zeros(rows, device=DEV), torch.zeros(4, device=DEV)
+        gs.gs_policy_loss(z, t.to(DEV), f32(old), None, f32(adv), f32(weights), gs.PolicyHParams(), logp, out, got, workspace())
+        within(got, stats, off_stats, "stats")
+        if gradient:
+            within(out, want, g_bound, "dlogits")
