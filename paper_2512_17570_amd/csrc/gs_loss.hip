@@ -886,18 +886,27 @@ static int64_t vecs_of(const gs_logits &X)
     return X.vocab / (X.dtype == GS_BF16 ? Bf16::PER : F32::PER) + (on_lines ? 0 : 7);
 }
 // Whether rows go in parts though they could be held: a long row takes one CU's share of the memory's rate, unless there are about as many
-// rows as CUs.  One launch against one without a gradient, two with one.  us, held against parts, bf16:
-//   rows              1           16           64           128          256
-//   65536, scored     6.1/4.3     6.7/5.7      6.9/6.6      7.2/7.9      8.7/10.5
-//   131072, scored    8.8/4.3     9.7/5.1      10.1/8.2     11.6/10.7    17.9/17.0
-//   65536, policy     7.6/6.5     8.1/7.8      8.4/10.7     9.7/14.0
-//   131072, policy    12.7/6.6    13.4/8.5     13.9/13.8    16.7/21.0
-// (32000: scored 4.4/3.8 with one row and 4.8/4.8 with 16, policy 5.5/6.4.)
+// rows as CUs.  One launch against one without a gradient, two with one.  By elements, of which both types take as long from some rows on: a
+// row's exponentials are as many.  us, held against parts:
+//   rows                       1           16           32           64           128          256
+//   32768 fp32, scored         4.1/4.0     5.0/4.2      4.5/4.1      4.9/4.2      5.6/4.8      7.0/6.1
+//   49152 bf16, scored         4.6/3.8     5.0/4.3      5.0/4.4      5.1/4.9      5.4/5.6      6.5/7.5
+//   81920 fp32, scored         6.2/4.1     6.8/4.6      6.7/5.2      8.6/5.8      9.6/10.2     14.7/16.2
+//   81920 bf16, scored         6.2/4.0     6.7/4.5      6.6/5.3      6.6/5.9      7.5/7.1      9.3/11.5
+//   131072 bf16, scored        8.1/4.0     8.4/4.1      8.5/4.7      9.4/6.0      10.5/8.8     16.2/15.5
+//   32768 fp32, policy         5.6/6.5     7.4/7.8      7.8/8.8      8.0/10.7     11.2/16.1
+//   49152 fp32, policy         7.4/6.7     9.3/8.3      9.4/9.7      10.7/12.3    13.8/20.5
+//   49152 bf16, policy         6.5/6.7     8.3/8.3      8.6/8.5      8.8/10.8     10.0/13.9
+//   81920 fp32, policy         10.4/6.8    10.7/9.1     12.4/10.5    14.1/15.9    18.2/27.2
+//   81920 bf16, policy         8.7/6.8     10.1/8.5     10.3/10.4    11.3/12.6    13.5/19.8
+//   131072 bf16, policy        12.9/7.0    13.7/8.4     14.4/10.7    15.5/15.4    17.6/25.2
+// (20480 fp32: scored 3.2/3.6 with one row and 3.4/4.1 with 16, policy 5.0/6.7 and 6.1/7.8; 32000 bf16: scored 3.8/3.9 and 4.1/4.1.)
 static bool in_parts(const gs_logits &X, bool gradient)
 {
-    const int64_t vecs = vecs_of(X);
-    if (vecs > HELD_MAX) return true;
-    return X.rows <= (vecs > 12 * 1024 ? (gradient ? 64 : 256) : vecs > 5000 ? (gradient ? 16 : 64) : 0);
+    if (vecs_of(X) > HELD_MAX) return true;
+    const int64_t n = X.vocab;
+    if (gradient) return X.rows <= (n > 100000 ? 64 : n > 60000 ? 32 : n > 45000 ? 16 : 0);
+    return X.rows <= (n > 55000 ? 128 : n > 30000 ? 64 : 0);
 }
 
 template <typename E>

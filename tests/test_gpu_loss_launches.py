@@ -7,7 +7,7 @@ import torch
 
 import loss_oracle as O
 from gpu_util import DEV, gs
-from test_gpu_losses import BF16, F32, Rows, f32, policy_check, within, workspace
+from test_gpu_losses import BF16, F32, Rows, logp_check, policy_check, within, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -18,6 +18,18 @@ def test_policy_loss_of_many_rows_in_parts(rows, vocab, dtype, kw):
     """Rows too long to be held, more of them than meet in a launch: the sums are another launch's, of the log-probabilities that the
     gradient's, or the joining one, has left."""
     policy_check(Rows(rows, vocab, dtype, seed=rows, offset=1 if kw.get("in_place") else 0, gap=3 if kw.get("in_place") else 0), **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [1, 16, 17, 32, 33, 64, 65, 128, 129])
+@pytest.mark.parametrize("line", [30_000, 45_000, 55_000, 60_000, 100_000])
+def test_few_rows_held_and_in_parts(line, rows, dtype):
+    for vocab in (line, line + 1):
+        if vocab > 98_000 and dtype == F32:
+            continue
+        x = Rows(rows, vocab, dtype, seed=rows, offset=rows % 3, prompt=0.2 if rows > 1 else 0.0)
+        logp_check(x, stats=rows % 2 == 0)
+        policy_check(x, in_place=True, accumulate=rows % 2 == 1)
 
 
 def long_batch(rows, vocab, dtype):

@@ -226,6 +226,22 @@ def test_vocabularies_at_the_lines_between_kernels(lib, dtype):
                     check_batch(lib, Batch(rows, vecs * per + d, dtype, offset, gap))
 
 
+# (type, vocabulary, rows, rows in parts faster) where one is ahead by 5 % and more
+SCORED = [(F32, 20_480, 1, 0), (F32, 20_480, 32, 0), (F32, 24_576, 16, 0), (F32, 32_768, 16, 1), (F32, 65_536, 64, 1), (F32, 57_344, 128, 1), (F32, 57_344, 192, 0),
+          (F32, 81_920, 96, 1), (F32, 81_920, 256, 0), (BF16, 40_960, 24, 1), (BF16, 40_960, 128, 0), (BF16, 81_920, 96, 1), (BF16, 114_688, 192, 0),
+          (BF16, 131_072, 128, 1), (BF16, 163_840, 256, 0), (BF16, 16_000, 1, 0)]
+POLICY = [(F32, 20_480, 1, 0), (F32, 32_768, 1, 0), (F32, 32_768, 16, 0), (F32, 49_152, 4, 1), (F32, 49_152, 48, 0), (F32, 65_536, 32, 1), (F32, 65_536, 64, 0),
+          (F32, 98_000, 32, 1), (F32, 98_000, 64, 0), (BF16, 40_960, 4, 0), (BF16, 57_344, 16, 1), (BF16, 57_344, 64, 0), (BF16, 131_072, 48, 1),
+          (BF16, 131_072, 96, 0), (BF16, 180_000, 64, 1)]
+
+
+def test_rows_go_in_parts_where_that_is_faster(lib):
+    for dtype, vocab, rows, parts in SCORED:
+        assert token_logp(lib, Batch(rows, vocab, dtype), False)[0].is_a("k_part" if parts else "k_held"), (dtype, vocab, rows)
+    for dtype, vocab, rows, parts in POLICY:
+        assert policy_loss(lib, Batch(rows, vocab, dtype), True, 0)[0].is_a("k_part" if parts else "k_held"), (dtype, vocab, rows)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_numbers_of_rows_at_their_lines(lib, dtype):
     for rows in (1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 1000, 2048, 2049, 3971, 3972, 4096, 4097, 50_000):
