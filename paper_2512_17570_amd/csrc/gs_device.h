@@ -101,6 +101,8 @@ struct Meeting {
     int n;                        // 0: no meeting, another launch finishes
 };
 constexpr int MEET_MAX = 256;     // every workgroup reads the slots of all
+// word q of slot i: those of a kind side by side, so that a wave's loads are whole lines
+__device__ __forceinline__ uint64_t *word(const Meeting &M, int i, int q) { return M.slots + (int64_t)q * M.n + i; }
 
 // by lane 0 of the wave that looks afterwards; alone, there is nothing to leave
 template <int W>
@@ -109,7 +111,7 @@ __device__ __forceinline__ void leave(const Meeting &M, int me, const uint32_t (
     if (M.n == 1) return;
 #pragma unroll
     for (int i = 0; i < W; ++i)
-        __hip_atomic_store(M.slots + (int64_t)me * W + i, (uint64_t)M.tag << 32 | w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(word(M, me, i), (uint64_t)M.tag << 32 | w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 // By the whole wave, whose lane 0 has in w what it has left: true in the workgroup that finishes, with the words of slot `lane` in w;
 // left_words() has those of later slots.  Up to 64 slots and with `again` (a result may be written twice) every one that sees all may, since it
@@ -132,7 +134,7 @@ __device__ __forceinline__ bool last_of(const Meeting &M, bool again, uint32_t (
     for (int i = lane; i < M.n; i += 64) {
         uint64_t x[W];
 #pragma unroll
-        for (int q = 0; q < W; ++q) x[q] = __hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int q = 0; q < W; ++q) x[q] = __hip_atomic_load(word(M, i, q), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
         for (int q = 0; q < W; ++q) {
             here = here && (uint32_t)(x[q] >> 32) == M.tag;
@@ -149,7 +151,7 @@ template <int W>
 __device__ __forceinline__ void left_words(const Meeting &M, int i, uint32_t (&w)[W])
 {
 #pragma unroll
-    for (int q = 0; q < W; ++q) w[q] = (uint32_t)__hip_atomic_load(M.slots + (int64_t)i * W + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int q = 0; q < W; ++q) w[q] = (uint32_t)__hip_atomic_load(word(M, i, q), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 template <int W>
 __device__ __forceinline__ void clear(const Meeting &M)

@@ -811,9 +811,9 @@ __global__ __launch_bounds__(SUM_BLOCK) void k_zero(float *p, int64_t n)
 }
 
 // ---- launchers --------------------------------------------------------------------------------
-// Workgroups that meet with more work behind them than a sum: each looks at the words of all.  Policy loss, 33 / 64 / 100 / 128 rows of 8000 bf16
-// 5.7/5.6/6.4/6.8 us, with a launch of its own for the sums 6.5/6.7/6.9/7.1; of 32000 7.8/8.1/9.0/9.7 against 8.9/8.8/9.0/9.2, and
-// 32003 fp32 8.3/9.0/10.7/10.5 against 9.1/9.7/9.9/10.2.  128 / 256 pairs 5.4/6.9 against 6.6.
+// Workgroups that meet with more work behind them than a sum: each looks at the words of all.  Policy loss, 64 / 100 / 128 rows of 8000 bf16
+// 5.8/6.1/6.3 us, with a launch of its own for the sums 6.7/6.9/7.1; of 32000 8.1/9.2/8.9 against 8.8/9.0/9.2, and 32003 fp32
+// 8.2/9.4/10.3 against 9.7/9.9/10.2.  128 / 256 pairs 5.4/6.9 against 6.6.
 constexpr int MEET_FEW = 128;
 static Meeting meeting(void *ws, int n) { return {static_cast<uint64_t *>(ws), next_tag(), n}; }
 // of the workgroups that go through n tokens or pairs
