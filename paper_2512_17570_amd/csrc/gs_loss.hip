@@ -152,9 +152,11 @@ __device__ __forceinline__ Terms policy_terms(float logp, const Token &k, const 
     Terms t;
     const float a = k.advantage, x = logp - k.old_logp, ratio = expf(x), held = fminf(fmaxf(ratio, P.low), P.high) * a;
     float plain = ratio * a;
-    if (ratio == INFINITY && x < INFINITY) {      // too large for 32 bits, which its product with no advantage or a tiny one is not
+    // too large for 32 bits, which its product with no advantage or a tiny one is not
+    const bool beyond = ratio == INFINITY && x < INFINITY;
+    if (__builtin_expect(__ballot(beyond) != 0, 0)) {
         const float root = expf(0.25f * fminf(x, 300.0f));
-        plain = a * root * root * root * root;
+        plain = beyond ? a * root * root * root * root : plain;
     }
     t.clipped = held < plain;     // NaN: the plain product, which then is one
     t.pg = -(t.clipped ? held : plain);
