@@ -490,8 +490,9 @@ void gs_pinned_free(void *ptr);
  *     dlogp/dz_i = it ([i = t] - exp(it (z_i - M)) / S).
  * A target outside [0, vocab) (-1, -100: padding, a prompt) marks a row without a token: nothing in its logits
  * counts, its logp is 0 and its gradient +0.  Logits may hold -inf (excluded tokens); a row of nothing
- * else, or one with a NaN or +inf, gives NaN, as the formula does.  Maxima, sums and
- * log-probabilities are held in 32 bits, sums over tokens in 64; gradients are rounded once, to the logits' type.
+ * else, or one with a NaN or +inf, gives NaN, as the formula does.  Maxima, sums,
+ * log-probabilities and what a token adds to a loss are held in 32 bits, sums over tokens and pairs in 64; gradients are rounded once, to the
+ * logits' type.
  * All results are the same from call to call.
  * ------------------------------------------------------------------------------------------ */
 
@@ -501,7 +502,7 @@ typedef enum {
 } gs_dtype;
 
 /* rows x vocab logits; row r starts at element r * row_stride.  data: device, aligned to its type; row_stride >= vocab
- * (any value with one row), vocab in [1, 2^30].  rows == 0 is an empty batch (pointers are then not looked at). */
+ * (any value with one row), vocab in [1, 2^30], rows up to 2^40.  rows == 0 is an empty batch (pointers are then not looked at). */
 typedef struct {
     const void *data;
     int64_t rows;
@@ -587,7 +588,7 @@ typedef struct {
  *   margins    device fp32, `pairs`;  dlogp: device fp32, `tokens`
  *   d_loss     device fp32, one value; added to what is there with accumulate != 0
  *   workspace  as for gs_grad_sqnorm
- * dlogp may not overlap an input.  An empty sequence has D = 0; pairs == 0 leaves a loss of 0 and dlogp +0.
+ * dlogp may not overlap an input.  An empty sequence has D = 0; pairs == 0 leaves a loss of 0 and dlogp +0.  Up to 2^40 tokens and 2^23 - 1 pairs.
  */
 gs_status gs_preference_loss(const float *logp, const float *ref_logp, const float *weights, int64_t tokens,
                              const int64_t *offsets, int64_t pairs, const gs_preference_hparams *hp, float *margins, float *dlogp,
@@ -608,7 +609,7 @@ typedef struct {
 #define GS_MAX_TENSORS 65536
 
 /*
- * S = sum over all elements of all tensors of g^2, squares and sum in fp64, in a fixed order.  *d_sqnorm, accumulate, the
+ * S = sum over all elements of all tensors (up to 2^44 together) of g^2, squares and sum in fp64, in a fixed order.  *d_sqnorm, accumulate, the
  * workspace as for gs_grad_sqnorm; the step reads *d_sqnorm as it does that call's.
  *   tensors   host array of `count` (0 .. GS_MAX_TENSORS) tensors, copied by value; empty tensors may be among them, of which no
  *             address is looked at; `out` is not looked at

@@ -105,11 +105,11 @@ struct F32 {
 // single again.  Only what lies in the row is touched.
 struct Cut {
     int head, vecs, singles;      // singles: those in front and behind together
-    template <int PER> static __device__ __forceinline__ Cut of(const void *p, int n, bool vectors)
+    template <int PER> static __device__ __forceinline__ Cut of(const void *p, int n)
     {
         constexpr int SIZE = 16 / PER;
         Cut c;
-        c.head = vectors ? min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE) : n;
+        c.head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE);
         c.vecs = (n - c.head) / PER;
         c.singles = n - c.vecs * PER;
         return c;
@@ -229,7 +229,7 @@ __device__ __forceinline__ void finish_policy(const Meeting &M, uint32_t (&w)[5]
 template <typename E, int BLOCK>
 __device__ __forceinline__ void zero_row(typename E::T *out, int n)
 {
-    const Cut c = Cut::of<E::PER>(out, n, true);
+    const Cut c = Cut::of<E::PER>(out, n);
     u32x4 *v = reinterpret_cast<u32x4 *>(out + c.head);
     for (int i = threadIdx.x; i < c.vecs; i += BLOCK) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, v + i);
     for (int i = threadIdx.x; i < c.singles; i += BLOCK) out[c.single<E::PER>(i)] = 0;
@@ -247,13 +247,12 @@ __device__ __forceinline__ void grad_singly(const typename E::T *row, typename E
 }
 
 // ---- rows held in registers -------------------------------------------------------------------
-// One workgroup a row, as before, but the row is read once: its lanes keep NV vectors each, from the first maximum to the
-// gradient.  The first LO vectors of a lane lie in the row whatever its length; the rest may not, and are -inf.
+// One workgroup a row, which is read once: its lanes keep NV vectors each, from the first maximum to the gradient.  The first LO vectors of a lane lie in the row whatever its length; the rest may not, and are -inf.
 //
 // A wave takes its exponentials from a maximum of its own, as soon as its vectors are there, and waits for the others once, for the
 // row's maximum and sum; its gradient is then f exp2((m_wave - m) k) times those exponentials.  Of the first KEEP vectors the
 // exponentials stay (four bytes an element), of the others the logits (two in bf16), and the exponential is taken again: 8192 x 131072,
-// of 16 vectors none / 5 / 9 kept 0.85/0.78/0.76 ms (with a maximum of the whole row first, and all taken again, 0.89).
+// of 16 vectors none / 5 / 8 kept 0.80/0.78/0.77 ms (with a maximum of the whole row first, and all taken again, 0.89).
 // A longer row leaves room for one workgroup on a CU, whose reading and writing then take turns; other CUs' fill the gaps.  Loads and
 // stores carry the non-temporal hint: written through as well, or without the hint, they lose 1-3 and 2-8 %, loads without it 12 % where
 // nothing is written.  Vectors are counted from a line's start: with rows that start anywhere (50001) 0.143 ms against 0.151.
@@ -332,7 +331,7 @@ __global__ __launch_bounds__(BLOCK) void k_held(Logits L, int64_t row0, int64_t 
     Token token = {};
     if constexpr (POLICY) token = token_of(P, r);
     const T *row = static_cast<const T *>(L.x) + r * L.stride;
-    const Cut c = Cut::of<PER>(row, L.vocab, true);
+    const Cut c = Cut::of<PER>(row, L.vocab);
     // vectors counted from the start of the first one's 128-byte line, so that a wave's accesses are whole lines
     const int skip = in_line(row + c.head), end = skip + c.vecs;
     const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head) - skip;
@@ -444,8 +443,9 @@ __device__ __forceinline__ MaxSum join_parts(MaxSum a, float k)
     return {m, wave_join<false>(a.s * __builtin_amdgcn_exp2f((a.m - base) * k))};
 }
 
-// The part's maximum and its sum of exp2(k (z - maximum)).  Lines that are read again afterwards stay in the caches.  A row has one
-// entry more than parts: the token's own logit, which a gradient written in place would not leave for the others to read.
+// The part's maximum and its sum of exp2(k (z - maximum)).  Lines may stay in the caches for the gradient, which reads them again: they do
+// while a launch's rows are fewer than the memory-side cache holds, of more none is left by then (4096 x 128256 fp32 0.99 ms, 6.3 GB at 6.4 TB/s).
+// A row has one entry more than parts: the token's own logit, which a gradient written in place would not leave for the others to read.
 //   FINISH: the last of a row's workgroups also joins them, for a log-probability with no gradient after it
 struct Finish {
     Meeting meet;
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(PART_BLOCK) void k_part(Logits L, int64_t row0, int
     }
     const int from = (int)part * len, n = min(len, L.vocab - from);
     const typename E::T *row = static_cast<const typename E::T *>(L.x) + r * L.stride + from;
-    const Cut c = Cut::of<E::PER>(row, n, true);
+    const Cut c = Cut::of<E::PER>(row, n);
     const u32x4 *v = reinterpret_cast<const u32x4 *>(row + c.head);
     const float zs = (int)threadIdx.x < c.singles ? E::load(row + c.single<E::PER>(threadIdx.x)) : -INFINITY;
     float m = -INFINITY, s = 0.0f;
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(GRAD_BLOCK) void k_grad(GradArgs A)
         a = {A.row_stats[2 * r], A.row_stats[2 * r + 1]};
     }
     const bool vectors = d == 0.0f || common(row, out);
-    const Cut c = Cut::of<PER>(d == 0.0f ? out : row, L.vocab, true);
+    const Cut c = Cut::of<PER>(d == 0.0f ? out : row, L.vocab);
     const int skip = in_line((d == 0.0f ? out : row) + c.head), end = skip + c.vecs;
     const int i0 = (int)run * GRAD_VECS + (int)threadIdx.x;
     u32x4 *vo = reinterpret_cast<u32x4 *>(out + c.head) - skip;
@@ -896,6 +896,7 @@ static int64_t vecs_of(const gs_logits &X)
 //   81920 fp32, scored         6.2/4.1     6.8/4.6      6.7/5.2      8.6/5.8      9.6/10.2     14.7/16.2
 //   81920 bf16, scored         6.2/4.0     6.7/4.5      6.6/5.3      6.6/5.9      7.5/7.1      9.3/11.5
 //   131072 bf16, scored        8.1/4.0     8.4/4.1      8.5/4.7      9.4/6.0      10.5/8.8     16.2/15.5
+//   (the policy loss with its gradient; without one it takes the same lines)
 //   32768 fp32, policy         5.6/6.5     7.4/7.8      7.8/8.8      8.0/10.7     11.2/16.1
 //   49152 fp32, policy         7.4/6.7     9.3/8.3      9.4/9.7      10.7/12.3    13.8/20.5
 //   49152 bf16, policy         6.5/6.7     8.3/8.3      8.6/8.5      8.8/10.8     10.0/13.9
