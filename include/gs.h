@@ -528,7 +528,7 @@ gs_status gs_token_logp(const gs_logits *logits, const int64_t *targets, float t
  * with (M, S) as gs_token_logp left them for the same logits, targets and temperature.  A row with dlogp[r] == 0, or without a token,
  * gets +0 whatever it holds.
  *   dlogits      device, the logits' type and shape, row r at element r * dlogits_stride (>= vocab); may be the logits
- *                themselves (same address and stride), else must not overlap them
+ *                themselves (same address and stride), else must not overlap them (rows of one buffer in turn do not)
  */
 gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, float temperature, const float *row_stats,
                              const float *dlogp, void *dlogits, int64_t dlogits_stride, void *stream);

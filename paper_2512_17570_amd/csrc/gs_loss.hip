@@ -989,7 +989,7 @@ static hipError_t launch_rows(const gs_logits &X, const Logits &L, const Policy 
 }
 
 // ---- checks -----------------------------------------------------------------------------------
-// no output overlaps another array; ranges `a` and `b` may, where `skip` says so (an output that is its own input)
+// no output overlaps another array; ranges `a` and `b` may, where `skip` says so
 static bool apart(const Range *s, int n, bool skip = false, int a = -1, int b = -1)
 {
     for (int i = 0; i < n; ++i)
@@ -1020,6 +1020,15 @@ static bool good_output(const gs_logits &x, const void *out, int64_t stride)
 {
     if (x.rows > 1 && stride < x.vocab) return false;
     return good(out, size_of(x.dtype)) && extent(x.rows, x.vocab, stride, size_of(x.dtype)) >= 0;
+}
+// Whether an output may lie where the logits do: it is their own memory, row for row, or its rows lie between theirs, at the same distance.
+static bool fits_logits(const gs_logits &x, const void *out, int64_t stride)
+{
+    if (out == x.data && (x.rows == 1 || stride == x.row_stride)) return true;
+    if (x.rows == 1 || stride != x.row_stride) return false;
+    const int64_t size = size_of(x.dtype), step = stride * size, by = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(x.data)) % step;
+    const int64_t gap = by < 0 ? by + step : by;           // from a row of logits to the next row of the output
+    return gap >= x.vocab * size && step - gap >= x.vocab * size;
 }
 static bool good_temperature(float t) { return t >= 1e-4f && t <= 1e4f; }
 static bool finite_from(float x, float lo) { return std::isfinite(x) && x >= lo; }
@@ -1067,11 +1076,10 @@ gs_status gs_token_logp_grad(const gs_logits *logits, const int64_t *targets, fl
     const int64_t rows = logits->rows, size = size_of(logits->dtype);
     if (rows == 0) return GS_OK;
     if (!good(targets, 8) || !good(row_stats, 4) || !good(dlogp, 4) || !good_output(*logits, dlogits, dlogits_stride)) return GS_ERR_INVALID_ARG;
-    const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
     const Range s[] = {range_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
                        range_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), range_of(targets, rows * 8, false),
                        range_of(row_stats, rows * 8, false), range_of(dlogp, rows * 4, false)};
-    if (!apart(s, 5, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
+    if (!apart(s, 5, fits_logits(*logits, dlogits, dlogits_stride), 0, 1)) return GS_ERR_INVALID_ARG;
     GradArgs A = {};
     A.L = logits_of(*logits, targets);
     A.P = scaled_by(temperature);
@@ -1102,13 +1110,12 @@ gs_status gs_policy_loss(const gs_logits *logits, const int64_t *targets, const 
     if (!good_workspace(d_workspace, workspace_bytes)) return GS_ERR_WORKSPACE;
     if (rows == 0 && accumulate) return GS_OK;
     if (rows) {
-        const bool in_place = dlogits == logits->data && (rows == 1 || dlogits_stride == logits->row_stride);
         const Range s[] = {range_of(logits->data, extent(rows, logits->vocab, logits->row_stride, size), false),
                            range_of(dlogits, extent(rows, logits->vocab, dlogits_stride, size), true), range_of(targets, rows * 8, false),
                            range_of(old_logp, rows * 4, false), range_of(ref_logp, rows * 4, false), range_of(advantages, rows * 4, false),
                            range_of(weights, rows * 4, false), range_of(logp, rows * 4, true), range_of(d_stats, 16, true),
                            range_of(d_workspace, (int64_t)workspace_bytes, true)};
-        if (!apart(s, 10, in_place, 0, 1)) return GS_ERR_INVALID_ARG;
+        if (!apart(s, 10, dlogits && fits_logits(*logits, dlogits, dlogits_stride), 0, 1)) return GS_ERR_INVALID_ARG;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     Policy P = scaled_by(hp->temperature);

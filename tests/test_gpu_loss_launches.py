@@ -32,6 +32,28 @@ def test_few_rows_held_and_in_parts(line, rows, dtype):
         policy_check(x, in_place=True, accumulate=rows % 2 == 1)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab,gap", [(5, 1000, 0), (7, 1003, 5), (3, 50_001, 0), (3, 98_400, 1), (140, 3000, 0)])
+def test_gradients_beside_their_logits(rows, vocab, gap, dtype):
+    """Rows of logits and of gradients in turn in one buffer: as into a buffer of their own, and the logits as they were."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    both = torch.randn(rows, 2 * vocab + gap, generator=g, device=DEV).to(dtype)
+    t = torch.randint(-1, vocab, (rows,), generator=g, device=DEV)
+    adv, old = torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV) - 9
+    for x, out in ((both[:, :vocab], both[:, vocab:2 * vocab]), (both[:, vocab + gap:], both[:, :vocab])):
+        kept, want = x.clone(), torch.empty(rows, vocab, dtype=dtype, device=DEV)
+        logp, rs, stats = torch.zeros(rows, device=DEV), torch.zeros(rows, 2, device=DEV), torch.zeros(4, device=DEV)
+        gs.gs_token_logp(x, t, logp, rs, d_workspace=workspace())
+        for call in (lambda o: gs.gs_token_logp_grad(x, t, rs, adv, o),
+                     lambda o: gs.gs_policy_loss(x, t, old, None, adv, None, gs.PolicyHParams(), logp, o, stats, workspace())):
+            call(want)
+            call(out)
+            assert torch.equal(x, kept)
+            # rows cut in other places take their vectors' exponentials another way round
+            off = 2.0 ** -7 if dtype == BF16 else 1e-5
+            assert float((out.double() - want.double()).abs().max()) <= off * float(want.abs().max())
+
+
 def long_batch(rows, vocab, dtype):
     g = torch.Generator(device=DEV).manual_seed(rows)
     z = torch.empty(rows, vocab, dtype=dtype, device=DEV)

@@ -267,6 +267,23 @@ def test_any_batch(lib, seed):
         check_batch(lib, Batch(rows, vocab, dtype, rng.randrange(64), rng.choice([0, 0, 1, rng.randrange(200)])), rng.randrange(2))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradients_beside_their_logits(lib, dtype):
+    """Rows of logits and of gradients in turn in one buffer do not overlap, from either side; an element further they do."""
+    vocab, size, hp = 1000, SIZE[dtype], (f32 * 4)(1.0, 0.2, 0.2, 0.1)
+    for rows, stride, at, good in ((5, 2000, 1000, True), (5, 2000, -1000, True), (5, 2000, 999, False), (5, 2000, 1001, False), (5, 2000, -1001, False), (5, 2000, -999, False),
+                                   (5, 2007, 1000, True), (5, 2007, 1007, True), (5, 2007, 1008, False), (5, 2007, 3 * 2007 + 1003, True), (5, 2007, 3 * 2007 + 3, False),
+                                   (5, 1999, 1000, False), (1, 2000, 1000, True), (1, 2000, 999, False), (5, 2000, 0, True), (5, 2000, 9000, True), (5, 2000, 2000, False)):
+        x = Logits(A[0], rows, vocab, stride, dtype)
+        out = A[0] + at * size
+        got = [lib.gs_token_logp_grad(ctypes.byref(x), vp(A[2]), f32(1.0), vp(A[4]), vp(A[3]), vp(out), i64(stride), None),
+               lib.gs_policy_loss(ctypes.byref(x), vp(A[2]), hp, vp(A[6]), vp(A[7]), vp(A[8]), vp(A[9]), vp(A[3]), vp(out), i64(stride), vp(A[10]), 0, vp(WS),
+                                  ctypes.c_size_t(WS_BYTES), None)]
+        assert got == ([0, 0] if good else [-1, -1]), (rows, stride, at)
+    x = Logits(A[0], 5, vocab, 2000, dtype)                # rows of another distance do
+    assert lib.gs_token_logp_grad(ctypes.byref(x), vp(A[2]), f32(1.0), vp(A[4]), vp(A[3]), vp(A[0] + 1000 * size), i64(4000), None) == -1
+
+
 @pytest.mark.parametrize("accumulate", [0, 1])
 @pytest.mark.parametrize("pairs", [0, 1, 64, 127, 128, 129, 512, 513, 32_768, 65_537, 262_143, 262_144, 262_145, 600_000, 8_388_607])
 def test_pairs(lib, pairs, accumulate):
