@@ -4,9 +4,9 @@
 // One pass that reads every element (the norm) and one that reads and writes it (the clip): HBM-bound.  A launch takes a
 // table of tensors in its arguments, so nothing is copied to the device first and nothing is kept from call to call; its workgroups
 // are tiles of one tensor each, and find which by a look at the first tile of every tensor.
-//   Measured: 805 M fp32 gradients in 12 tensors, norm 0.468 ms (6.9 TB/s), clip into other buffers 1.00 ms (6.4); 201 M in 48 tensors of
-// both types 65 and 118 us (6.2, 6.8: the end of what the norm read is still in the memory-side cache, 183 us together against 189 in the
-// norm's own order); 48 tensors of 2048 to 8192 bf16 elements 5.0 and 3.6 us on the GPU, 9 to 12 us a pass, as fast as the host calls.  A plain
+//   Measured: 805 M fp32 gradients in 12 tensors, norm 0.474 ms (6.8 TB/s), clip into other buffers 1.00 ms (6.4); 201 M in 48 tensors of
+// both types 64 and 118 us (6.3, 6.8: the end of what the norm read is still in the memory-side cache, 184 us together against 189 in the
+// norm's own order); 48 tensors of 2048 to 8192 bf16 elements 5.3 and 4.0 us on the GPU, 9 to 12 us a pass, as fast as the host calls.  A plain
 // copy reaches 6.7 TB/s on the same card, reading 7.1.
 #include <hip/hip_runtime.h>
 
