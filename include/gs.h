@@ -11,8 +11,8 @@
  * figure).  Because the update is element-wise it may be applied to any contiguous range:
  * in full, split into an immediate part and a deferred part (delay ratio alpha, Sec. 4.4),
  * or chunk by chunk over states that live in host memory (Sec. 2.2 chunk loop; Sec. 4.3).
- *   Beside the step: the losses that post-training takes its gradients from, and the norm and clip of
- * gradients that are many tensors (their own conventions on shapes and alignment stand with them).
+ *   Beside the step: the losses that post-training takes its gradients from, with logits or without, the norm and clip of
+ * gradients that are many tensors, layer norm and dropout (their own conventions on shapes and alignment stand with them).
  *
  * Conventions for every entry point
  *   - Plain C types only.  "device" pointers are HIP device addresses, "host" pointers are
@@ -628,6 +628,130 @@ gs_status gs_grads_sqnorm(const gs_tensor *tensors, int64_t count, double *d_sqn
  */
 gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d_sqnorm, float max_norm, float *d_norm,
                         void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A linear head without its logits.  With x a hidden state (a row of `hidden` bf16 values) and W, b the head's working
+ * weights,
+ *     z_i = sum_h x_h W_ih + b_i                 (products of bf16 values, sums and z in 32 bits, never rounded)
+ * takes the place of a row of logits above: M, S, logp, targets, temperature and rows without a token are as there.  z is
+ * never in memory: the forward pass leaves a maximum and a sum for each tile of words, the gradient makes z again,
+ * a piece of the vocabulary at a time.  Rows without a token, or without a factor, cost no product, and what they hold
+ * counts nowhere.
+ * ------------------------------------------------------------------------------------------ */
+
+/* x: `rows` (0 .. 2^20) hidden states of `hidden` (1 .. 2^17) bf16 values, row r at element r * x_stride; w: `vocab` (1 .. 2^30) rows of
+ * weights, row i at element i * w_stride; strides >= hidden (any value with one row).  bias: `vocab` bf16 values, or NULL.
+ * Every address is a multiple of 2; the products run straight from w where its rows are aligned to 16 bytes and
+ * hidden is a multiple of 64, else from a copy of a piece at a time in the workspace. */
+typedef struct {
+    const uint16_t *x;
+    const uint16_t *w;
+    const uint16_t *bias;
+    int64_t rows, hidden, vocab;
+    int64_t x_stride, w_stride;
+} gs_head;
+
+/* Where gradients go, bf16, each written whole (no sum onto what is there: they are one micro-batch's buffers, as gs_accum_adamw and
+ * gs_accum_add take them); NULL for those that nobody needs.  dx: the shape of x, row r at r * dx_stride; dw: of w, at
+ * i * dw_stride; dbias: `vocab` (also without a bias). */
+typedef struct {
+    uint16_t *dx;
+    uint16_t *dw;
+    uint16_t *dbias;
+    int64_t dx_stride, dw_stride;
+} gs_head_grads;
+
+/* Bytes of device workspace that the calls below need for such a head, with or without a gradient; 0 for sizes that they refuse.
+ * The workspace is aligned to 256 bytes; nothing has to be in it before, and nothing is kept in it from call to call. */
+size_t gs_head_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab, int gradient);
+
+/* gs_token_logp of a head's rows: scoring of sequences, or of the token just drawn (rows == 1). */
+gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temperature, float *logp, float *row_stats, void *d_workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of a loss in x, W and b, from its gradient in the token log-probabilities (of gs_preference_loss, say), with row_stats as
+ * gs_head_logp left them for the same head, targets and temperature:
+ *     dz = dlogp dlogp/dz,   dx = dz W,   dW = dz^T x,   db = sum over rows of dz
+ * dz is rounded once to bf16, sums over words and rows are held in 32 bits and rounded once more.  A row with dlogp == 0, or without a token, gets
+ * dx = +0 whatever it holds.
+ */
+gs_status gs_head_logp_grad(const gs_head *head, const int64_t *targets, float temperature, const float *row_stats, const float *dlogp,
+                            const gs_head_grads *grads, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Cross entropy, with its gradient as of gs_head_logp_grad for dlogp = -weights:
+ *     loss = sum_r weights[r] (-logp_r)
+ *   weights    device fp32, `rows`, or NULL for ones: a mask times whatever the loss is divided by.  Where it is 0 the row is as one without a
+ *              token
+ *   logp       device fp32, `rows`, written
+ *   grads      NULL: no gradient (an evaluation)
+ *   d_loss     device fp32, one value; added to what is there with accumulate != 0 (micro-batches); the sum over rows is held in 64 bits
+ */
+gs_status gs_head_cross_entropy(const gs_head *head, const int64_t *targets, const float *weights, float temperature, float *logp,
+                                const gs_head_grads *grads, float *d_loss, int accumulate, void *d_workspace, size_t workspace_bytes,
+                                void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * What a layer has around its products: layer norm with its gradient, and dropout onto the residual stream.
+ * ------------------------------------------------------------------------------------------ */
+
+/* rows x cols values; row r starts at element r * row_stride.  data: device, aligned to its type; row_stride >= cols (any value with one
+ * row), cols in [1, 2^24], rows up to 2^31.  rows == 0 is an empty batch (of which no address is looked at). */
+typedef struct {
+    const void *data;
+    int64_t rows;
+    int64_t cols;
+    int64_t row_stride;
+    int32_t dtype;          /* gs_dtype */
+} gs_matrix;
+
+/*
+ * Layer norm of each row:
+ *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),   y = (x - mean) rstd gamma + beta
+ * Sums, mean and rstd in 32 bits, the squares after the mean is known; y is rounded once, to x's type.
+ *   gamma, beta   device, `cols` values of weight_dtype each, or NULL for ones and zeros
+ *   eps           >= 0, finite
+ *   y             device, x's type, row r at element r * y_stride; may be x itself (same address and stride)
+ *   row_stats     NULL, or device fp32, 2 x `rows`: (mean, rstd) of every row, for the gradient
+ */
+gs_status gs_layer_norm(const gs_matrix *x, const void *gamma, const void *beta, int32_t weight_dtype, float eps, void *y, int64_t y_stride,
+                        float *row_stats, void *stream);
+
+/* Bytes of device workspace that gs_layer_norm_grad needs; 0 for sizes that it refuses. */
+size_t gs_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Gradient of a layer norm, from that in y:
+ *     xhat = (x - mean) rstd,   g = dy gamma
+ *     dx = rstd (g - sum g / cols - xhat sum g xhat / cols),   dgamma = sum over rows of dy xhat,   dbeta = sum over rows of dy
+ * Sums are held in 32 bits, over rows in parts that are joined in 64; every result is rounded once.  The sums' order is fixed.
+ *   row_stats      (mean, rstd) as gs_layer_norm left them for the same x
+ *   dy, dx         device, x's type, at strides of their own; dx may be dy itself (same address and stride)
+ *   dgamma, dbeta  device, `cols` values of weight_dtype, written; both or neither (NULL)
+ *   workspace      aligned to 256 bytes, of gs_layer_norm_workspace_bytes; not looked at without dgamma
+ */
+gs_status gs_layer_norm_grad(const gs_matrix *x, const void *gamma, int32_t weight_dtype, const float *row_stats, const void *dy,
+                             int64_t dy_stride, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, void *d_workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout, onto a residual or not, over n elements of a flat array:
+ *     out_i = residual_i + (keep(offset + i) ? x_i / (1 - P) : 0),      P = T / 65536,  T = round(65536 p)
+ * with x in 32 bits and one rounding at the end.  keep(e) is bits_e >= T, with 16 random bits for each element e: word (e mod 8) / 2, the lower half for
+ * even e and the upper for odd, of Philox4x32-10 with the key (seed's lower half, its upper half) and the counter (lower, upper half of
+ * e / 8, lower, upper half of *d_step).  So the mask is in no memory: the backward pass is this call on the gradient, without the residual and
+ * with the same numbers, and any part of a tensor may be done by itself with its first element's number as `offset`, with the same bits.
+ * What a dropped element holds (NaN, infinities) does not count.
+ *   x          device, n values of dtype (0 <= n <= 2^40), aligned to their type
+ *   residual   the same, or NULL
+ *   out        the same; may be exactly x or exactly the residual
+ *   p          in [0, 1]; with 1, or as near as makes T 65536, everything is dropped
+ *   seed       of a run, a layer, a place in it; offset: of element 0; offset + n does not pass 2^64
+ *   d_step     NULL for 0, or a device value that the program counts up, so that a captured graph draws anew on each replay
+ */
+gs_status gs_dropout(const void *x, const void *residual, void *out, int64_t n, int32_t dtype, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t *d_step, void *stream);
 
 /* ------------------------------------------------------------------------------------------ */
 const char *gs_strerror(gs_status s);

@@ -122,6 +122,21 @@ class gs_tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+class gs_head(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("hidden", ctypes.c_int64), ("vocab", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64)]
+
+
+class gs_head_grads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("dbias", ctypes.c_void_p), ("dx_stride", ctypes.c_int64),
+                ("dw_stride", ctypes.c_int64)]
+
+
+class gs_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _pp = ctypes.c_void_p      # a table of addresses, as bytes
@@ -600,6 +615,165 @@ def gs_grads_clip(tensors, d_sqnorm, max_norm: float, d_norm=None, outs=None, st
     st = _lib.gs_grads_clip(table, count, _gpu(d_sqnorm, 1, torch.float64, "d_sqnorm"), max_norm,
                             _gpu(d_norm, 1, torch.float32, "d_norm", True), _stream(stream))
     return _check(st, "gs_grads_clip", check)
+
+
+# ---- a head without its logits, layer norm, dropout -----------------------------------------------------------------
+
+_u64 = ctypes.c_uint64
+_sz = ctypes.c_size_t
+_lib.gs_head_workspace_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
+_lib.gs_head_workspace_bytes.restype = _sz
+_lib.gs_head_logp.argtypes = [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]
+_lib.gs_head_logp.restype = ctypes.c_int
+_lib.gs_head_logp_grad.argtypes = [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.gs_head_logp_grad.restype = ctypes.c_int
+_lib.gs_head_cross_entropy.argtypes = [_vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, ctypes.c_int, _vp, _sz, _vp]
+_lib.gs_head_cross_entropy.restype = ctypes.c_int
+_lib.gs_layer_norm.argtypes = [_vp, _vp, _vp, ctypes.c_int32, ctypes.c_float, _vp, _i64, _vp, _vp]
+_lib.gs_layer_norm.restype = ctypes.c_int
+_lib.gs_layer_norm_workspace_bytes.argtypes = [_i64, _i64]
+_lib.gs_layer_norm_workspace_bytes.restype = _sz
+_lib.gs_layer_norm_grad.argtypes = [_vp, _vp, ctypes.c_int32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
+_lib.gs_layer_norm_grad.restype = ctypes.c_int
+_lib.gs_dropout.argtypes = [_vp, _vp, _vp, _i64, ctypes.c_int32, ctypes.c_float, _u64, _u64, _vp, _vp]
+_lib.gs_dropout.restype = ctypes.c_int
+
+
+def _on_current(*tensors) -> None:
+    """Work runs on the current device: a tensor of another one is refused."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _rows_of(x, name: str, dtypes) -> tuple:
+    """(address, rows, columns, row stride) of a 2-D GPU tensor whose rows are contiguous."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is needed")
+    if x.dtype not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(str(d) for d in dtypes)}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if x.dim() != 2 or (x.size(1) > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: a 2-D tensor with contiguous rows is needed")
+    return x.data_ptr(), x.size(0), x.size(1), x.stride(0)
+
+
+def _rows_like(x, name: str, shape: tuple, dtype) -> tuple:
+    """(address, row stride) of such a tensor of a given shape and type."""
+    data, rows, cols, stride = _rows_of(x, name, (dtype,))
+    if (rows, cols) != shape:
+        raise ValueError(f"{name}: shape {(rows, cols)}, {shape} is needed")
+    return data, stride
+
+
+def gs_head_workspace_bytes(rows: int, hidden: int, vocab: int, gradient: bool = True) -> int:
+    return int(_lib.gs_head_workspace_bytes(rows, hidden, vocab, int(bool(gradient))))
+
+
+def _head(x, w, bias) -> gs_head:
+    xp, rows, hidden, xs = _rows_of(x, "x", (torch.bfloat16,))
+    wp, vocab, width, ws = _rows_of(w, "w", (torch.bfloat16,))
+    if width != hidden:
+        raise ValueError(f"w: rows of {width} elements, hidden states have {hidden}")
+    return gs_head(xp, wp, _gpu(bias, vocab, torch.bfloat16, "bias", True), rows, hidden, vocab, xs, ws)
+
+
+def _head_grads(h: gs_head, dx, dw, dbias) -> gs_head_grads:
+    bf16 = torch.bfloat16
+    xp, xs = (None, 0) if dx is None else _rows_like(dx, "dx", (h.rows, h.hidden), bf16)
+    wp, ws = (None, 0) if dw is None else _rows_like(dw, "dw", (h.vocab, h.hidden), bf16)
+    return gs_head_grads(xp, wp, _gpu(dbias, h.vocab, bf16, "dbias", True), xs, ws)
+
+
+def gs_head_logp(x, w, bias, targets, logp, row_stats=None, temperature: float = 1.0, d_workspace=None,
+                 workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
+    """x: hidden states (rows, hidden); w: (vocab, hidden); bias: (vocab,) or None."""
+    h = _head(x, w, bias)
+    _on_current(x, w, bias, targets, logp, row_stats, d_workspace)
+    st = _lib.gs_head_logp(ctypes.byref(h), _gpu(targets, h.rows, torch.int64, "targets"), temperature, _gpu(logp, h.rows, torch.float32, "logp"),
+                           _gpu(row_stats, 2 * h.rows, torch.float32, "row_stats", True), _addr(d_workspace),
+                           _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_head_logp", check)
+
+
+def gs_head_logp_grad(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace, temperature: float = 1.0,
+                      workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
+    h = _head(x, w, bias)
+    _on_current(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace)
+    g = _head_grads(h, dx, dw, dbias)
+    st = _lib.gs_head_logp_grad(ctypes.byref(h), _gpu(targets, h.rows, torch.int64, "targets"), temperature,
+                                _gpu(row_stats, 2 * h.rows, torch.float32, "row_stats"), _gpu(dlogp, h.rows, torch.float32, "dlogp"),
+                                ctypes.byref(g), _addr(d_workspace), _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_head_logp_grad", check)
+
+
+def gs_head_cross_entropy(x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace, temperature: float = 1.0,
+                          accumulate: bool = False, workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
+    """With dx, dw and dbias all None there is no gradient, and less workspace is needed."""
+    h = _head(x, w, bias)
+    _on_current(x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace)
+    g = None if dx is None and dw is None and dbias is None else _head_grads(h, dx, dw, dbias)
+    st = _lib.gs_head_cross_entropy(ctypes.byref(h), _gpu(targets, h.rows, torch.int64, "targets"), _gpu(weights, h.rows, torch.float32, "weights", True),
+                                    temperature, _gpu(logp, h.rows, torch.float32, "logp"), None if g is None else ctypes.byref(g),
+                                    _gpu(d_loss, 1, torch.float32, "d_loss"), int(bool(accumulate)), _addr(d_workspace),
+                                    _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_head_cross_entropy", check)
+
+
+def _norm_weights(cols: int, **weights):
+    """(addresses, type) of a layer norm's vectors, which have one type."""
+    given = [t for t in weights.values() if t is not None]
+    for t in given:
+        if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or t.dtype != given[0].dtype:
+            raise TypeError(f"{', '.join(weights)}: bfloat16 or float32 tensors of one type are needed")
+    dtype = given[0].dtype if given else torch.float32
+    return [_gpu(t, cols, dtype, name, True) for name, t in weights.items()], _DTYPES[dtype]
+
+
+def gs_layer_norm(x, gamma, beta, y, row_stats=None, eps: float = 1e-5, stream=None, check: bool = True) -> int:
+    """x, y: (rows, cols), bfloat16 or float32; gamma, beta: (cols,), of a type of their own, or None."""
+    xp, rows, cols, xs = _rows_of(x, "x", tuple(_DTYPES))
+    yp, ys = _rows_like(y, "y", (rows, cols), x.dtype)
+    (g, b), wt = _norm_weights(cols, gamma=gamma, beta=beta)
+    _on_current(x, gamma, beta, y, row_stats)
+    st = _lib.gs_layer_norm(ctypes.byref(gs_matrix(xp, rows, cols, xs, _DTYPES[x.dtype])), g, b, wt, eps, yp, ys,
+                            _gpu(row_stats, 2 * rows, torch.float32, "row_stats", True), _stream(stream))
+    return _check(st, "gs_layer_norm", check)
+
+
+def gs_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.gs_layer_norm_workspace_bytes(rows, cols))
+
+
+def gs_layer_norm_grad(dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace=None, workspace_bytes: int | None = None, stream=None,
+                       check: bool = True) -> int:
+    """dgamma and dbeta may both be None; then no workspace is needed."""
+    xp, rows, cols, xs = _rows_of(x, "x", tuple(_DTYPES))
+    dyp, dys = _rows_like(dy, "dy", (rows, cols), x.dtype)
+    dxp, dxs = _rows_like(dx, "dx", (rows, cols), x.dtype)
+    (g, dg, db), wt = _norm_weights(cols, gamma=gamma, dgamma=dgamma, dbeta=dbeta)
+    _on_current(dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace)
+    st = _lib.gs_layer_norm_grad(ctypes.byref(gs_matrix(xp, rows, cols, xs, _DTYPES[x.dtype])), g, wt,
+                                 _gpu(row_stats, 2 * rows, torch.float32, "row_stats"), dyp, dys, dxp, dxs, dg, db, _addr(d_workspace),
+                                 _workspace_bytes(d_workspace, workspace_bytes), _stream(stream))
+    return _check(st, "gs_layer_norm_grad", check)
+
+
+def gs_dropout(x, residual, out, p: float, seed: int, offset: int = 0, d_step=None, stream=None, check: bool = True) -> int:
+    """Contiguous tensors of one type and size; residual may be None.  d_step: an int64 GPU tensor, or None."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _DTYPES:
+        raise TypeError("x: a bfloat16 or float32 tensor is needed")
+    n = x.numel()
+    for name, t in (("residual", residual), ("out", out)):
+        if isinstance(t, torch.Tensor) and t.numel() != n:
+            raise ValueError(f"{name}: holds {t.numel()} elements, x has {n}")
+    if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+        raise ValueError("seed, offset: whole numbers of 64 bits are needed")
+    _on_current(x, residual, out, d_step)
+    st = _lib.gs_dropout(_gpu(x, n, x.dtype, "x"), _gpu(residual, n, x.dtype, "residual", True), _gpu(out, n, x.dtype, "out"), n, _DTYPES[x.dtype], p,
+                         seed, offset, _gpu(d_step, 1, torch.int64, "d_step", True), _stream(stream))
+    return _check(st, "gs_dropout", check)
 
 
 def gs_cu_stream_create(num_cus: int, check: bool = True):
