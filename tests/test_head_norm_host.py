@@ -209,11 +209,11 @@ def kernels(request, tmp_path_factory):
     subprocess.run([B.HIPCC, *flags, "--offload-device-only", "-S", "-I", os.path.join(B.ROOT, "include"), "-I", B.CSRC, os.path.join(B.CSRC, request.param),
                     "-o", out], check=True, capture_output=True, text=True)
     text = open(out).read()
-    found = {}
+    found, kernels = {}, {re.search(r"\.name: +(\S+)", b)[1]: b for b in text.split("\n  - .agpr_count:")[1:]}
     for name, block in re.findall(r"\.amdhsa_kernel (\S+)\n(.*?)\.end_amdhsa_kernel", text, re.S):
         number = lambda key: int(re.search(rf"{key} (\d+)", block)[1])  # noqa: E731
         start = text.index(f"\n{name}:")
-        lanes = int(re.search(rf"\.max_flat_workgroup_size: (\d+)\n(?:.*\n)*?.*\.name: +{re.escape(name)}\n", text)[1])
+        lanes = int(re.search(r"\.max_flat_workgroup_size: (\d+)", kernels[name])[1])
         found[name] = number("next_free_vgpr"), number("private_segment_fixed_size"), number("group_segment_fixed_size"), lanes, text[start:text.index(".section", start)]
     assert found
     return found
