@@ -19,12 +19,16 @@ namespace gs {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// a value that all lanes of a wave have, in scalar registers
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
 __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 {
     bf16x2 h = {(__bf16)a, (__bf16)b};             // rounded to nearest even, NaN stays NaN
@@ -32,181 +36,199 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 }
 
 // ---- a tile of a product -----------------------------------------------------------------------
-// C[m][n] = sum_k A[m][k] B[n][k] over a tile of BM x BN, WM x WN waves of MI x NI blocks of 32 x 32 each.  The operands come to LDS
-// BK of k at a time by loads that go there without passing registers, STAGES of them in turn, two on their way while one is worked on.
+// C[m][n] = sum_k A[m][k] B[n][k] over a tile of BM x BN, WM x WN waves of MI x NI blocks of 16 x 16 each.  The operands come to LDS
+// BK of k at a time by loads that go there without passing registers, one stage on its way while another is worked on.
 // An operand is either rows of k (ALONG: k is contiguous) or rows of m or n (k is the distance between rows); the second kind is read from
 // LDS by the transposing load.
-constexpr int BK = 32, STAGES = 4;
+//
+// What bounds it is power: the chip holds its clock (1.9 GHz here, of 2.4) to what the matrix cores, LDS and loads draw together, and each adds to
+// the time.  16 x 16 x 32 products draw least (alone, of random values, 2160 TFLOP/s; 32 x 32 x 16, whose sums go through the registers twice as
+// often, 1900); rows of 128 bytes are whole lines of the caches (64 bytes a row, four stages: 1190 TFLOP/s against 1300 for 8192 x 4096 x 16384, both steps
+// together).  Four waves of 128 x 128, which read a third less LDS: level, they wait where eight do not.
+constexpr int BK = 64, PART = 32, PARTS = BK / PART, STAGES = 2;
 template <int BM_, int BN_, int WM_, int WN_> struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, BLOCK = WAVES * 64;
-    static constexpr int MI = BM / WM / 32, NI = BN / WN / 32;
+    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
     static constexpr int STAGE = (BM + BN) * BK * 2;
 };
-// One operand: `rows` rows (of m or n, or of k), `cols` elements each that may be read, a multiple of 8 and aligned to 16 bytes.
+// One operand: `rows` rows (of m or n, or of k), `cols` elements each that may be read, a multiple of 8 and aligned to 16 bytes; stride < 2^23.
 struct Operand {
     const uint16_t *p;
     int64_t stride;
     int64_t rows, cols;
 };
 
-// 16 bytes a lane to LDS, one lane's behind another's.  By hand because the compiler holds every transposing read back until all loads on their way to
-// LDS have come; nothing is returned in registers, and who reads waits for vmcnt and a barrier.
-__device__ __forceinline__ void load_to_lds(const uint16_t *g, char *lds)
+// 16 bytes a lane from base + offset to LDS, one lane's behind another's.  By hand because the compiler holds every transposing read back until all loads on
+// their way to LDS have come; nothing is returned in registers, and who reads waits for vmcnt and a barrier.
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t offset, char *lds)
 {
     const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(g) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
 
-// ALONG: LDS has W rows of 64 bytes, whose four 16-byte chunks are exchanged by the row's bits 2 and 3, so that 16 lanes that read a chunk
-// of 16 rows find each bank once.  Else 32 rows (k) of 2 W bytes, whose 32-byte slots are exchanged by the row's lowest two bits for the
-// same reason.  Positions beyond the operand's rows or columns read its last ones; what comes of those is not used (or meets zeros).
-template <int W, int WAVES, int FRAGS, bool ALONG> struct Side {
-    static constexpr int LOADS = W / 16 / WAVES;
-    const uint16_t *at[LOADS];
-    int64_t step_by;                      // elements from a step to the next
-    int64_t beyond[LOADS];                // elements that the last step's rows of k lie behind the operand's last one
-    uint32_t frag[ALONG ? 2 : FRAGS];     // ALONG: of the first block's two halves of BK; else of each block
+// ALONG: LDS has W rows of 128 bytes, whose eight 16-byte chunks are exchanged by the row's bits 1 to 3, so that 16 lanes that read a chunk
+// of 16 rows find each bank once.  Else BK rows (k) of 2 W bytes, whose 32-byte slots are exchanged by the row's bits 0, 1 and 3 for the
+// same reason.  Positions beyond the operand's rows or columns read its last ones; what comes of those is not used, or meets zeros.  Rows of k may end
+// within the last step if ENDS is set.
+template <int W, int WAVES, int FRAGS, bool ALONG, bool ENDS> struct Side {
+    static constexpr int LOADS = W / 8 / WAVES;
+    static_assert(LOADS >= 1 && W * BK * 2 == LOADS * WAVES * 1024, "whole loads of each wave");
+    static_assert((FRAGS & (FRAGS - 1)) == 0 && W >= 128, "blocks are told apart by bits of an address");
+    const char *base;                     // of the tile
+    int64_t step_by;                      // bytes from a step to the next
+    uint32_t at[LOADS], beyond[LOADS];    // bytes from the base; of them, what the last step's rows of k lie behind the operand's last one
+    uint32_t frag;                        // of the wave's first block in a stage
     int place;                            // in the stage of this wave's first load
 
+    static __device__ __forceinline__ int slot(int row) { return 2 * (row & 3) | ((row >> 3) & 1); }
     __device__ __forceinline__ void start(const Operand &X, int64_t first, int64_t k0, int steps, int wave, int lane, int sub)
     {
         place = wave * LOADS * 1024;
-        step_by = ALONG ? BK : BK * X.stride;
-        const int64_t last = X.rows - 1;
+        step_by = 2 * (ALONG ? BK : BK * X.stride);
+        base = reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(X.p + (ALONG ? first * X.stride + k0 : k0 * X.stride + first))));
+        const uint32_t stride = (uint32_t)X.stride * 2;
 #pragma unroll
         for (int q = 0; q < LOADS; ++q) {
             const int i = wave * LOADS + q;
             if constexpr (ALONG) {
-                const int64_t r = first + i * 16 + (lane >> 2);
-                at[q] = X.p + (r < last ? r : last) * X.stride + k0 + ((lane & 3) ^ ((lane >> 4) & 3)) * 8;
+                const int row = i * 8 + (lane >> 3), most = (int)min(X.rows - 1 - first, (int64_t)W);
+                at[q] = (uint32_t)min(row, most) * stride + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
             } else {
                 constexpr int LANES = W / 8, PER = 64 / LANES;        // lanes a row, rows a load
-                const int row = i * PER + lane / LANES, p = lane % LANES;
-                const int64_t c = first + (((p >> 1) ^ (2 * (row & 3))) << 4) + (p & 1) * 8;
-                at[q] = X.p + (k0 + row) * X.stride + (c < X.cols - 8 ? c : X.cols - 8);
-                beyond[q] = max(k0 + (int64_t)(steps - 1) * BK + row - last, (int64_t)0) * X.stride;
+                const int row = i * PER + lane / LANES, p = lane % LANES, most = (int)min(X.cols - 8 - first, (int64_t)W);
+                at[q] = (uint32_t)row * stride + min((((p >> 1) ^ slot(row)) << 4) + (p & 1) * 8, most) * 2;
+                if constexpr (ENDS) beyond[q] = (uint32_t)max(row - (int)min(X.rows - 1 - k0 - (int64_t)(steps - 1) * BK, (int64_t)BK), 0) * stride;
             }
         }
         if constexpr (ALONG) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                frag[s] = (uint32_t)((sub * FRAGS * 32 + (lane & 31)) * 64 + (((2 * s + (lane >> 5)) ^ ((lane >> 2) & 3)) << 4));
+            frag = (uint32_t)((sub * FRAGS * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ ((lane >> 1) & 7)) << 4));
         } else {
-            const int kr = (lane & 15) >> 2;
-#pragma unroll
-            for (int f = 0; f < FRAGS; ++f)
-                frag[f] = (uint32_t)((8 * (lane >> 5) + kr) * (2 * W) + ((((sub * FRAGS + f) ^ kr) * 2 + ((lane >> 4) & 1)) << 5) + (lane & 3) * 8);
+            const int row = 8 * (lane >> 4) + ((lane & 15) >> 2);
+            frag = (uint32_t)(row * (2 * W) + (((sub * FRAGS) ^ slot(row)) << 5) + (lane & 3) * 8);
         }
     }
-    __device__ __forceinline__ void load(char *stage, int step, bool end) const
+    __device__ __forceinline__ void load(char *stage, int q, int step, bool end) const
     {
-#pragma unroll
-        for (int q = 0; q < LOADS; ++q) {
-            const uint16_t *g = at[q] + step * step_by;
-            if constexpr (!ALONG) g -= end ? beyond[q] : 0;
-            load_to_lds(g, stage + place + q * 1024);
-        }
+        uint32_t offset = at[q];
+        if constexpr (ENDS) offset -= end ? beyond[q] : 0;
+        load_to_lds(base + step * step_by, offset, stage + place + q * 1024);
     }
-    // the FRAGS blocks' operands of half s of a stage
-    __device__ __forceinline__ void read(const char *stage, int s, bf16x8 (&out)[FRAGS]) const
+    // block f's operand of part s of a stage
+    __device__ __forceinline__ bf16x8 read(uint32_t stage, int s, int f) const
     {
-#pragma unroll
-        for (int f = 0; f < FRAGS; ++f) {
-            if constexpr (ALONG) {
-                out[f] = *reinterpret_cast<const bf16x8 *>(stage + frag[s] + f * 2048);
-            } else {
-                const char *p = stage + frag[f] + s * (16 * 2 * W);
-                union {
-                    i16x4 h[2];
-                    bf16x8 v;
-                } u;
-                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p);
-                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(p + 4 * 2 * W));
-                out[f] = u.v;
-            }
+        typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        if constexpr (ALONG) {
+            return *reinterpret_cast<lds_bf16x8 *>((uintptr_t)((stage + frag) ^ (s << 6)) + f * 2048);
+        } else {
+            const uint32_t p = ((stage + frag) ^ (f << 5)) + s * (PART * 2 * W);
+            union {
+                i16x4 h[2];
+                bf16x8 v;
+            } u;
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4 *>((uintptr_t)p));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4 *>((uintptr_t)(p + 4 * 2 * W)));
+            return u.v;
         }
     }
 };
 
-// vmcnt(n), and every LDS read of this wave is back
-template <int N> __device__ __forceinline__ void wait_loads()
-{
-    static_assert(N < 64, "");
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-}
+// every load of this wave has come, and every LDS read is back
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // acc = the tile's product over `steps` steps of BK from k0 on.  Every access lies in the operands, whatever `steps` is: loads ahead of the end
 // repeat the last step's.  At the end every wave has passed a barrier and no load is on its way, so the LDS can be used again.
-template <typename T, bool A_ALONG, bool B_ALONG>
+//
+// A step is two parts of 32 of k.  While a part is multiplied, the next one is read from LDS: the last part's reads are of the next stage, and before
+// them lies the step's one barrier, at which that stage has come and every wave has read all of its own, whose place the stage after
+// the next one then takes.
+template <typename T, bool A_ALONG, bool B_ALONG, bool B_ENDS>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int64_t m0, int64_t n0, int64_t k0, int steps, char *lds,
-                                        f32x16 (&acc)[T::MI][T::NI])
+                                        f32x4 (&acc)[T::MI][T::NI])
 {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    Side<T::BM, T::WAVES, T::MI, A_ALONG> a;
-    Side<T::BN, T::WAVES, T::NI, B_ALONG> b;
+    Side<T::BM, T::WAVES, T::MI, A_ALONG, false> a;
+    Side<T::BN, T::WAVES, T::NI, B_ALONG, B_ENDS> b;
     a.start(A, m0, k0, steps, wave, lane, wave / T::WN);
     b.start(B, n0, k0, steps, wave, lane, wave % T::WN);
-    constexpr int L = decltype(a)::LOADS + decltype(b)::LOADS;
+    constexpr int A_LOADS = decltype(a)::LOADS, L = A_LOADS + decltype(b)::LOADS, MN = T::MI * T::NI;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < T::NI; ++j) acc[i][j] = f32x16{};
+        for (int j = 0; j < T::NI; ++j) acc[i][j] = f32x4{};
     if (steps <= 0) return;
     const int end = steps - 1;
-    auto load = [&](int t) {
-        char *stage = lds + (t % STAGES) * T::STAGE;
+    auto load = [&](int t, int q) {
+        char *stage = lds + (t & 1) * T::STAGE;
         const int s = t < end ? t : end;
-        a.load(stage, s, s == end);
-        b.load(stage + T::BM * BK * 2, s, s == end);
+        if (q < A_LOADS) a.load(stage, q, s, s == end);
+        else b.load(stage + T::BM * BK * 2, q - A_LOADS, s, s == end);
     };
-    bf16x8 fa[2][T::MI], fb[2][T::NI];
-    auto read = [&](int t, int s) {
-        const char *stage = lds + (t % STAGES) * T::STAGE;
-        a.read(stage, s, fa[s]);
-        b.read(stage + T::BM * BK * 2, s, fb[s]);
-    };
-    auto multiply = [&](int s) {
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds);
+    bf16x8 fa[T::MI], fb[2][T::NI];
+    auto read_a = [&](int t, int s, int i) { fa[i] = a.read(lds0 + (t & 1) * T::STAGE, s, i); };
+    auto read_b = [&](int t, int s, int j) { fb[s & 1][j] = b.read(lds0 + (t & 1) * T::STAGE + T::BM * BK * 2, s, j); };
+    // A part's products, with a read or a load behind some, so that none of them keeps the matrix cores waiting: a row of blocks' operand is read again as
+    // soon as its last product has begun.  Loads begin behind the barrier and end half a step later.  The order is held as it stands here.
+    constexpr int BAR = T::NI;                              // products of the last part in front of the barrier
+    constexpr int EACH = MN * PARTS / 2 / L, FIRST = (MN - BAR) / EACH < L ? (MN - BAR) / EACH : L;      // products to a load; loads in the last part
+    static_assert(EACH >= 1 && BAR + T::NI <= MN, "a place for each load and read");
+    auto part = [&](int t, int s) {
+        const bool last = s == PARTS - 1;
+        const int tr = last ? t + 1 : t, sr = last ? 0 : s + 1;
 #pragma unroll
-        for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-            for (int j = 0; j < T::NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s][i], fb[s][j], acc[i][j], 0, 0, 0);
+        for (int p = 0; p < MN; ++p) {
+            if (last && p == BAR) {
+                wait_loads();
+                barrier();
+            }
+            const int i = p / T::NI, j = p % T::NI;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[s & 1][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j == 0 && i > 0) read_a(tr, sr, i - 1);
+            if (p == MN - 1) read_a(tr, sr, i);
+            if (p >= BAR && p - BAR < T::NI) read_b(tr, sr, p - BAR);
+            if (last) {
+                if (p >= BAR && (p - BAR) % EACH == 0 && (p - BAR) / EACH < FIRST) load(t + 2, (p - BAR) / EACH);
+            } else {
+                const int g = s * MN + p;
+                if (g % EACH == 0 && FIRST + g / EACH < L) load(t + 1, FIRST + g / EACH);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    load(0);
-    load(1);
-    load(2);
-    wait_loads<2 * L>();
+#pragma unroll
+    for (int q = 0; q < L; ++q) load(0, q);
+    wait_loads();
     barrier();
-    read(0, 0);
+#pragma unroll
+    for (int q = 0; q < FIRST; ++q) load(1, q);
+#pragma unroll
+    for (int f = 0; f < T::NI; ++f) read_b(0, 0, f);
+#pragma unroll
+    for (int f = 0; f < T::MI; ++f) read_a(0, 0, f);
     for (int t = 0; t < steps; ++t) {
-        wait_loads<L>();                  // stage t + 1 is there, and what this wave reads of stage t - 1 has been read
-        barrier();                        // the same of every wave
-        load(t + 3);
-        read(t, 1);
-        __builtin_amdgcn_sched_barrier(0);     // each half is read while the one before is multiplied
-        multiply(0);
-        __builtin_amdgcn_sched_barrier(0);
-        read(t + 1, 0);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1);
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) part(t, s);
     }
-    wait_loads<0>();
+    wait_loads();
     barrier();
 }
-// where element r of a wave's block lies: row of m (4 consecutive ones for r, r + 1, r + 2, r + 3), column of n
-__device__ __forceinline__ int row_of(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
-__device__ __forceinline__ int column_of(int lane) { return lane & 31; }
+// where element r of a wave's block lies: row of m, column of n
+__device__ __forceinline__ int row_of(int r, int lane) { return 4 * (lane >> 4) + r; }
+__device__ __forceinline__ int column_of(int lane) { return lane & 15; }
 
 // Tiles in groups of 8 along the first dimension, dealt so that each of the 8 dies has neighbours: its 32 CUs work on about 8 x 4 tiles at a
 // time, whose operands its L2 holds.  false: no tile.
 __device__ __forceinline__ bool my_tile(int64_t tiles1, int64_t tiles2, int64_t &t1, int64_t &t2)
 {
-    const int64_t all = tiles1 * tiles2, per = (all + 7) / 8, id = blockIdx.x, t = (id & 7) * per + (id >> 3);
+    // a launch has fewer than 2^32 work items, and so fewer than 2^24 tiles
+    const uint32_t second = (uint32_t)tiles2, all = (uint32_t)tiles1 * second, per = (all + 7) / 8, id = blockIdx.x, t = (id & 7) * per + (id >> 3);
     if ((id >> 3) >= per || t >= all) return false;
-    const int64_t group = t / (8 * tiles2), in = t - group * 8 * tiles2, width = tiles1 - group * 8 < 8 ? tiles1 - group * 8 : 8;
-    t1 = group * 8 + in % width;
-    t2 = in / width;
+    const uint32_t group = t / (8 * second), in = t - group * 8 * second, left = (uint32_t)tiles1 - group * 8, width = left < 8 ? left : 8;
+    t1 = __builtin_amdgcn_readfirstlane((int)(group * 8 + in % width));
+    t2 = __builtin_amdgcn_readfirstlane((int)(in / width));
     return true;
 }
 
@@ -286,27 +308,25 @@ struct Logit {
 };
 
 // Words of a lane's elements, counted from its wave's first one on; `before` are of the first element of a block.
-__device__ __forceinline__ int words_before(int lane) { return 4 * (lane >> 5); }
-__device__ __forceinline__ constexpr int word_of(int i, int r) { return i * 32 + 8 * (r >> 2) + (r & 3); }
+__device__ __forceinline__ int words_before(int lane) { return 4 * (lane >> 4); }
+__device__ __forceinline__ constexpr int word_of(int i, int r) { return i * 16 + r; }
 
 template <typename T>
-__device__ __forceinline__ void add_bias(const Logit &G, int64_t w0, int lane, f32x16 (&acc)[T::MI][T::NI])
+__device__ __forceinline__ void add_bias(const Logit &G, int64_t w0, int lane, f32x4 (&acc)[T::MI][T::NI])
 {
     if (!G.bias) return;
     const int64_t first = w0 + words_before(lane), last = G.vocab - 1;
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+    for (int i = 0; i < T::MI; ++i) {
+        float b[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float b[4];
+        for (int r = 0; r < 4; ++r) b[r] = __uint_as_float((uint32_t)G.bias[min(first + word_of(i, r), last)] << 16);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) b[e] = __uint_as_float((uint32_t)G.bias[min(first + word_of(i, 4 * q + e), last)] << 16);
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int j = 0; j < T::NI; ++j) acc[i][j][4 * q + e] += b[e];
-            asm volatile("" ::: "memory");        // not all of a wave's biases at once
-        }
+            for (int j = 0; j < T::NI; ++j) acc[i][j][r] += b[r];
+        asm volatile("" ::: "memory");        // not all of a wave's biases at once
+    }
 }
 // a lane's words that there are, and the place of a target among them (-1: not here)
 __device__ __forceinline__ int words_left(const Logit &G, int64_t w0, int lane)
@@ -328,16 +348,16 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_stats(Operand
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
-    f32x16 acc[T::MI][T::NI];
-    product<T, true, true>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
+    f32x4 acc[T::MI][T::NI];
+    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
-    const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 32;
+    const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 16;
     add_bias<T>(G, w0, lane, acc);
     const int left = words_left(G, w0, lane);
     float2 *joint = reinterpret_cast<float2 *>(lds);        // [WM][BN]
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) {
-        const int n = (wn * T::NI + j) * 32 + column_of(lane);
+        const int n = (wn * T::NI + j) * 16 + column_of(lane);
         const int64_t row = tr * T::BN + n;
         const int target = row < count ? place_of(G.targets[G.live.index[row]], w0, lane) : -1;
         float m = -INFINITY, z = 0.0f;
@@ -345,21 +365,23 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_stats(Operand
 #pragma unroll
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
+            for (int r = 0; r < 4; ++r) {
                 if (word_of(i, r) >= left) acc[i][j][r] = -INFINITY;
                 if (word_of(i, r) == target) z = acc[i][j][r], here = true;
                 m = fmaxf(m, acc[i][j][r]);
             }
         if (here) G.target_logit[row] = z;
+        m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float base = m == -INFINITY ? 0.0f : m;       // of nothing but -inf: a sum of 0
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(G.k * (acc[i][j][r] - base));
+            for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(G.k * (acc[i][j][r] - base));
+        s += __shfl_xor(s, 16);
         s += __shfl_xor(s, 32);
-        if (lane < 32) joint[wm * T::BN + n] = float2{m, s};
+        if (lane < 16) joint[wm * T::BN + n] = float2{m, s};
     }
     __syncthreads();
     for (int n = threadIdx.x; n < T::BN; n += T::BLOCK) {
@@ -380,33 +402,31 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dz(Operand W,
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
-    f32x16 acc[T::MI][T::NI];
-    product<T, true, true>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
+    f32x4 acc[T::MI][T::NI];
+    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
-    const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 32;
+    const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 16;
     add_bias<T>(G, w0, lane, acc);
     const int left = words_left(G, w0, lane);
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) {
-        const int64_t row = tr * T::BN + (wn * T::NI + j) * 32 + column_of(lane);
+        const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
         const bool live = row < count;
         const int target = live ? place_of(G.targets[G.live.index[row]], w0, lane) : -1;
         const int words = live ? left : 0;
         const float4 R = live ? G.row[row] : float4{};
         uint16_t *out = G.dz + row * G.dz_stride + (w0 - G.word0) + words_before(lane);
 #pragma unroll
-        for (int i = 0; i < T::MI; ++i)
+        for (int i = 0; i < T::MI; ++i) {
+            float d[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float d[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int w = word_of(i, 4 * q + e);
-                    const float p = __builtin_amdgcn_exp2f(G.k * (acc[i][j][4 * q + e] - R.x)) * R.y;
-                    d[e] = w < words ? R.z * ((w == target ? 1.0f : 0.0f) - p) : 0.0f;
-                }
-                *reinterpret_cast<u32x2 *>(out + word_of(i, 4 * q)) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
+            for (int r = 0; r < 4; ++r) {
+                const int w = word_of(i, r);
+                const float p = __builtin_amdgcn_exp2f(G.k * (acc[i][j][r] - R.x)) * R.y;
+                d[r] = w < words ? R.z * ((w == target ? 1.0f : 0.0f) - p) : 0.0f;
             }
+            *reinterpret_cast<u32x2 *>(out + word_of(i, 0)) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
+        }
     }
 }
 
@@ -426,18 +446,18 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dx(Operand DZ
     if (!my_tile(G.rows / T::BM, (G.hidden + T::BN - 1) / T::BN, tr, th)) return;
     if (tr * T::BM >= *G.live.count) return;
     const int per = (G.steps + G.splits - 1) / G.splits, from = blockIdx.y * per, mine = G.steps - from < per ? G.steps - from : per;
-    f32x16 acc[T::MI][T::NI];
-    product<T, true, false>(DZ, W, tr * T::BM, th * T::BN, (int64_t)from * BK, mine, lds, acc);
+    f32x4 acc[T::MI][T::NI];
+    product<T, true, false, true>(DZ, W, tr * T::BM, th * T::BN, (int64_t)from * BK, mine, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t row = tr * T::BM + (wm * T::MI + i) * 32 + row_of(r, lane);
+        for (int r = 0; r < 4; ++r) {
+            const int64_t row = tr * T::BM + (wm * T::MI + i) * 16 + row_of(r, lane);
             float *out = G.sum + ((int64_t)blockIdx.y * G.rows + row) * G.hidden;
 #pragma unroll
             for (int j = 0; j < T::NI; ++j) {
-                const int64_t h = th * T::BN + (wn * T::NI + j) * 32 + column_of(lane);
+                const int64_t h = th * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
                 if (h < G.hidden) out[h] = G.first ? acc[i][j][r] : out[h] + acc[i][j][r];
             }
         }
@@ -457,21 +477,21 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dw(Operand DZ
     __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
     int64_t tw, th;
     if (!my_tile((G.words + T::BM - 1) / T::BM, (G.hidden + T::BN - 1) / T::BN, tw, th)) return;
-    f32x16 acc[T::MI][T::NI];
+    f32x4 acc[T::MI][T::NI];
     const int count = *G.live.count;
-    product<T, false, false>(DZ, X, tw * T::BM, th * T::BN, 0, (count + BK - 1) / BK, lds, acc);
+    product<T, false, false, false>(DZ, X, tw * T::BM, th * T::BN, 0, (count + BK - 1) / BK, lds, acc);
     const float unit = count ? G.row[0].w : 1.0f;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t w = tw * T::BM + (wm * T::MI + i) * 32 + row_of(r, lane);
+        for (int r = 0; r < 4; ++r) {
+            const int64_t w = tw * T::BM + (wm * T::MI + i) * 16 + row_of(r, lane);
             if (w >= G.words) continue;
             uint16_t *out = G.dw + (G.word0 + w) * G.stride;
 #pragma unroll
             for (int j = 0; j < T::NI; ++j) {
-                const int64_t h = th * T::BN + (wn * T::NI + j) * 32 + column_of(lane);
+                const int64_t h = th * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
                 if (h < G.hidden) out[h] = (uint16_t)f32_to_bf16_bits(acc[i][j][r] * unit);
             }
         }
@@ -677,7 +697,7 @@ static Call call_of(const gs_head &h, const int64_t *targets, float temperature,
     C.it = 1.0f / temperature;
     C.live = {C.index() + 64, C.index()};
     C.stream = static_cast<hipStream_t>(stream);
-    C.packed = h.hidden % 64 != 0 || !multiple16(h.w, C.h.w_stride);
+    C.packed = h.hidden % 64 != 0 || !multiple16(h.w, C.h.w_stride) || C.h.w_stride >= 1 << 23;
     return C;
 }
 
