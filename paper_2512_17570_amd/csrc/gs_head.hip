@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "gs_device.h"
 #include "gs_internal.h"
@@ -73,7 +74,7 @@ __device__ __forceinline__ void load_to_lds(const char *base, uint32_t offset, c
 template <int W, int WAVES, int FRAGS, bool ALONG, bool ENDS> struct Side {
     static constexpr int LOADS = W / 8 / WAVES;
     static_assert(LOADS >= 1 && W * BK * 2 == LOADS * WAVES * 1024, "whole loads of each wave");
-    static_assert((FRAGS & (FRAGS - 1)) == 0 && W >= 128, "blocks are told apart by bits of an address");
+    static_assert((FRAGS & (FRAGS - 1)) == 0 && (ALONG || W >= 128), "blocks are told apart by bits of an address");
     const char *base;                     // of the tile
     int64_t step_by;                      // bytes from a step to the next
     uint32_t at[LOADS], beyond[LOADS];    // bytes from the base; of them, what the last step's rows of k lie behind the operand's last one
@@ -143,13 +144,13 @@ __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory
 // A step is two parts of 32 of k.  While a part is multiplied, the next one is read from LDS: the last part's reads are of the next stage, and before
 // them lies the step's one barrier, at which that stage has come and every wave has read all of its own, whose place the stage after
 // the next one then takes.
-template <typename T, bool A_ALONG, bool B_ALONG, bool B_ENDS>
+template <typename T, bool A_ALONG, bool B_ALONG, bool A_ENDS>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int64_t m0, int64_t n0, int64_t k0, int steps, char *lds,
                                         f32x4 (&acc)[T::MI][T::NI])
 {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    Side<T::BM, T::WAVES, T::MI, A_ALONG, false> a;
-    Side<T::BN, T::WAVES, T::NI, B_ALONG, B_ENDS> b;
+    Side<T::BM, T::WAVES, T::MI, A_ALONG, A_ENDS> a;
+    Side<T::BN, T::WAVES, T::NI, B_ALONG, false> b;
     a.start(A, m0, k0, steps, wave, lane, wave / T::WN);
     b.start(B, n0, k0, steps, wave, lane, wave % T::WN);
     constexpr int A_LOADS = decltype(a)::LOADS, L = A_LOADS + decltype(b)::LOADS, MN = T::MI * T::NI;
@@ -232,14 +233,52 @@ __device__ __forceinline__ bool my_tile(int64_t tiles1, int64_t tiles2, int64_t 
     return true;
 }
 
+// A wave's blocks as rows of bf16: `value(i, j, r)` of element (m, n) goes to out[n * stride + m] for n < rows, m < cols, counted from the wave's first.
+// A lane has four neighbours of m; through LDS (a place of its wave alone) they become rows of whole lines, 16 bytes a lane.  Any alignment of two.
+typedef u32x4 loose_u32x4 __attribute__((aligned(2)));
+template <typename T, typename F>
+__device__ __forceinline__ void store_rows(char *lds, int wave, int lane, F value, uint16_t *out, int64_t stride, int rows, int cols)
+{
+    constexpr int WIDTH = T::MI * 32, PITCH = WIDTH + 16, PASS = T::NI < 2 ? 1 : 2, CHUNKS = WIDTH / 16, AT_ONCE = 64 / CHUNKS;      // bytes of a row; blocks of n a time
+    static_assert(T::WAVES * PASS * 16 * PITCH <= STAGES * T::STAGE && T::NI % PASS == 0 && AT_ONCE * CHUNKS == 64, "");
+    char *mine = lds + wave * (PASS * 16 * PITCH);
+#pragma unroll
+    for (int j0 = 0; j0 < T::NI; j0 += PASS) {
+#pragma unroll
+        for (int j = 0; j < PASS; ++j)
+#pragma unroll
+            for (int i = 0; i < T::MI; ++i)
+                *reinterpret_cast<u32x2 *>(mine + (j * 16 + column_of(lane)) * PITCH + (i * 16 + row_of(0, lane)) * 2) =
+                    u32x2{two_bf16(value(i, j0 + j, 0), value(i, j0 + j, 1)), two_bf16(value(i, j0 + j, 2), value(i, j0 + j, 3))};
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < PASS * 16; q += AT_ONCE) {        // a wave's own accesses to LDS stay in order
+            const int n = q + lane / CHUNKS, m = lane % CHUNKS * 8, row = j0 * 16 + n;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + n * PITCH + m * 2);
+            if (row >= rows || m >= cols) continue;
+            uint16_t *to = out + row * stride + m;
+            if (m + 8 <= cols) {
+                *reinterpret_cast<loose_u32x4 *>(to) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (m + e < cols) to[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+        asm volatile("" ::: "memory");
+    }
+}
+
 // ---- the kernels -------------------------------------------------------------------------------
 // Rows that count, one after another: the rows with a token (and a factor other than 0).
 struct Live {
-    int32_t *index;        // the batch's row that is the j-th to count
     int32_t *count;
+    int32_t *index;        // the batch's row that is the j-th to count
+    int32_t *place;        // of a row of the batch among those; -1: it does not count
 };
 constexpr int LIVE_BLOCK = 1024;
-__global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets, const float *factor, int rows, int vocab, Live L)
+// Rows that do not count get logp 0 and statistics (0, 1) here, where there are any to write.
+__global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets, const float *factor, int rows, int vocab, Live L, float *logp, float *row_stats)
 {
     __shared__ int waves[LIVE_BLOCK / 64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -250,6 +289,8 @@ __global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets
         if (r < rows) {
             const int64_t t = targets[r];
             live = t >= 0 && t < vocab && (!factor || factor[r] != 0.0f);
+            if (!live && logp) logp[r] = 0.0f;
+            if (!live && row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
         }
         const uint64_t mask = __ballot(live);
         if (lane == 0) waves[wave] = __popcll(mask);
@@ -259,7 +300,9 @@ __global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets
             if (w < wave) at += waves[w];
             sum += waves[w];
         }
-        if (live) L.index[at + __popcll(mask & ((1ull << lane) - 1))] = r;
+        at += __popcll(mask & ((1ull << lane) - 1));
+        if (live) L.index[at] = r;
+        if (r < rows) L.place[r] = live ? at : -1;
         before += sum;
         __syncthreads();
     }
@@ -302,13 +345,14 @@ struct Logit {
     float it;                 // 1 / temperature
     float2 *partials;         // [tile of words][rows]: maximum, sum
     float *target_logit;      // [rows]
+    float *z;                 // null, or [rows][z_stride], this piece's: z is kept, in 32 bits
     const float4 *row;        // [rows]: M, 1 / S, the gradient's factor over `unit`, unit
-    uint16_t *dz;             // [rows][dz_stride]
-    int64_t dz_stride;
+    uint16_t *dz;             // [rows][stride]
+    int64_t stride, z_stride;
 };
 
 // Words of a lane's elements, counted from its wave's first one on; `before` are of the first element of a block.
-__device__ __forceinline__ int words_before(int lane) { return 4 * (lane >> 4); }
+__device__ __forceinline__ int words_before(int lane) { return row_of(0, lane); }
 __device__ __forceinline__ constexpr int word_of(int i, int r) { return i * 16 + r; }
 
 template <typename T>
@@ -338,10 +382,22 @@ __device__ __forceinline__ int place_of(int64_t target, int64_t w0, int lane)
     const int64_t p = target - w0 - words_before(lane);
     return p >= 0 && p < 4096 ? (int)p : -1;
 }
+// of the four lanes that have a column's elements
+__device__ __forceinline__ float column_max(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float column_sum(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
+// what exponentials are taken from: of nothing but -inf they sum to 0
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+// (m, s) joined with another maximum and sum
+__device__ __forceinline__ void join(float k, float &m, float &s, float2 q)
+{
+    const float top = fmaxf(m, q.x), base = base_of(top);
+    s = s * __builtin_amdgcn_exp2f(k * (m - base)) + q.y * __builtin_amdgcn_exp2f(k * (q.x - base));
+    m = top;
+}
 
 // Maximum and sum of exponentials of each row of the batch over a tile of words.
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_stats(Operand W, Operand X, int steps, Logit G)
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X, int steps, Logit G)
 {
     __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
     int64_t tw, tr;
@@ -362,6 +418,11 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_stats(Operand
         const int target = row < count ? place_of(G.targets[G.live.index[row]], w0, lane) : -1;
         float m = -INFINITY, z = 0.0f;
         bool here = false;
+        if (G.z) {
+            float *out = G.z + row * G.z_stride + (w0 - G.word0) + words_before(lane);
+#pragma unroll
+            for (int i = 0; i < T::MI; ++i) *reinterpret_cast<f32x4 *>(out + word_of(i, 0)) = acc[i][j];
+        }
 #pragma unroll
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
@@ -371,31 +432,32 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_stats(Operand
                 m = fmaxf(m, acc[i][j][r]);
             }
         if (here) G.target_logit[row] = z;
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float base = m == -INFINITY ? 0.0f : m;       // of nothing but -inf: a sum of 0
+        m = column_max(m);
+        const float base = base_of(m);
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(G.k * (acc[i][j][r] - base));
-        s += __shfl_xor(s, 16);
-        s += __shfl_xor(s, 32);
+        s = column_sum(s);
         if (lane < 16) joint[wm * T::BN + n] = float2{m, s};
     }
     __syncthreads();
     for (int n = threadIdx.x; n < T::BN; n += T::BLOCK) {
-        float m = -INFINITY, s = 0.0f;
-        for (int q = 0; q < T::WM; ++q) m = fmaxf(m, joint[q * T::BN + n].x);
-        const float base = m == -INFINITY ? 0.0f : m;
-        for (int q = 0; q < T::WM; ++q) s += joint[q * T::BN + n].y * __builtin_amdgcn_exp2f(G.k * (joint[q * T::BN + n].x - base));
+        float m = joint[n].x, s = joint[n].y;
+        for (int q = 1; q < T::WM; ++q) join(G.k, m, s, joint[q * T::BN + n]);
         G.partials[(G.word0 / T::BM + tw) * G.rows + tr * T::BN + n] = float2{m, s};
     }
 }
 
-// dz of a tile of words, rounded to bf16; zeros in rows from count on and for words behind the vocabulary, which products that follow may meet
+// dz of an element
+__device__ __forceinline__ float dz_of(const Logit &G, const float4 &R, float z, bool target)
+{
+    return R.z * ((target ? 1.0f : 0.0f) - __builtin_amdgcn_exp2f(G.k * (z - R.x)) * R.y);
+}
+// dz of a tile of words, rounded to bf16; zeros in rows from count on and for words behind the vocabulary, which products that follow meet
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dz(Operand W, Operand X, int steps, Logit G)
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, int steps, Logit G)
 {
     __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
     int64_t tw, tr;
@@ -412,22 +474,32 @@ __global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dz(Operand W,
     for (int j = 0; j < T::NI; ++j) {
         const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
         const bool live = row < count;
-        const int target = live ? place_of(G.targets[G.live.index[row]], w0, lane) : -1;
-        const int words = live ? left : 0;
+        const int target = live ? place_of(G.targets[G.live.index[row]], w0, lane) : -1, words = live ? left : 0;
         const float4 R = live ? G.row[row] : float4{};
-        uint16_t *out = G.dz + row * G.dz_stride + (w0 - G.word0) + words_before(lane);
 #pragma unroll
-        for (int i = 0; i < T::MI; ++i) {
-            float d[4];
+        for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int w = word_of(i, r);
-                const float p = __builtin_amdgcn_exp2f(G.k * (acc[i][j][r] - R.x)) * R.y;
-                d[r] = w < words ? R.z * ((w == target ? 1.0f : 0.0f) - p) : 0.0f;
-            }
-            *reinterpret_cast<u32x2 *>(out + word_of(i, 0)) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
-        }
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = word_of(i, r) < words ? dz_of(G, R, acc[i][j][r], word_of(i, r) == target) : 0.0f;
     }
+    uint16_t *out = G.dz + (tr * T::BN + wn * T::NI * 16) * G.stride + (w0 - G.word0);
+    store_rows<T>(lds, wave, lane, [&](int i, int j, int r) { return acc[i][j][r]; }, out, G.stride, T::NI * 16, T::MI * 16);
+}
+// the same from z that was kept: a lane four words
+__global__ __launch_bounds__(256) void k_head_dz_kept(Logit G)
+{
+    const int64_t row = blockIdx.x, w = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
+    const int count = *G.live.count;
+    if (row >= (count + 255) / 256 * 256 || w >= (G.words + 255) / 256 * 256) return;
+    float d[4] = {};
+    if (row < count) {
+        const float4 R = G.row[row];
+        const f32x4 z = *reinterpret_cast<const f32x4 *>(G.z + row * G.z_stride + w);
+        const int64_t target = G.targets[G.live.index[row]] - G.word0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (w + i < G.words) d[i] = dz_of(G, R, z[i], w + i == target);
+    }
+    *reinterpret_cast<u32x2 *>(G.dz + row * G.stride + w) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
 }
 
 // sum[split][row][h] (+)= dz W over a piece of the vocabulary
@@ -439,28 +511,29 @@ struct ToRows {
     int splits, steps;        // steps: of the piece
 };
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dx(Operand DZ, Operand W, ToRows G)
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, ToRows G)
 {
     __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
     int64_t tr, th;
-    if (!my_tile(G.rows / T::BM, (G.hidden + T::BN - 1) / T::BN, tr, th)) return;
-    if (tr * T::BM >= *G.live.count) return;
+    if (!my_tile(G.rows / T::BN, (G.hidden + T::BM - 1) / T::BM, tr, th)) return;
+    if (tr * T::BN >= *G.live.count) return;
     const int per = (G.steps + G.splits - 1) / G.splits, from = blockIdx.y * per, mine = G.steps - from < per ? G.steps - from : per;
     f32x4 acc[T::MI][T::NI];
-    product<T, true, false, true>(DZ, W, tr * T::BM, th * T::BN, (int64_t)from * BK, mine, lds, acc);
+    product<T, false, true, true>(W, DZ, th * T::BM, tr * T::BN, (int64_t)from * BK, mine, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
+    const int64_t h0 = th * T::BM + wm * T::MI * 16 + row_of(0, lane);
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+    for (int j = 0; j < T::NI; ++j) {
+        const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
+        float *out = G.sum + ((int64_t)blockIdx.y * G.rows + row) * G.hidden;          // hidden: of the sums' rows, a multiple of 4
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t row = tr * T::BM + (wm * T::MI + i) * 16 + row_of(r, lane);
-            float *out = G.sum + ((int64_t)blockIdx.y * G.rows + row) * G.hidden;
-#pragma unroll
-            for (int j = 0; j < T::NI; ++j) {
-                const int64_t h = th * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
-                if (h < G.hidden) out[h] = G.first ? acc[i][j][r] : out[h] + acc[i][j][r];
-            }
+        for (int i = 0; i < T::MI; ++i) {
+            const int64_t h = h0 + i * 16;
+            if (h >= G.hidden) continue;
+            f32x4 *to = reinterpret_cast<f32x4 *>(out + h);
+            *to = G.first ? acc[i][j] : *to + acc[i][j];
         }
+    }
 }
 
 // dW[word][h] = dz^T x of a piece of the vocabulary
@@ -472,29 +545,19 @@ struct ToWeights {
     const float4 *row;
 };
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, T::BLOCK / 256) void k_head_dw(Operand DZ, Operand X, ToWeights G)
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, ToWeights G)
 {
     __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
     int64_t tw, th;
-    if (!my_tile((G.words + T::BM - 1) / T::BM, (G.hidden + T::BN - 1) / T::BN, tw, th)) return;
+    if (!my_tile((G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
     f32x4 acc[T::MI][T::NI];
     const int count = *G.live.count;
-    product<T, false, false, false>(DZ, X, tw * T::BM, th * T::BN, 0, (count + BK - 1) / BK, lds, acc);
+    product<T, false, false, false>(X, DZ, th * T::BM, tw * T::BN, 0, (count + BK - 1) / BK, lds, acc);
     const float unit = count ? G.row[0].w : 1.0f;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
-#pragma unroll
-    for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t w = tw * T::BM + (wm * T::MI + i) * 16 + row_of(r, lane);
-            if (w >= G.words) continue;
-            uint16_t *out = G.dw + (G.word0 + w) * G.stride;
-#pragma unroll
-            for (int j = 0; j < T::NI; ++j) {
-                const int64_t h = th * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
-                if (h < G.hidden) out[h] = (uint16_t)f32_to_bf16_bits(acc[i][j][r] * unit);
-            }
-        }
+    const int64_t w0 = tw * T::BN + wn * T::NI * 16, h0 = th * T::BM + wm * T::MI * 16;
+    store_rows<T>(lds, wave, lane, [&](int i, int j, int r) { return acc[i][j][r] * unit; }, G.dw + (G.word0 + w0) * G.stride + h0, G.stride,
+                  (int)min(G.words - w0, (int64_t)4096), (int)min(G.hidden - h0, (int64_t)4096));
 }
 
 // db[word] = sum over rows of dz: a lane two words, a wave a share of the rows
@@ -505,6 +568,7 @@ __global__ __launch_bounds__(1024) void k_head_db(const uint16_t *dz, int64_t dz
     const int64_t w = (int64_t)blockIdx.x * 128 + lane * 2;           // a piece's rows have whole tiles of words
     const int count = *live.count;
     float a = 0.0f, b = 0.0f;
+#pragma unroll 8
     for (int r = wave; r < count; r += 16) {
         const uint32_t q = *reinterpret_cast<const uint32_t *>(dz + (int64_t)r * dz_stride + w);
         a += bf16_lo(q);
@@ -530,39 +594,49 @@ __device__ __forceinline__ float unit_of(float factor)
     const uint32_t u = __float_as_uint(factor) & 0x7fffffffu;
     return u >= 0x00800000u && u < 0x7f800000u ? __uint_as_float((u & 0x007fffffu) | 0x3f800000u) : 1.0f;
 }
-// Rows' maxima and sums, joined over the tiles of words: 32 rows a workgroup, 8 lanes a row.
+// Rows' maxima and sums, joined over the tiles of words: R rows a workgroup, 256 / R lanes a row.
 struct Join {
     const float2 *partials;
     const float *target_logit;
-    int64_t tiles, rows;       // rows: of the packed batch
+    int64_t tiles, rows;       // rows: of the packed batch, or of the batch without a list of those that count
     float k, it;
     float *logp, *row_stats;   // of the batch
     const float *weights;      // of the rows, or null for ones: factors of a loss's gradient are -weights / temperature
     float4 *row;               // null: no gradient follows
     Live live;
+    const int64_t *targets;    // without such a list
+    int vocab;
 };
+template <int R>
 __global__ __launch_bounds__(256) void k_head_join(Join J)
 {
-    __shared__ float2 part[8][32];
-    const int n = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + n;
-    const int count = *J.live.count;
-    if ((int64_t)blockIdx.x * 32 >= count) return;
+    constexpr int LANES = 256 / R;
+    __shared__ float2 part[LANES][R];
+    const int n = threadIdx.x % R, slice = threadIdx.x / R;
+    const int64_t j = (int64_t)blockIdx.x * R + n;
+    const int64_t count = J.live.count ? *J.live.count : J.rows;
+    if ((int64_t)blockIdx.x * R >= count) return;
     float m = -INFINITY, s = 0.0f;
-    for (int64_t t = slice; t < J.tiles; t += 8) {
-        const float2 q = J.partials[t * J.rows + j];
-        const float top = fmaxf(m, q.x), base = top == -INFINITY ? 0.0f : top;
-        s = s * __builtin_amdgcn_exp2f(J.k * (m - base)) + q.y * __builtin_amdgcn_exp2f(J.k * (q.x - base));
-        m = top;
-    }
+#pragma unroll 4
+    for (int64_t t = slice; t < J.tiles; t += LANES) join(J.k, m, s, J.partials[t * J.rows + j]);
     part[slice][n] = float2{m, s};
-    __syncthreads();
+#pragma unroll
+    for (int h = LANES / 2; h; h /= 2) {
+        __syncthreads();
+        if (slice < h) {
+            join(J.k, m, s, part[slice + h][n]);
+            part[slice][n] = float2{m, s};
+        }
+    }
     if (slice != 0 || j >= count) return;
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, part[i][n].x);
-    const float base = m == -INFINITY ? 0.0f : m;
-    s = 0.0f;
-    for (int i = 0; i < 8; ++i) s += part[i][n].y * __builtin_amdgcn_exp2f(J.k * (part[i][n].x - base));
-    const int64_t r = J.live.index[j];
+    int64_t r = j;
+    if (J.live.count) {
+        r = J.live.index[j];
+    } else if (const int64_t t = J.targets[j]; t < 0 || t >= J.vocab) {
+        J.logp[r] = 0.0f;
+        if (J.row_stats) J.row_stats[2 * r] = 0.0f, J.row_stats[2 * r + 1] = 1.0f;
+        return;
+    }
     J.logp[r] = J.it * (J.target_logit[j] - m) - logf(s);
     if (J.row_stats) J.row_stats[2 * r] = m, J.row_stats[2 * r + 1] = s;
     if (!J.row) return;
@@ -579,15 +653,6 @@ __global__ __launch_bounds__(256) void k_head_rows(Live live, const float *row_s
     row[j] = float4{row_stats[2 * r], 1.0f / row_stats[2 * r + 1], it * dlogp[r] / unit, unit};
 }
 
-// Rows that do not count: logp 0, statistics (0, 1).  (Before k_head_join, which writes the others.)
-__global__ __launch_bounds__(256) void k_head_none(int64_t rows, float *logp, float *row_stats)
-{
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (r >= rows) return;
-    logp[r] = 0.0f;
-    if (row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
-}
-
 // loss (+)= sum of weights times -logp over the rows that count
 __global__ __launch_bounds__(1024) void k_head_loss(Live live, const float *logp, const float *weights, float *loss, int accumulate)
 {
@@ -602,49 +667,146 @@ __global__ __launch_bounds__(1024) void k_head_loss(Live live, const float *logp
     if (threadIdx.x == 0) *loss = (float)(s + (accumulate ? (double)*loss : 0.0));
 }
 
-// dx of the rows that count from their sums, and zeros
-__global__ __launch_bounds__(256) void k_head_rows_out(Live live, const float *sum, int splits, int64_t rows, int64_t hidden, const float4 *row, uint16_t *dx, int64_t stride)
+// dx of the rows that count from their sums, zeros in the others: a lane four elements
+__global__ __launch_bounds__(256) void k_head_rows_out(Live live, const float *sum, int splits, int64_t rows, int64_t width, int64_t hidden, const float4 *row,
+                                                       uint16_t *dx, int64_t stride)
 {
-    const int64_t j = blockIdx.x;
-    if (j >= *live.count) return;
-    uint16_t *out = dx + (int64_t)live.index[j] * stride;
-    const float unit = row[j].w;
-    for (int64_t h = threadIdx.x; h < hidden; h += 256) {
-        float s = sum[j * hidden + h];
-        for (int i = 1; i < splits; ++i) s += sum[((int64_t)i * rows + j) * hidden + h];
-        out[h] = (uint16_t)f32_to_bf16_bits(s * unit);
+    const int64_t r = blockIdx.x, h = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
+    if (h >= hidden) return;
+    const int64_t j = live.place[r];
+    f32x4 s = {};
+    if (j >= 0) {
+        const float *from = sum + j * width + h;
+#pragma unroll 8
+        for (int i = 0; i < splits; ++i) s += *reinterpret_cast<const f32x4 *>(from + i * rows * width);
+        s *= row[j].w;
+    }
+    uint16_t *out = dx + r * stride + h;
+    const u32x2 q = {two_bf16(s[0], s[1]), two_bf16(s[2], s[3])};
+    if (h + 4 <= hidden) {
+        typedef u32x2 loose_u32x2 __attribute__((aligned(2)));
+        *reinterpret_cast<loose_u32x2 *>(out) = q;
+    } else {
+        for (int e = 0; e < 4; ++e)
+            if (h + e < hidden) out[e] = (uint16_t)(q[e >> 1] >> (16 * (e & 1)));
     }
 }
-__global__ __launch_bounds__(256) void k_head_zero(uint16_t *p, int64_t stride, int64_t cols)
+
+// ---- up to 16 rows, scored -----------------------------------------------------------------------
+// Every weight is read once and meets few rows: HBM is the bound, and the weights go from there to registers.  A workgroup takes FEW_WORDS words, its four waves take
+// turns along k, 128 at a time; the matrix cores' other columns are idle.  Rows of the batch that there are not repeat the last one.
+constexpr int FEW_ROWS = 16, FEW_WORDS = 32, FEW_WAVES = 4, FEW_K = 128;
+template <bool VEC>
+__device__ __forceinline__ bf16x8 load_k(const uint16_t *p, int64_t k, int64_t n)
 {
-    for (int64_t c = threadIdx.x; c < cols; c += 256) p[blockIdx.x * stride + c] = 0;
+    if (VEC && k + 8 <= n) return __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(p + k));
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = k + i < n ? p[k + i] : 0;
+    return __builtin_bit_cast(bf16x8, u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16});
+}
+struct Few {
+    const uint16_t *x, *w, *bias;
+    int64_t x_stride, w_stride, hidden, vocab;
+    int rows;
+    const int64_t *targets;
+    float k;
+    float2 *partials;          // [workgroup][rows]
+    float *target_logit;
+};
+template <bool VEC>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few(Few G)
+{
+    constexpr int MI = FEW_WORDS / 16, KI = FEW_K / 32;
+    __shared__ f32x4 part[FEW_WAVES - 1][MI][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15;
+    const int64_t w0 = (int64_t)blockIdx.x * FEW_WORDS, H = G.hidden;
+    const uint16_t *x = G.x + min(n, G.rows - 1) * G.x_stride, *w[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) w[i] = G.w + min(w0 + i * 16 + n, G.vocab - 1) * G.w_stride;
+    f32x4 acc[MI] = {};
+    auto some = [&](int64_t k0, auto whole) {
+        bf16x8 fw[MI][KI], fx[KI];
+#pragma unroll
+        for (int q = 0; q < KI; ++q) {
+            const int64_t k = k0 + q * 32 + (lane >> 4) * 8;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fw[i][q] = load_k<VEC>(w[i], k, whole ? k + 8 : H);
+            if (VEC && (whole || k + 8 <= H)) fx[q] = *reinterpret_cast<const bf16x8 *>(x + k);
+            else fx[q] = load_k<false>(x, k, H);
+        }
+#pragma unroll
+        for (int q = 0; q < KI; ++q)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[i][q], fx[q], acc[i], 0, 0, 0);
+    };
+    int64_t k0 = wave * FEW_K;
+    for (; VEC && k0 + FEW_K <= H; k0 += FEW_WAVES * FEW_K) some(k0, std::true_type{});
+    for (; k0 < H; k0 += FEW_WAVES * FEW_K) some(k0, std::false_type{});
+    if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) part[wave - 1][i][lane] = acc[i];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const int64_t left = G.vocab - w0 - row_of(0, lane), target = n < G.rows ? G.targets[n] - w0 - row_of(0, lane) : -1;
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int q = 0; q < FEW_WAVES - 1; ++q) acc[i] += part[q][i][lane];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (G.bias) acc[i][r] += __uint_as_float((uint32_t)G.bias[min(w0 + i * 16 + row_of(r, lane), G.vocab - 1)] << 16);
+            if (i * 16 + r >= left) acc[i][r] = -INFINITY;
+            if (i * 16 + r == target) G.target_logit[n] = acc[i][r];
+            m = fmaxf(m, acc[i][r]);
+        }
+    }
+    m = column_max(m);
+    const float base = base_of(m);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(G.k * (acc[i][r] - base));
+    s = column_sum(s);
+    if (lane < G.rows && lane < 16) G.partials[(int64_t)blockIdx.x * G.rows + lane] = float2{m, s};
 }
 
 // ---- the plan of a call ------------------------------------------------------------------------
-typedef Tile<256, 256, 2, 4> Big;
+typedef Tile<256, 256, 2, 4> Big;          // many rows
+typedef Tile<256, 64, 4, 1> Slim;          // up to 64 rows that count beside each other
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 256 << 20;          // of dz
+constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits
+constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
 
 struct Plan {
     int64_t rows;            // of the packed batch
-    int64_t width;           // of its rows, and of packed weights
+    int64_t width;           // of its rows, of packed weights and of sums to the rows
     int64_t piece;           // words
-    int64_t tiles;           // of words, 256 each
+    int64_t packed;          // words of a piece where weights have to be packed
+    int64_t tiles;           // of words
     int splits;              // of the sums to the rows
-    size_t index, x, partials, target, row, dz, sum, w, all;      // places in the workspace, and its size
+    bool slim, kept;
+    size_t index, x, partials, target, row, z, dz, sum, w, all;      // places in the workspace, and its size
 };
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
-// Packed weights are reckoned with in any case where they may be needed: alignment is not known when the size is asked for.
+// Packed weights are reckoned with in any case: their alignment is not known when the size is asked for.
 static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
 {
     Plan P = {};
-    P.rows = up(std::max<int64_t>(rows, 1), 256);
+    P.slim = rows <= Slim::BN;
+    const int64_t tile = P.slim ? Slim::BN : Big::BN;
+    P.rows = up(std::max<int64_t>(rows, 1), tile);
     P.width = up(hidden, 64);
     P.tiles = up(vocab, 256) / 256;
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * P.rows * 256));
-    P.piece = std::min(P.tiles, most) * 256;
-    const int64_t out = P.rows / 256 * (up(hidden, 256) / 256);                // tiles of the sums to the rows
+    P.kept = gradient && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
+    P.piece = (P.kept ? P.tiles : std::min(P.tiles, most)) * 256;
+    P.packed = std::min(P.piece, std::max<int64_t>(1, kPackedBytes / (2 * P.width * 256)) * 256);
+    const int64_t out = P.rows / tile * (up(hidden, 256) / 256);                // tiles of the sums to the rows
     P.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(P.piece / 1024, 32), 512 / out));
     size_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -652,14 +814,15 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
         at += (size_t)up(bytes, 256);
         return here;
     };
-    P.index = take(P.rows * 4 + 256);
+    P.index = take((2 * P.rows + 64) * 4);
     P.x = take(P.rows * P.width * 2);
-    P.partials = take(P.tiles * P.rows * 8);
+    P.partials = take(std::max(P.tiles * P.rows, rows <= FEW_ROWS ? up(vocab, FEW_WORDS) / FEW_WORDS * FEW_ROWS : 0) * 8);
     P.target = take(P.rows * 4);
     P.row = take(P.rows * 16);
+    P.z = P.kept ? take(P.rows * P.tiles * 256 * 4) : at;
     P.dz = gradient ? take(P.rows * P.piece * 2) : at;
-    P.sum = gradient ? take(P.splits * P.rows * hidden * 4) : at;
-    P.w = take(P.piece * P.width * 2);
+    P.sum = gradient ? take(P.splits * P.rows * P.width * 4) : at;
+    P.w = take(P.packed * P.width * 2);
     P.all = at;
     return P;
 }
@@ -673,7 +836,6 @@ struct Call {
     Live live;
     hipStream_t stream;
     bool packed;             // the weights cannot be read where they lie
-    int32_t *index() const { return reinterpret_cast<int32_t *>(ws + P.index); }
     uint16_t *x() const { return reinterpret_cast<uint16_t *>(ws + P.x); }
     uint16_t *w() const { return reinterpret_cast<uint16_t *>(ws + P.w); }
     uint16_t *dz() const { return reinterpret_cast<uint16_t *>(ws + P.dz); }
@@ -695,28 +857,24 @@ static Call call_of(const gs_head &h, const int64_t *targets, float temperature,
     C.ws = static_cast<char *>(ws);
     C.targets = targets;
     C.it = 1.0f / temperature;
-    C.live = {C.index() + 64, C.index()};
+    int32_t *index = reinterpret_cast<int32_t *>(C.ws + C.P.index);
+    C.live = {index, index + 64, index + 64 + C.P.rows};
     C.stream = static_cast<hipStream_t>(stream);
     C.packed = h.hidden % 64 != 0 || !multiple16(h.w, C.h.w_stride) || C.h.w_stride >= 1 << 23;
     return C;
 }
 
-// the rows that count, packed
-static hipError_t pack_rows(const Call &C, const float *factor)
+static hipError_t pack(const Call &C, const uint16_t *from, int64_t stride, const Live &live, int64_t there, int64_t rows, uint16_t *to)
 {
-    k_head_live<<<1, LIVE_BLOCK, 0, C.stream>>>(C.targets, factor, (int)C.h.rows, (int)C.h.vocab, C.live);
-    if (multiple16(C.h.x, C.h.x_stride)) k_head_pack<true><<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(C.h.x, C.h.x_stride, C.h.hidden, C.live, C.P.rows, C.x(), C.P.width);
-    else k_head_pack<false><<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(C.h.x, C.h.x_stride, C.h.hidden, C.live, C.P.rows, C.x(), C.P.width);
+    if (multiple16(from, stride)) k_head_pack<true><<<(uint32_t)rows, 256, 0, C.stream>>>(from, stride, C.h.hidden, live, there, to, C.P.width);
+    else k_head_pack<false><<<(uint32_t)rows, 256, 0, C.stream>>>(from, stride, C.h.hidden, live, there, to, C.P.width);
     return hipGetLastError();
 }
-// the weights of a piece of the vocabulary, from word0 on
-static Operand weights(const Call &C, int64_t word0, int64_t words)
+// the rows that count, packed
+static hipError_t pack_rows(const Call &C, const float *factor, float *logp, float *row_stats)
 {
-    if (!C.packed) return {C.h.w + word0 * C.h.w_stride, C.h.w_stride, words, C.h.hidden};
-    if (multiple16(C.h.w, C.h.w_stride))
-        k_head_pack<true><<<(uint32_t)words, 256, 0, C.stream>>>(C.h.w + word0 * C.h.w_stride, C.h.w_stride, C.h.hidden, Live{}, words, C.w(), C.P.width);
-    else k_head_pack<false><<<(uint32_t)words, 256, 0, C.stream>>>(C.h.w + word0 * C.h.w_stride, C.h.w_stride, C.h.hidden, Live{}, words, C.w(), C.P.width);
-    return {C.w(), C.P.width, words, C.P.width};
+    k_head_live<<<1, LIVE_BLOCK, 0, C.stream>>>(C.targets, factor, (int)C.h.rows, (int)C.h.vocab, C.live, logp, row_stats);
+    return pack(C, C.h.x, C.h.x_stride, C.live, C.P.rows, C.P.rows, C.x());
 }
 static Logit logit_of(const Call &C, int64_t word0, int64_t words)
 {
@@ -732,62 +890,90 @@ static Logit logit_of(const Call &C, int64_t word0, int64_t words)
     G.it = C.it;
     G.partials = C.partials();
     G.target_logit = C.target();
+    G.z = C.P.kept ? reinterpret_cast<float *>(C.ws + C.P.z) + word0 : nullptr;
+    G.z_stride = C.P.tiles * 256;
     G.row = C.row();
     G.dz = C.dz();
-    G.dz_stride = C.P.piece;
+    G.stride = C.P.piece;
     return G;
 }
 static uint32_t grid_of(int64_t tiles) { return (uint32_t)(up(tiles, 8)); }
 
+// each(first word, words, their weights) of every piece
 template <typename F> static hipError_t pieces(const Call &C, F each)
 {
-    for (int64_t w = 0; w < C.h.vocab; w += C.P.piece) {
-        const int64_t words = std::min(C.P.piece, C.h.vocab - w);
-        if (hipError_t e = each(w, words, weights(C, w, words)); e != hipSuccess) return e;
+    const int64_t piece = C.packed ? C.P.packed : C.P.piece;
+    for (int64_t w = 0; w < C.h.vocab; w += piece) {
+        const int64_t words = std::min(piece, C.h.vocab - w);
+        Operand W = {C.h.w + w * C.h.w_stride, C.h.w_stride, words, C.h.hidden};
+        if (C.packed) {
+            if (hipError_t e = pack(C, W.p, W.stride, Live{}, words, words, C.w()); e != hipSuccess) return e;
+            W = {C.w(), C.P.width, words, C.P.width};
+        }
+        if (hipError_t e = each(w, words, W); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <typename T>
 static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
 {
     const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
     hipError_t e = pieces(C, [&](int64_t w, int64_t words, const Operand &W) {
-        Logit G = logit_of(C, w, words);
-        k_head_stats<Big><<<grid_of(up(words, 256) / 256 * (C.P.rows / 256)), Big::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
+        k_head_stats<T><<<grid_of(up(words, T::BM) / T::BM * (C.P.rows / T::BN)), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), logit_of(C, w, words));
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    if (C.h.rows) k_head_none<<<(uint32_t)((C.h.rows + 255) / 256), 256, 0, C.stream>>>(C.h.rows, logp, row_stats);
-    const Join J = {C.partials(), C.target(), C.P.tiles, C.P.rows, kLog2e * C.it, C.it, logp, row_stats, row_weights, gradient ? C.row() : nullptr, C.live};
-    k_head_join<<<(uint32_t)(C.P.rows / 32), 256, 0, C.stream>>>(J);
+    const Join J = {C.partials(), C.target(), C.P.tiles, C.P.rows, kLog2e * C.it, C.it, logp, row_stats, row_weights, gradient ? C.row() : nullptr, C.live, nullptr, 0};
+    if (C.P.slim) k_head_join<1><<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(J);
+    else k_head_join<32><<<(uint32_t)(C.P.rows / 32), 256, 0, C.stream>>>(J);
+    return hipGetLastError();
+}
+static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
+{
+    return C.P.slim ? forward<Slim>(C, logp, row_stats, row_weights, gradient) : forward<Big>(C, logp, row_stats, row_weights, gradient);
+}
+static hipError_t forward_few(const Call &C, float *logp, float *row_stats)
+{
+    const gs_head &h = C.h;
+    const Few G = {h.x, h.w, h.bias, h.x_stride, h.w_stride, h.hidden, h.vocab, (int)h.rows, C.targets, kLog2e * C.it, C.partials(), C.target()};
+    const int64_t tiles = up(h.vocab, FEW_WORDS) / FEW_WORDS;
+    if (multiple16(h.x, h.x_stride) && multiple16(h.w, h.w_stride)) k_head_few<true><<<(uint32_t)tiles, FEW_WAVES * 64, 0, C.stream>>>(G);
+    else k_head_few<false><<<(uint32_t)tiles, FEW_WAVES * 64, 0, C.stream>>>(G);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const Join J = {C.partials(), C.target(), tiles, h.rows, kLog2e * C.it, C.it, logp, row_stats, nullptr, nullptr, Live{}, C.targets, (int)h.vocab};
+    k_head_join<1><<<(uint32_t)h.rows, 256, 0, C.stream>>>(J);
     return hipGetLastError();
 }
 
-static hipError_t backward(const Call &C, const gs_head_grads &D)
+template <typename T>
+static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
 {
     const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
-    const int64_t H = C.h.hidden, htiles = up(H, 256) / 256, rtiles = C.P.rows / 256;
+    const int64_t H = C.P.width, htiles = up(H, 256) / 256, rtiles = C.P.rows / T::BN;
     hipError_t e = pieces(C, [&](int64_t w, int64_t words, const Operand &W) {
-        Logit G = logit_of(C, w, words);
         const int64_t wtiles = up(words, 256) / 256;
-        k_head_dz<Big><<<grid_of(wtiles * rtiles), Big::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
+        const Logit G = logit_of(C, w, words);
+        if (have_z) k_head_dz_kept<<<dim3((uint32_t)C.P.rows, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G);
+        else k_head_dz<T><<<grid_of(wtiles * rtiles), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
         const Operand DZ = {C.dz(), C.P.piece, C.P.rows, C.P.piece};
         if (D.dx) {
             const ToRows R = {C.live, C.P.rows, H, C.sum(), w == 0, C.P.splits, (int)(up(words, BK) / BK)};
-            k_head_dx<Big><<<dim3(grid_of(rtiles * htiles), (uint32_t)C.P.splits), Big::BLOCK, 0, C.stream>>>(DZ, W, R);
+            k_head_dx<T><<<dim3(grid_of(rtiles * htiles), (uint32_t)C.P.splits), T::BLOCK, 0, C.stream>>>(W, DZ, R);
         }
         if (D.dw) {
-            const ToWeights R = {C.live, w, words, H, D.dw, D.dw_stride, C.row()};
-            k_head_dw<Big><<<grid_of(wtiles * htiles), Big::BLOCK, 0, C.stream>>>(DZ, X, R);
+            const ToWeights R = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : H, C.row()};
+            k_head_dw<Big><<<grid_of(wtiles * (up(C.h.hidden, 256) / 256)), Big::BLOCK, 0, C.stream>>>(X, DZ, R);
         }
         if (D.dbias) k_head_db<<<(uint32_t)((words + 127) / 128), 1024, 0, C.stream>>>(C.dz(), C.P.piece, C.live, words, C.row(), D.dbias + w);
         return hipGetLastError();
     });
     if (e != hipSuccess || !D.dx || !C.h.rows) return e;
-    k_head_zero<<<(uint32_t)C.h.rows, 256, 0, C.stream>>>(D.dx, D.dx_stride, H);
-    k_head_rows_out<<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(C.live, C.sum(), C.P.splits, C.P.rows, H, C.row(), D.dx, D.dx_stride);
+    k_head_rows_out<<<dim3((uint32_t)C.h.rows, (uint32_t)((C.h.hidden + 1023) / 1024)), 256, 0, C.stream>>>(C.live, C.sum(), C.P.splits, C.P.rows, H, C.h.hidden, C.row(),
+                                                                                                          D.dx, C.h.rows > 1 ? D.dx_stride : C.h.hidden);
     return hipGetLastError();
 }
+static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z) { return C.P.slim ? backward<Slim>(C, D, have_z) : backward<Big>(C, D, have_z); }
 
 // ---- checks -------------------------------------------------------------------------------------
 static bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -876,8 +1062,13 @@ gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temper
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
     const Call C = call_of(*head, targets, temperature, false, d_workspace, stream);
-    hipError_t e = pack_rows(C, nullptr);
-    if (e == hipSuccess) e = forward(C, logp, row_stats, nullptr, false);
+    hipError_t e;
+    if (rows <= FEW_ROWS) {
+        e = forward_few(C, logp, row_stats);
+    } else {
+        e = pack_rows(C, nullptr, logp, row_stats);
+        if (e == hipSuccess) e = forward(C, logp, row_stats, nullptr, false);
+    }
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_head_logp launch");
 }
 
@@ -897,12 +1088,12 @@ gs_status gs_head_logp_grad(const gs_head *head, const int64_t *targets, float t
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
     const Call C = call_of(*head, targets, temperature, true, d_workspace, stream);
-    hipError_t e = pack_rows(C, dlogp);
+    hipError_t e = pack_rows(C, dlogp, nullptr, nullptr);
     if (e == hipSuccess) {
-        k_head_rows<<<(uint32_t)(C.P.rows / 256), 256, 0, C.stream>>>(C.live, row_stats, dlogp, C.it, C.row());
+        k_head_rows<<<(uint32_t)((C.P.rows + 255) / 256), 256, 0, C.stream>>>(C.live, row_stats, dlogp, C.it, C.row());
         e = hipGetLastError();
     }
-    if (e == hipSuccess) e = backward(C, *grads);
+    if (e == hipSuccess) e = backward(C, *grads, false);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_head_logp_grad launch");
 }
 
@@ -925,13 +1116,13 @@ gs_status gs_head_cross_entropy(const gs_head *head, const int64_t *targets, con
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
     const Call C = call_of(*head, targets, temperature, grads != nullptr, d_workspace, stream);
-    hipError_t e = pack_rows(C, weights);
+    hipError_t e = pack_rows(C, weights, logp, nullptr);
     if (e == hipSuccess) e = forward(C, logp, nullptr, weights, grads != nullptr);
     if (e == hipSuccess) {
         k_head_loss<<<1, 1024, 0, C.stream>>>(C.live, logp, weights, d_loss, accumulate);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && grads) e = backward(C, *grads);
+    if (e == hipSuccess && grads) e = backward(C, *grads, C.P.kept);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_head_cross_entropy launch");
 }
 

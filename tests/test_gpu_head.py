@@ -158,9 +158,10 @@ def test_nan_and_infinity_in_a_row_stay_there():
     assert not bool(c.dx[rest].isnan().any())
 
 
-@pytest.mark.parametrize("rows, hidden, vocab, bias", [(8192, 64, 40_000, True), (20_000, 72, 9_000, False), (3, 64, 300_000, True)])
+@pytest.mark.parametrize("rows, hidden, vocab, bias", [(8192, 64, 40_000, True), (20_000, 72, 9_000, False), (3, 64, 300_000, True), (5, 8, 2_200_000, True),
+                                                       (20, 8200, 10_000, True), (300, 8200, 9_000, False)])
 def test_many_pieces_and_tiles(rows, hidden, vocab, bias):
-    """More words than a piece has, more rows than a group of tiles."""
+    """More words than a piece has, with z kept and made again, weights packed in pieces of their own, more rows than a group of tiles."""
     Case(rows, hidden, vocab, prompt=True, bias=bias).check_loss()
 
 
