@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 
 // ---- a tile of a product -----------------------------------------------------------------------
 // C[m][n] = sum_k A[m][k] B[n][k] over a tile of BM x BN, WM x WN waves of MI x NI blocks of 16 x 16 each.  The operands come to LDS
-// BK of k at a time by loads that go there without passing registers, one stage on its way while another is worked on.
+// BK of k at a time by loads that go there without passing registers, STAGES of them in turn, one worked on while the others are on their way.
 // An operand is either rows of k (ALONG: k is contiguous) or rows of m or n (k is the distance between rows); the second kind is read from
 // LDS by the transposing load.
 //
@@ -46,11 +46,11 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 // the time.  16 x 16 x 32 products draw least (alone, of random values, 2160 TFLOP/s; 32 x 32 x 16, whose sums go through the registers twice as
 // often, 1900); rows of 128 bytes are whole lines of the caches (64 bytes a row, four stages: 1190 TFLOP/s against 1300 for 8192 x 4096 x 16384, both steps
 // together).  Four waves of 128 x 128, which read a third less LDS: level, they wait where eight do not.
-constexpr int BK = 64, PART = 32, PARTS = BK / PART, STAGES = 2;
-template <int BM_, int BN_, int WM_, int WN_> struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, BLOCK = WAVES * 64;
+constexpr int BK = 64, PART = 32, PARTS = BK / PART;
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct Tile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, BLOCK = WAVES * 64, STAGES = STAGES_;
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
-    static constexpr int STAGE = (BM + BN) * BK * 2;
+    static constexpr int STAGE = (BM + BN) * BK * 2, LDS = STAGES * STAGE;
 };
 // One operand: `rows` rows (of m or n, or of k), `cols` elements each that may be read, a multiple of 8 and aligned to 16 bytes; stride < 2^23.
 struct Operand {
@@ -134,16 +134,20 @@ template <int W, int WAVES, int FRAGS, bool ALONG, bool ENDS> struct Side {
     }
 };
 
-// every load of this wave has come, and every LDS read is back
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// all loads of this wave but the last N have come, and every LDS read is back
+template <int N> __device__ __forceinline__ void wait_loads()
+{
+    static_assert(N < 64, "what the counter holds");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // acc = the tile's product over `steps` steps of BK from k0 on.  Every access lies in the operands, whatever `steps` is: loads ahead of the end
 // repeat the last step's.  At the end every wave has passed a barrier and no load is on its way, so the LDS can be used again.
 //
 // A step is two parts of 32 of k.  While a part is multiplied, the next one is read from LDS: the last part's reads are of the next stage, and before
-// them lies the step's one barrier, at which that stage has come and every wave has read all of its own, whose place the stage after
-// the next one then takes.
+// them lies the step's one barrier, at which that stage has come and every wave has read all of its own, whose place the stage STAGES steps
+// ahead then takes.
 template <typename T, bool A_ALONG, bool B_ALONG, bool A_ENDS>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int64_t m0, int64_t n0, int64_t k0, int steps, char *lds,
                                         f32x4 (&acc)[T::MI][T::NI])
@@ -161,15 +165,15 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
     if (steps <= 0) return;
     const int end = steps - 1;
     auto load = [&](int t, int q) {
-        char *stage = lds + (t & 1) * T::STAGE;
+        char *stage = lds + t % T::STAGES * T::STAGE;
         const int s = t < end ? t : end;
         if (q < A_LOADS) a.load(stage, q, s, s == end);
         else b.load(stage + T::BM * BK * 2, q - A_LOADS, s, s == end);
     };
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds);
     bf16x8 fa[T::MI], fb[2][T::NI];
-    auto read_a = [&](int t, int s, int i) { fa[i] = a.read(lds0 + (t & 1) * T::STAGE, s, i); };
-    auto read_b = [&](int t, int s, int j) { fb[s & 1][j] = b.read(lds0 + (t & 1) * T::STAGE + T::BM * BK * 2, s, j); };
+    auto read_a = [&](int t, int s, int i) { fa[i] = a.read(lds0 + t % T::STAGES * T::STAGE, s, i); };
+    auto read_b = [&](int t, int s, int j) { fb[s & 1][j] = b.read(lds0 + t % T::STAGES * T::STAGE + T::BM * BK * 2, s, j); };
     // A part's products, with a read or a load behind some, so that none of them keeps the matrix cores waiting: a row of blocks' operand is read again as
     // soon as its last product has begun.  Loads begin behind the barrier and end half a step later.  The order is held as it stands here.
     constexpr int BAR = T::NI;                              // products of the last part in front of the barrier
@@ -181,7 +185,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
 #pragma unroll
         for (int p = 0; p < MN; ++p) {
             if (last && p == BAR) {
-                wait_loads();
+                wait_loads<(T::STAGES - 2) * L>();
                 barrier();
             }
             const int i = p / T::NI, j = p % T::NI;
@@ -191,20 +195,22 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
             if (p == MN - 1) read_a(tr, sr, i);
             if (p >= BAR && p - BAR < T::NI) read_b(tr, sr, p - BAR);
             if (last) {
-                if (p >= BAR && (p - BAR) % EACH == 0 && (p - BAR) / EACH < FIRST) load(t + 2, (p - BAR) / EACH);
+                if (p >= BAR && (p - BAR) % EACH == 0 && (p - BAR) / EACH < FIRST) load(t + T::STAGES, (p - BAR) / EACH);
             } else {
                 const int g = s * MN + p;
-                if (g % EACH == 0 && FIRST + g / EACH < L) load(t + 1, FIRST + g / EACH);
+                if (g % EACH == 0 && FIRST + g / EACH < L) load(t + T::STAGES - 1, FIRST + g / EACH);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
 #pragma unroll
-    for (int q = 0; q < L; ++q) load(0, q);
-    wait_loads();
+    for (int t = 0; t < T::STAGES - 1; ++t)
+#pragma unroll
+        for (int q = 0; q < L; ++q) load(t, q);
+    wait_loads<(T::STAGES - 2) * L>();
     barrier();
 #pragma unroll
-    for (int q = 0; q < FIRST; ++q) load(1, q);
+    for (int q = 0; q < FIRST; ++q) load(T::STAGES - 1, q);
 #pragma unroll
     for (int f = 0; f < T::NI; ++f) read_b(0, 0, f);
 #pragma unroll
@@ -213,7 +219,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
 #pragma unroll
         for (int s = 0; s < PARTS; ++s) part(t, s);
     }
-    wait_loads();
+    wait_loads<0>();
     barrier();
 }
 // where element r of a wave's block lies: row of m, column of n
@@ -240,7 +246,7 @@ template <typename T, typename F>
 __device__ __forceinline__ void store_rows(char *lds, int wave, int lane, F value, uint16_t *out, int64_t stride, int rows, int cols)
 {
     constexpr int WIDTH = T::MI * 32, PITCH = WIDTH + 16, PASS = T::NI < 2 ? 1 : 2, CHUNKS = WIDTH / 16, AT_ONCE = 64 / CHUNKS;      // bytes of a row; blocks of n a time
-    static_assert(T::WAVES * PASS * 16 * PITCH <= STAGES * T::STAGE && T::NI % PASS == 0 && AT_ONCE * CHUNKS == 64, "");
+    static_assert(T::WAVES * PASS * 16 * PITCH <= T::LDS && T::NI % PASS == 0 && AT_ONCE * CHUNKS == 64, "");
     char *mine = lds + wave * (PASS * 16 * PITCH);
 #pragma unroll
     for (int j0 = 0; j0 < T::NI; j0 += PASS) {
@@ -399,7 +405,7 @@ __device__ __forceinline__ void join(float k, float &m, float &s, float2 q)
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X, int steps, Logit G)
 {
-    __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, tr;
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
@@ -459,7 +465,7 @@ __device__ __forceinline__ float dz_of(const Logit &G, const float4 &R, float z,
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, int steps, Logit G)
 {
-    __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, tr;
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
@@ -513,7 +519,7 @@ struct ToRows {
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, ToRows G)
 {
-    __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tr, th;
     if (!my_tile(G.rows / T::BN, (G.hidden + T::BM - 1) / T::BM, tr, th)) return;
     if (tr * T::BN >= *G.live.count) return;
@@ -547,7 +553,7 @@ struct ToWeights {
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, ToWeights G)
 {
-    __shared__ __attribute__((aligned(128))) char lds[STAGES * T::STAGE];
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, th;
     if (!my_tile((G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
     f32x4 acc[T::MI][T::NI];
@@ -699,7 +705,7 @@ constexpr int FEW_ROWS = 16, FEW_WORDS = 32, FEW_WAVES = 4, FEW_K = 128;
 template <bool VEC>
 __device__ __forceinline__ bf16x8 load_k(const uint16_t *p, int64_t k, int64_t n)
 {
-    if (VEC && k + 8 <= n) return __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(p + k));
+    if (VEC && k + 8 <= n) return *reinterpret_cast<const bf16x8 *>(p + k);
     uint32_t e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = k + i < n ? p[k + i] : 0;
@@ -773,23 +779,107 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few(Few G)
     if (lane < G.rows && lane < 16) G.partials[(int64_t)blockIdx.x * G.rows + lane] = float2{m, s};
 }
 
+// The sum of a wave, in all its lanes.
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ float add_dpp32(float x)
+{
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum32(float x)
+{
+    x = add_dpp32<0xb1>(x);
+    x = add_dpp32<0x4e>(x);
+    x = add_dpp32<0x141>(x);
+    x = add_dpp32<0x140>(x);
+    x = add_dpp32<0x142, 0xa>(x);
+    x = add_dpp32<0x143, 0xc>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+// Up to R <= 4 rows: a wave's lanes lie along k, so that each load is whole lines of one word's weights, where the matrix cores' operand is 64 bytes of each of 16
+// words; products of pairs are added up in 32 bits.  SPLIT waves share a word, each with NC parts of 512 of k, for which it keeps the rows in
+// registers: as few as those allow, since the sum over a wave's lanes costs as much as 900 products.
+constexpr int DOT_ROWS = 4, DOT_K = 512, DOT_HIDDEN = FEW_WAVES * DOT_K * 4;
+template <int R, int NC, int SPLIT>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_head_dot(Few G)
+{
+    constexpr int WORDS = FEW_WORDS * SPLIT / FEW_WAVES, AT_ONCE = 16 / NC < WORDS ? 16 / NC : WORDS;        // words of a wave: all, on their way at a time
+    static_assert(WORDS % AT_ONCE == 0 && R <= 2 * FEW_WAVES, "");
+    __shared__ float part[SPLIT][R][FEW_WORDS];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, share = wave % SPLIT, first = wave / SPLIT * WORDS;
+    const int64_t w0 = (int64_t)blockIdx.x * FEW_WORDS;
+    const int k0 = share * DOT_K + lane * 8;
+    u32x4 x[R][NC];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int k = k0 + c * (SPLIT * DOT_K);
+            x[r][c] = k < G.hidden ? *reinterpret_cast<const u32x4 *>(G.x + min(r, G.rows - 1) * G.x_stride + k) : u32x4{};
+        }
+#pragma unroll 1
+    for (int b = first; b < first + WORDS; b += AT_ONCE) {
+        u32x4 w[AT_ONCE][NC];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const uint16_t *p = G.w + min(w0 + b + i, G.vocab - 1) * G.w_stride;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int k = k0 + c * (SPLIT * DOT_K);
+                w[i][c] = k < G.hidden ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + k)) : u32x4{};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float s = 0.0f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w[i][c][e]), __builtin_bit_cast(bf16x2, (uint32_t)x[r][c][e]), s, false);
+                s = wave_sum32(s);
+                if (lane == 0) part[share][r][b + i] = s;
+            }
+    }
+    __syncthreads();
+    const int n = lane / FEW_WORDS + 2 * wave, w = lane % FEW_WORDS;        // half a wave a row
+    if (n >= G.rows) return;
+    float z = part[0][n][w];
+#pragma unroll
+    for (int q = 1; q < SPLIT; ++q) z += part[q][n][w];
+    if (G.bias) z += __uint_as_float((uint32_t)G.bias[min(w0 + w, G.vocab - 1)] << 16);
+    if (w0 + w >= G.vocab) z = -INFINITY;
+    if (w0 + w == G.targets[n]) G.target_logit[n] = z;
+    float m = z;
+#pragma unroll
+    for (int h = 16; h; h /= 2) m = fmaxf(m, __shfl_xor(m, h));
+    float s = __builtin_amdgcn_exp2f(G.k * (z - base_of(m)));
+#pragma unroll
+    for (int h = 16; h; h /= 2) s += __shfl_xor(s, h);
+    if (w == 0) G.partials[(int64_t)blockIdx.x * G.rows + n] = float2{m, s};
+}
+
 // ---- the plan of a call ------------------------------------------------------------------------
-typedef Tile<256, 256, 2, 4> Big;          // many rows
-typedef Tile<256, 64, 4, 1> Slim;          // up to 64 rows that count beside each other
+typedef Tile<256, 256, 2, 4, 2> Big;          // many rows
+typedef Tile<128, 128, 2, 2, 2> Mid;          // up to 128, or too few for the others
+typedef Tile<128, 64, 4, 1, 3> Slim;          // up to 64: the weights' way from memory is all the time there is
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 256 << 20;          // of dz
 constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
+constexpr int64_t MID_TILES = 200;                  // large tiles of z below which there are too few for the chip
 
 struct Plan {
     int64_t rows;            // of the packed batch
     int64_t width;           // of its rows, of packed weights and of sums to the rows
     int64_t piece;           // words
     int64_t packed;          // words of a piece where weights have to be packed
-    int64_t tiles;           // of words
+    int64_t tiles;           // of 256 words
+    int64_t joined;          // maxima and sums of a row
     int splits;              // of the sums to the rows
-    bool slim, kept;
+    int words, side;         // of a tile: words (or hidden columns), rows
+    bool kept;
     size_t index, x, partials, target, row, z, dz, sum, w, all;      // places in the workspace, and its size
 };
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -797,16 +887,17 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
 {
     Plan P = {};
-    P.slim = rows <= Slim::BN;
-    const int64_t tile = P.slim ? Slim::BN : Big::BN;
-    P.rows = up(std::max<int64_t>(rows, 1), tile);
+    P.side = rows <= Slim::BN ? Slim::BN : rows <= Mid::BN || up(rows, Big::BN) / Big::BN * (up(vocab, Big::BM) / Big::BM) < MID_TILES ? Mid::BN : Big::BN;
+    P.words = P.side == Big::BN ? Big::BM : Slim::BM;
+    P.rows = up(std::max<int64_t>(rows, 1), P.side);
     P.width = up(hidden, 64);
     P.tiles = up(vocab, 256) / 256;
+    P.joined = up(vocab, P.words) / P.words;
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * P.rows * 256));
     P.kept = gradient && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
     P.piece = (P.kept ? P.tiles : std::min(P.tiles, most)) * 256;
     P.packed = std::min(P.piece, std::max<int64_t>(1, kPackedBytes / (2 * P.width * 256)) * 256);
-    const int64_t out = P.rows / tile * (up(hidden, 256) / 256);                // tiles of the sums to the rows
+    const int64_t out = P.rows / P.side * (up(hidden, P.words) / P.words);      // tiles of the sums to the rows
     P.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(P.piece / 1024, 32), 512 / out));
     size_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -816,7 +907,7 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     };
     P.index = take((2 * P.rows + 64) * 4);
     P.x = take(P.rows * P.width * 2);
-    P.partials = take(std::max(P.tiles * P.rows, rows <= FEW_ROWS ? up(vocab, FEW_WORDS) / FEW_WORDS * FEW_ROWS : 0) * 8);
+    P.partials = take(std::max(P.joined * P.rows, rows <= FEW_ROWS ? up(vocab, FEW_WORDS) / FEW_WORDS * FEW_ROWS : 0) * 8);
     P.target = take(P.rows * 4);
     P.row = take(P.rows * 16);
     P.z = P.kept ? take(P.rows * P.tiles * 256 * 4) : at;
@@ -924,21 +1015,39 @@ static hipError_t forward(const Call &C, float *logp, float *row_stats, const fl
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    const Join J = {C.partials(), C.target(), C.P.tiles, C.P.rows, kLog2e * C.it, C.it, logp, row_stats, row_weights, gradient ? C.row() : nullptr, C.live, nullptr, 0};
-    if (C.P.slim) k_head_join<1><<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(J);
+    const Join J = {C.partials(), C.target(), C.P.joined, C.P.rows, kLog2e * C.it, C.it, logp, row_stats, row_weights, gradient ? C.row() : nullptr, C.live, nullptr, 0};
+    if (C.P.side < Big::BN) k_head_join<1><<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(J);
     else k_head_join<32><<<(uint32_t)(C.P.rows / 32), 256, 0, C.stream>>>(J);
     return hipGetLastError();
 }
 static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
 {
-    return C.P.slim ? forward<Slim>(C, logp, row_stats, row_weights, gradient) : forward<Big>(C, logp, row_stats, row_weights, gradient);
+    return (C.P.side == Slim::BN ? forward<Slim> : C.P.side == Mid::BN ? forward<Mid> : forward<Big>)(C, logp, row_stats, row_weights, gradient);
 }
+template <int R> static void launch_dot(const Few &G, uint32_t grid, hipStream_t stream)
+{
+    if (G.hidden <= DOT_K) k_head_dot<R, 1, 1><<<grid, FEW_WAVES * 64, 0, stream>>>(G);
+    else if (G.hidden <= 2 * DOT_K) k_head_dot<R, 2, 1><<<grid, FEW_WAVES * 64, 0, stream>>>(G);
+    else if (G.hidden <= 4 * DOT_K) k_head_dot<R, 4, 1><<<grid, FEW_WAVES * 64, 0, stream>>>(G);
+    else if (G.hidden <= 8 * DOT_K) k_head_dot<R, 4, 2><<<grid, FEW_WAVES * 64, 0, stream>>>(G);
+    else k_head_dot<R, 4, 4><<<grid, FEW_WAVES * 64, 0, stream>>>(G);
+}
+static void launch_dot(const Few &G, uint32_t grid, hipStream_t stream)
+{
+    if (G.rows == 1) launch_dot<1>(G, grid, stream);
+    else launch_dot<DOT_ROWS>(G, grid, stream);
+}
+// Rows that are scored without LDS: up to 4 in any case, up to 16 while the weights are few (us, against tiles, 16 rows: 2^25 values 21/24, 2^27 57/57, 2^28 123/129,
+// 2^29 267/187: half lines, but more workgroups).
+static bool few_rows(int64_t rows, int64_t hidden, int64_t vocab) { return rows <= DOT_ROWS || (rows <= FEW_ROWS && hidden * vocab <= (int64_t)1 << 28); }
 static hipError_t forward_few(const Call &C, float *logp, float *row_stats)
 {
     const gs_head &h = C.h;
     const Few G = {h.x, h.w, h.bias, h.x_stride, h.w_stride, h.hidden, h.vocab, (int)h.rows, C.targets, kLog2e * C.it, C.partials(), C.target()};
     const int64_t tiles = up(h.vocab, FEW_WORDS) / FEW_WORDS;
-    if (multiple16(h.x, h.x_stride) && multiple16(h.w, h.w_stride)) k_head_few<true><<<(uint32_t)tiles, FEW_WAVES * 64, 0, C.stream>>>(G);
+    const bool whole = multiple16(h.x, h.x_stride) && multiple16(h.w, h.w_stride);
+    if (whole && h.hidden % 8 == 0 && h.hidden <= DOT_HIDDEN && h.rows <= DOT_ROWS) launch_dot(G, (uint32_t)tiles, C.stream);
+    else if (whole) k_head_few<true><<<(uint32_t)tiles, FEW_WAVES * 64, 0, C.stream>>>(G);
     else k_head_few<false><<<(uint32_t)tiles, FEW_WAVES * 64, 0, C.stream>>>(G);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const Join J = {C.partials(), C.target(), tiles, h.rows, kLog2e * C.it, C.it, logp, row_stats, nullptr, nullptr, Live{}, C.targets, (int)h.vocab};
@@ -950,9 +1059,9 @@ template <typename T>
 static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
 {
     const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
-    const int64_t H = C.P.width, htiles = up(H, 256) / 256, rtiles = C.P.rows / T::BN;
+    const int64_t H = C.P.width, htiles = up(H, T::BM) / T::BM, rtiles = C.P.rows / T::BN;
     hipError_t e = pieces(C, [&](int64_t w, int64_t words, const Operand &W) {
-        const int64_t wtiles = up(words, 256) / 256;
+        const int64_t wtiles = up(words, T::BM) / T::BM;
         const Logit G = logit_of(C, w, words);
         if (have_z) k_head_dz_kept<<<dim3((uint32_t)C.P.rows, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G);
         else k_head_dz<T><<<grid_of(wtiles * rtiles), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
@@ -963,7 +1072,7 @@ static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
         }
         if (D.dw) {
             const ToWeights R = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : H, C.row()};
-            k_head_dw<Big><<<grid_of(wtiles * (up(C.h.hidden, 256) / 256)), Big::BLOCK, 0, C.stream>>>(X, DZ, R);
+            k_head_dw<Big><<<grid_of(up(words, 256) / 256 * (up(C.h.hidden, 256) / 256)), Big::BLOCK, 0, C.stream>>>(X, DZ, R);
         }
         if (D.dbias) k_head_db<<<(uint32_t)((words + 127) / 128), 1024, 0, C.stream>>>(C.dz(), C.P.piece, C.live, words, C.row(), D.dbias + w);
         return hipGetLastError();
@@ -973,7 +1082,10 @@ static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
                                                                                                           D.dx, C.h.rows > 1 ? D.dx_stride : C.h.hidden);
     return hipGetLastError();
 }
-static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z) { return C.P.slim ? backward<Slim>(C, D, have_z) : backward<Big>(C, D, have_z); }
+static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
+{
+    return (C.P.side == Slim::BN ? backward<Slim> : C.P.side == Mid::BN ? backward<Mid> : backward<Big>)(C, D, have_z);
+}
 
 // ---- checks -------------------------------------------------------------------------------------
 static bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -1063,7 +1175,7 @@ gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temper
     if (!R.apart()) return GS_ERR_INVALID_ARG;
     const Call C = call_of(*head, targets, temperature, false, d_workspace, stream);
     hipError_t e;
-    if (rows <= FEW_ROWS) {
+    if (few_rows(rows, head->hidden, head->vocab)) {
         e = forward_few(C, logp, row_stats);
     } else {
         e = pack_rows(C, nullptr, logp, row_stats);

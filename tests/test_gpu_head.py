@@ -69,7 +69,7 @@ class Case:
 
 
 SIZES = [(1, 1, 1), (1, 64, 1), (1, 64, 2), (2, 8, 255), (3, 64, 256), (15, 72, 257), (16, 128, 1000), (17, 100, 513), (33, 512, 300), (64, 7, 999), (65, 192, 1031),
-         (255, 64, 511), (256, 256, 512), (257, 264, 513), (300, 1000, 777), (513, 320, 1025), (700, 63, 90)]
+         (255, 64, 511), (256, 256, 512), (257, 264, 513), (300, 1000, 777), (513, 320, 1025), (700, 63, 90), (128, 448, 1500), (129, 128, 255), (1500, 128, 40_100)]
 
 
 @pytest.mark.parametrize("rows, hidden, vocab", SIZES)
@@ -78,6 +78,17 @@ def test_scores(rows, hidden, vocab):
     got = c.score(0.7)
     out, bound = oracle(c.x, c.w, c.bias, c.targets, None, 0.7, gradient=False)
     check(got, out, bound, ["logp", "M", "S"])
+
+
+@pytest.mark.parametrize("hidden", [8, 100, 504, 512, 2048, 2056, 4096, 4104, 8192, 8200])
+@pytest.mark.parametrize("rows", [1, 2, 4, 5, 8, 9, 16, 17])
+def test_scores_of_few_rows(rows, hidden):
+    """Both sides of the lines between the kernels for few rows."""
+    for vocab, bias in ((700, False), (65, True)):
+        c = Case(rows, hidden, vocab, bias=bias, prompt=rows > 4)
+        got = c.score(1.3)
+        out, bound = oracle(c.x, c.w, c.bias, c.targets, None, 1.3, gradient=False)
+        check(got, out, bound, ["logp", "M", "S"])
 
 
 @pytest.mark.parametrize("rows, hidden, vocab", SIZES)
