@@ -41,6 +41,12 @@ decltype(&::gs_policy_loss) f_policy_loss;
 decltype(&::gs_preference_loss) f_preference_loss;
 decltype(&::gs_grads_sqnorm) f_grads_sqnorm;
 decltype(&::gs_grads_clip) f_grads_clip;
+decltype(&::gs_head_logp) f_head_logp;
+decltype(&::gs_head_logp_grad) f_head_logp_grad;
+decltype(&::gs_head_cross_entropy) f_head_cross_entropy;
+decltype(&::gs_layer_norm) f_layer_norm;
+decltype(&::gs_layer_norm_grad) f_layer_norm_grad;
+decltype(&::gs_dropout) f_dropout;
 PyTypeObject *hparams_type, *policy_type, *preference_type;
 PyObject *policy_names[4], *preference_names[3];
 PyObject *in_bad_fork;
@@ -177,6 +183,74 @@ struct Reader {
         const gs_logits m = matrix(o);
         if (m.rows != x.rows || m.vocab != x.vocab || m.dtype != x.dtype) no();
         return m;
+    }
+
+    // a tensor on the current device; those of another one are refused in the general way
+    const at::Tensor *here(PyObject *o)
+    {
+        const at::Tensor *t = tensor(o);
+        if (t && t->get_device() != c10::hip::current_device()) return no(), nullptr;
+        return t;
+    }
+    template <typename T> T *typed_here(PyObject *o, int64_t count, at::ScalarType type, bool optional = false)
+    {
+        if (optional && o == Py_None) return nullptr;
+        return here(o) ? typed<T>(o, count, type) : nullptr;
+    }
+    void *space(PyObject *o) { return o == Py_None || here(o) ? address(o) : nullptr; }
+    // rows of `type` (of any, if that is Undefined) whose elements lie side by side; with shape, of that shape
+    gs_matrix rows(PyObject *o, at::ScalarType type, const gs_matrix *like = nullptr)
+    {
+        const at::Tensor *t = here(o);
+        if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1) || (type != at::ScalarType::Undefined && t->scalar_type() != type)) return no(), gs_matrix{};
+        const gs_matrix m = {t->data_ptr(), t->size(0), t->size(1), t->stride(0), dtype(*t)};
+        if (like && (m.rows != like->rows || m.cols != like->cols || m.dtype != like->dtype)) no();
+        return m;
+    }
+    gs_head head(PyObject *x, PyObject *w, PyObject *bias)
+    {
+        const gs_matrix a = rows(x, at::kBFloat16), b = rows(w, at::kBFloat16);
+        if (!usual || a.cols != b.cols) return no(), gs_head{};
+        return {static_cast<const uint16_t *>(a.data), static_cast<const uint16_t *>(b.data), typed_here<const uint16_t>(bias, b.rows, at::kBFloat16, true), a.rows, a.cols, b.rows,
+                a.row_stride, b.row_stride};
+    }
+    gs_head_grads head_grads(const gs_head &h, PyObject *dx, PyObject *dw, PyObject *db)
+    {
+        gs_head_grads g = {};
+        if (!usual) return g;
+        const gs_matrix x = {nullptr, h.rows, h.hidden, 0, GS_BF16}, w = {nullptr, h.vocab, h.hidden, 0, GS_BF16};
+        if (dx != Py_None) {
+            const gs_matrix m = rows(dx, at::kBFloat16, &x);
+            g.dx = static_cast<uint16_t *>(const_cast<void *>(m.data)), g.dx_stride = m.row_stride;
+        }
+        if (dw != Py_None) {
+            const gs_matrix m = rows(dw, at::kBFloat16, &w);
+            g.dw = static_cast<uint16_t *>(const_cast<void *>(m.data)), g.dw_stride = m.row_stride;
+        }
+        g.dbias = typed_here<uint16_t>(db, h.vocab, at::kBFloat16, true);
+        return g;
+    }
+    // a layer norm's vectors, of one type (fp32 if there is none)
+    template <int N> int32_t vectors(int64_t cols, PyObject *const (&o)[N], void *(&to)[N])
+    {
+        at::ScalarType type = at::ScalarType::Undefined;
+        for (int i = 0; i < N && usual; ++i) {
+            to[i] = nullptr;
+            if (o[i] == Py_None) continue;
+            const at::Tensor *t = here(o[i]);
+            if (!t || (type != at::ScalarType::Undefined && t->scalar_type() != type)) return (int32_t)no();
+            type = t->scalar_type();
+            to[i] = typed<void>(o[i], cols, type);
+        }
+        if (type == at::ScalarType::Undefined || type == at::kFloat) return GS_F32;
+        return type == at::kBFloat16 ? GS_BF16 : (int32_t)no();
+    }
+    uint64_t word(PyObject *o)
+    {
+        if (!PyLong_CheckExact(o)) return (uint64_t)no();
+        const uint64_t x = PyLong_AsUnsignedLongLong(o);
+        if (PyErr_Occurred()) PyErr_Clear(), no();
+        return x;
     }
 
     float real(PyObject *o)
@@ -548,6 +622,128 @@ PyObject *grads_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
     }, [&] { return f_grads_clip(list.data(), (int64_t)list.size(), sq, max_norm, norm, s); });
 }
 
+// x, w, bias, targets, logp, row_stats, temperature, d_workspace, workspace_bytes, stream
+PyObject *head_logp(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_head h = {};
+    const int64_t *targets = nullptr;
+    float *logp = nullptr, *stats = nullptr, temperature = 0;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    return run<10>(n, [&](Reader &r) {
+        h = r.head(a[0], a[1], a[2]);
+        targets = r.typed_here<const int64_t>(a[3], h.rows, at::kLong), logp = r.typed_here<float>(a[4], h.rows, at::kFloat);
+        stats = r.typed_here<float>(a[5], 2 * h.rows, at::kFloat, true), temperature = r.real(a[6]);
+        ws = r.space(a[7]), bytes = r.workspace_bytes(a[8], a[7]), s = r.stream(a[9]);
+    }, [&] { return f_head_logp(&h, targets, temperature, logp, stats, ws, bytes, s); });
+}
+
+// x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace, temperature, workspace_bytes, stream
+PyObject *head_logp_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_head h = {};
+    gs_head_grads g = {};
+    const int64_t *targets = nullptr;
+    const float *stats = nullptr, *dlogp = nullptr;
+    float temperature = 0;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    return run<13>(n, [&](Reader &r) {
+        h = r.head(a[0], a[1], a[2]);
+        targets = r.typed_here<const int64_t>(a[3], h.rows, at::kLong), stats = r.typed_here<const float>(a[4], 2 * h.rows, at::kFloat);
+        dlogp = r.typed_here<const float>(a[5], h.rows, at::kFloat), g = r.head_grads(h, a[6], a[7], a[8]);
+        ws = r.space(a[9]), temperature = r.real(a[10]), bytes = r.workspace_bytes(a[11], a[9]), s = r.stream(a[12]);
+    }, [&] { return f_head_logp_grad(&h, targets, temperature, stats, dlogp, &g, ws, bytes, s); });
+}
+
+// x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace, temperature, accumulate, workspace_bytes, stream
+PyObject *head_cross_entropy(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_head h = {};
+    gs_head_grads g = {};
+    const bool grads = n == 15 && (a[6] != Py_None || a[7] != Py_None || a[8] != Py_None);
+    const int64_t *targets = nullptr;
+    const float *weights = nullptr;
+    float *logp = nullptr, *loss = nullptr, temperature = 0;
+    void *ws = nullptr, *s = nullptr;
+    size_t bytes = 0;
+    int acc = 0;
+    return run<15>(n, [&](Reader &r) {
+        h = r.head(a[0], a[1], a[2]);
+        targets = r.typed_here<const int64_t>(a[3], h.rows, at::kLong), weights = r.typed_here<const float>(a[4], h.rows, at::kFloat, true);
+        logp = r.typed_here<float>(a[5], h.rows, at::kFloat), g = r.head_grads(h, a[6], a[7], a[8]), loss = r.typed_here<float>(a[9], 1, at::kFloat);
+        ws = r.space(a[10]), temperature = r.real(a[11]), acc = r.flag(a[12]), bytes = r.workspace_bytes(a[13], a[10]), s = r.stream(a[14]);
+    }, [&] { return f_head_cross_entropy(&h, targets, weights, temperature, logp, grads ? &g : nullptr, loss, acc, ws, bytes, s); });
+}
+
+// x, gamma, beta, y, row_stats, eps, stream
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_matrix x = {}, y = {};
+    void *w[2] = {}, *s = nullptr;
+    int32_t type = 0;
+    float *stats = nullptr, eps = 0;
+    return run<7>(n, [&](Reader &r) {
+        x = r.rows(a[0], at::ScalarType::Undefined), y = r.rows(a[3], at::ScalarType::Undefined, &x);
+        type = r.vectors(x.cols, {a[1], a[2]}, w);
+        stats = r.typed_here<float>(a[4], 2 * x.rows, at::kFloat, true), eps = r.real(a[5]), s = r.stream(a[6]);
+    }, [&] { return f_layer_norm(&x, w[0], w[1], type, eps, const_cast<void *>(y.data), y.row_stride, stats, s); });
+}
+
+// dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace, workspace_bytes, stream
+PyObject *layer_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    gs_matrix x = {}, dy = {}, dx = {};
+    void *w[3] = {}, *ws = nullptr, *s = nullptr;
+    int32_t type = 0;
+    const float *stats = nullptr;
+    size_t bytes = 0;
+    return run<10>(n, [&](Reader &r) {
+        x = r.rows(a[1], at::ScalarType::Undefined), dy = r.rows(a[0], at::ScalarType::Undefined, &x), dx = r.rows(a[4], at::ScalarType::Undefined, &x);
+        type = r.vectors(x.cols, {a[2], a[5], a[6]}, w);
+        stats = r.typed_here<const float>(a[3], 2 * x.rows, at::kFloat);
+        ws = r.space(a[7]), bytes = r.workspace_bytes(a[8], a[7]), s = r.stream(a[9]);
+    }, [&] {
+        return f_layer_norm_grad(&x, w[0], type, stats, dy.data, dy.row_stride, const_cast<void *>(dx.data), dx.row_stride, w[1], w[2], ws, bytes, s);
+    });
+}
+
+// x, residual, out, p, seed, offset, d_step, stream
+PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    const void *x = nullptr, *residual = nullptr;
+    void *out = nullptr, *s = nullptr;
+    int64_t count = 0;
+    int32_t type = 0;
+    float p = 0;
+    uint64_t seed = 0, offset = 0;
+    const uint64_t *step = nullptr;
+    return run<8>(n, [&](Reader &r) {
+        const at::Tensor *t = r.here(a[0]), *o = r.here(a[2]), *q = a[1] == Py_None ? nullptr : r.here(a[1]);
+        if (!r.usual) return;
+        count = t->numel(), type = r.dtype(*t);
+        if (o->numel() != count || (q && q->numel() != count)) return (void)r.no();
+        x = r.typed<void>(a[0], count, t->scalar_type()), residual = r.typed<void>(a[1], count, t->scalar_type(), true), out = r.typed<void>(a[2], count, t->scalar_type());
+        p = r.real(a[3]), seed = r.word(a[4]), offset = r.word(a[5]), step = r.typed_here<const uint64_t>(a[6], 1, at::kLong, true), s = r.stream(a[7]);
+    }, [&] { return f_dropout(x, residual, out, count, type, p, seed, offset, step, s); });
+}
+
+// the six entry points above, addresses in that order
+PyObject *setup_layers(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *f[6];
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "setup_layers takes 6 arguments"), nullptr;
+    for (int i = 0; i < 6; ++i)
+        if (!(f[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "null entry point");
+    f_head_logp = reinterpret_cast<decltype(f_head_logp)>(f[0]);
+    f_head_logp_grad = reinterpret_cast<decltype(f_head_logp_grad)>(f[1]);
+    f_head_cross_entropy = reinterpret_cast<decltype(f_head_cross_entropy)>(f[2]);
+    f_layer_norm = reinterpret_cast<decltype(f_layer_norm)>(f[3]);
+    f_layer_norm_grad = reinterpret_cast<decltype(f_layer_norm_grad)>(f[4]);
+    f_dropout = reinterpret_cast<decltype(f_dropout)>(f[5]);
+    Py_RETURN_NONE;
+}
+
 template <int N>
 bool intern(PyObject *(&to)[N], const char *const (&names)[N])
 {
@@ -610,7 +806,8 @@ PyMethodDef methods[] = {
     GS_METHOD(setup), GS_METHOD(grad_sqnorm), GS_METHOD(grad_sqnorm_noalloc), GS_METHOD(grad_accum_sqnorm),
     GS_METHOD(accum_add), GS_METHOD(acc_sqnorm), GS_METHOD(accum_adamw), GS_METHOD(adamw_from_acc),
     GS_METHOD(accum_adamw_oop), GS_METHOD(accum_adamw_spec), GS_METHOD(setup_loss), GS_METHOD(token_logp), GS_METHOD(token_logp_grad),
-    GS_METHOD(policy_loss), GS_METHOD(preference_loss), GS_METHOD(grads_sqnorm), GS_METHOD(grads_clip), {nullptr, nullptr, 0, nullptr}};
+    GS_METHOD(policy_loss), GS_METHOD(preference_loss), GS_METHOD(grads_sqnorm), GS_METHOD(grads_clip), GS_METHOD(setup_layers),
+    GS_METHOD(head_logp), GS_METHOD(head_logp_grad), GS_METHOD(head_cross_entropy), GS_METHOD(layer_norm), GS_METHOD(layer_norm_grad), GS_METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gs_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -64,47 +64,90 @@ template <typename E> __device__ __forceinline__ u32x4 load_vector(const typenam
 {
     return *reinterpret_cast<const typename Loose<sizeof(typename E::T)>::T *>(p);
 }
-// Elements [c, c + PER) of an array that has `n`, as far as it has them; 0 for the others.
-template <typename E> __device__ __forceinline__ void load_some(const typename E::T *p, int64_t c, int64_t n, float (&z)[E::PER])
+// a stream's, which is read once
+template <typename E> __device__ __forceinline__ u32x4 load_once(const typename E::T *p)
 {
-    if (c + E::PER <= n) {
-        E::widen(load_vector<E>(p + c), z);
-    } else {
-#pragma unroll
-        for (int i = 0; i < E::PER; ++i) z[i] = c + i < n ? E::load(p + c + i) : 0.0f;
-    }
+    return __builtin_nontemporal_load(reinterpret_cast<const typename Loose<sizeof(typename E::T)>::T *>(p));
 }
-template <typename E> __device__ __forceinline__ void store_some(typename E::T *p, int64_t c, int64_t n, const float (&z)[E::PER])
+// Past the caches where a wave's vectors are whole lines; cut ones (an address off 16 bytes) are left to them to join (4095 x 5003 fp32, dropout: 36 us against 88).
+template <typename E> __device__ __forceinline__ void store_vector(typename E::T *p, u32x4 q, bool through)
 {
-    if (c + E::PER <= n) {
-        *reinterpret_cast<typename Loose<sizeof(typename E::T)>::T *>(p + c) = E::narrow(z);
+    if (through) store_through(reinterpret_cast<u32x4 *>(p), q);
+    else *reinterpret_cast<typename Loose<sizeof(typename E::T)>::T *>(p) = q;
+}
+// whether rows of vectors all start on 16 bytes
+static bool whole_lines(const void *p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride_bytes) & 15) == 0; }
+// one element in its place of a vector
+template <typename E> __device__ __forceinline__ u32x4 vector_of(const typename E::T (&e)[E::PER])
+{
+    u32x4 q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (E::PER == 8) q[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+        else q[i] = __float_as_uint(e[i]);
+    }
+    return q;
+}
+// Elements [c, c + PER) of an array that has `n`, as far as it has them; 0 for the others.  WHOLE: n is a multiple of PER.
+template <typename E, bool ONCE, bool WHOLE = false> __device__ __forceinline__ u32x4 load_some(const typename E::T *p, int64_t c, int64_t n)
+{
+    if (WHOLE && c >= n) return u32x4{};
+    if (WHOLE || c + E::PER <= n) return ONCE ? load_once<E>(p + c) : load_vector<E>(p + c);
+    typename E::T e[E::PER];
+#pragma unroll
+    for (int i = 0; i < E::PER; ++i) e[i] = c + i < n ? p[c + i] : (typename E::T)0;
+    return vector_of<E>(e);
+}
+template <typename E, bool WHOLE = false> __device__ __forceinline__ void store_some(typename E::T *p, int64_t c, int64_t n, const float (&z)[E::PER], bool through)
+{
+    if (WHOLE || c + E::PER <= n) {
+        store_vector<E>(p + c, E::narrow(z), through);
     } else {
 #pragma unroll
         for (int i = 0; i < E::PER; ++i)
             if (c + i < n) E::store(p + c + i, z[i]);
     }
 }
-// PER values of the scale or the shift, in a type of their own
-template <typename W, int PER> __device__ __forceinline__ void load_weights(const void *w, int64_t c, int64_t n, float none, float (&z)[PER])
-{
-    const typename W::T *p = static_cast<const typename W::T *>(w);
-    if (!p) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) z[i] = none;
-    } else if (PER % W::PER == 0 && c + PER <= n) {
-        constexpr int N = PER / W::PER ? PER / W::PER : 1;
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
+// PER values of the scale or the shift, in a type of their own, as they lie there: `none` without an array
+template <typename W, int PER, bool WHOLE = false> struct Weights {
+    static constexpr int N = PER / W::PER ? PER / W::PER : 1;        // vectors; of bf16 beside fp32 rows, half of one
+    u32x4 q[N];
+    __device__ __forceinline__ void load(const void *w, int64_t c, int64_t n, float none)
+    {
+        const typename W::T *p = static_cast<const typename W::T *>(w);
+        if (!p) {
             float f[W::PER];
-            W::widen(load_vector<W>(p + c + q * W::PER), f);
 #pragma unroll
-            for (int i = 0; i < W::PER; ++i) z[q * W::PER + i] = f[i];
+            for (int i = 0; i < W::PER; ++i) f[i] = none;
+#pragma unroll
+            for (int v = 0; v < N; ++v) q[v] = W::narrow(f);
+        } else if constexpr (W::PER <= PER) {
+#pragma unroll
+            for (int v = 0; v < N; ++v) q[v] = load_some<W, false, WHOLE>(p, c + v * W::PER, n);
+        } else {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            typedef u32x2 loose_u32x2 __attribute__((aligned(2)));
+            if (WHOLE && c >= n) {
+                q[0] = u32x4{};
+            } else if (WHOLE || c + PER <= n) {
+                const u32x2 h = *reinterpret_cast<const loose_u32x2 *>(p + c);
+                q[0] = u32x4{h[0], h[1], 0, 0};
+            } else {
+                q[0] = load_some<W, false>(p, c, n);
+            }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) z[i] = c + i < n ? W::load(p + c + i) : 0.0f;
     }
-}
+    __device__ __forceinline__ void get(float (&z)[PER]) const
+    {
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+            float f[W::PER];
+            W::widen(q[v], f);
+#pragma unroll
+            for (int i = 0; i < W::PER && v * W::PER + i < PER; ++i) z[v * W::PER + i] = f[i];
+        }
+    }
+};
 
 // ---- sums of a team -----------------------------------------------------------------------------
 template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ float add_dpp32(float x)
@@ -147,6 +190,9 @@ template <int TEAM, int N> __device__ __forceinline__ void team_sums(float (&x)[
     }
 }
 
+// Elements are kept as they came and widened each time: without this the compiler keeps the widened ones, in twice the registers (bf16).
+__device__ __forceinline__ void as_it_came(u32x4 &q) { asm("" : "+v"(q)); }
+
 // ---- forward -------------------------------------------------------------------------------------
 struct NormArgs {
     const void *x;
@@ -156,9 +202,11 @@ struct NormArgs {
     void *y;
     int64_t y_stride;
     float *stats;
+    bool through;
 };
-// A row a team, NV vectors a lane; HELD: they hold the row, else it is read three times.
-template <typename E, typename W, int TEAM, int NV, bool HELD>
+// A row a team, NV vectors a lane; HELD: they hold the row, else it is read three times.  EARLY: scale and shift are on their way while the sums are taken, which
+// is a trip to memory less where the time is a chain of them, and as many registers again.
+template <typename E, typename W, int TEAM, int NV, bool HELD, bool EARLY>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm(NormArgs A)
 {
     constexpr int TEAMS = TEAM < 256 ? 256 / TEAM : 1, PER = E::PER;
@@ -169,63 +217,151 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm(NormArgs A)
     const int64_t n = A.cols;
     const typename E::T *x = static_cast<const typename E::T *>(A.x) + row * A.stride;
     typename E::T *y = static_cast<typename E::T *>(A.y) + row * A.y_stride;
-    float z[NV][PER], sum[1] = {0.0f};
+    u32x4 q[NV];
+    Weights<W, PER> gamma[NV], beta[NV];
+    float z[PER], sum[1] = {0.0f};
     const int64_t by = (int64_t)TEAM * PER;
     if constexpr (HELD) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) load_some<E>(x, v * by + lane * PER, n, z[v]);
+        for (int v = 0; v < NV; ++v) q[v] = load_some<E, true>(x, v * by + lane * PER, n);
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; EARLY && v < NV; ++v) {
+            gamma[v].load(A.gamma, v * by + lane * PER, n, 1.0f);
+            beta[v].load(A.beta, v * by + lane * PER, n, 0.0f);
+        }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sum[0] += z[v][i];
+        for (int v = 0; v < NV; ++v) {
+            E::widen(q[v], z);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[0] += z[i];
+        }
     } else {
         for (int64_t c = lane * PER; c < n; c += by) {
-            load_some<E>(x, c, n, z[0]);
+            E::widen(load_some<E, false>(x, c, n), z);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sum[0] += z[0][i];
+            for (int i = 0; i < PER; ++i) sum[0] += z[i];
         }
     }
     team_sums<TEAM>(sum, lds[0]);
     const float mean = sum[0] / (float)n;
     sum[0] = 0.0f;
+    auto squares = [&](int64_t c, u32x4 v) {
+        E::widen(v, z);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const float d = z[i] - mean;
+            if (c + i < n) sum[0] += d * d;
+        }
+    };
     if constexpr (HELD) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                z[v][i] -= mean;
-                if (v * by + lane * PER + i < n) sum[0] += z[v][i] * z[v][i];
-            }
-    } else {
-        for (int64_t c = lane * PER; c < n; c += by) {
-            load_some<E>(x, c, n, z[0]);
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (c + i < n) sum[0] += (z[0][i] - mean) * (z[0][i] - mean);
+        for (int v = 0; v < NV; ++v) {
+            as_it_came(q[v]);
+            squares(v * by + lane * PER, q[v]);
         }
+    } else {
+        for (int64_t c = lane * PER; c < n; c += by) squares(c, load_some<E, false>(x, c, n));
     }
     team_sums<TEAM>(sum, lds[1]);
     const float rstd = 1.0f / sqrtf(sum[0] / (float)n + A.eps);
     if (A.stats && lane == 0) A.stats[2 * row] = mean, A.stats[2 * row + 1] = rstd;
-    auto write = [&](int64_t c, float (&d)[PER]) {
+    auto write = [&](int64_t c, u32x4 v, const Weights<W, PER> &gv, const Weights<W, PER> &bv) {
         float g[PER], b[PER];
-        load_weights<W, PER>(A.gamma, c, n, 1.0f, g);
-        load_weights<W, PER>(A.beta, c, n, 0.0f, b);
+        E::widen(v, z);
+        gv.get(g);
+        bv.get(b);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) d[i] = d[i] * rstd * g[i] + b[i];
-        store_some<E>(y, c, n, d);
+        for (int i = 0; i < PER; ++i) z[i] = (z[i] - mean) * rstd * g[i] + b[i];
+        store_some<E>(y, c, n, z, A.through);
     };
     if constexpr (HELD) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (v * by + lane * PER < n) write(v * by + lane * PER, z[v]);
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = v * by + lane * PER;
+            if (c >= n) continue;
+            if (!EARLY) {
+                gamma[v].load(A.gamma, c, n, 1.0f);
+                beta[v].load(A.beta, c, n, 0.0f);
+            }
+            as_it_came(q[v]);
+            write(c, q[v], gamma[v], beta[v]);
+        }
     } else {
         for (int64_t c = lane * PER; c < n; c += by) {
-            load_some<E>(x, c, n, z[0]);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) z[0][i] -= mean;
-            write(c, z[0]);
+            gamma[0].load(A.gamma, c, n, 1.0f);
+            beta[0].load(A.beta, c, n, 0.0f);
+            write(c, load_some<E, false>(x, c, n), gamma[0], beta[0]);
         }
+    }
+}
+
+// The same for many rows: workgroups that stay, take rows in turn and have the next one on its way while one is worked on; scale and shift are read once.
+template <typename E, typename W, int TEAM, int NV, bool WHOLE>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_many(NormArgs A)
+{
+    constexpr int TEAMS = TEAM < 256 ? 256 / TEAM : 1, PER = E::PER;
+    __shared__ float lds[2][2][TEAM / 64];
+    const int team = TEAMS > 1 ? threadIdx.x / TEAM : 0, lane = TEAMS > 1 ? threadIdx.x % TEAM : threadIdx.x;
+    const int64_t n = A.cols, by = (int64_t)TEAM * PER, step = (int64_t)gridDim.x * TEAMS;
+    Weights<W, PER, WHOLE> gamma[NV], beta[NV];
+    u32x4 q[2][NV];
+    auto fetch = [&](int64_t row, int to) {
+        const typename E::T *x = static_cast<const typename E::T *>(A.x) + row * A.stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) q[to][v] = load_some<E, true, WHOLE>(x, v * by + lane * PER, n);
+    };
+    auto work = [&](int64_t row, int at) {
+        float z[PER], sum[1] = {0.0f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            E::widen(q[at][v], z);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[0] += z[i];
+        }
+        team_sums<TEAM>(sum, lds[at][0]);
+        const float mean = sum[0] / (float)n;
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            as_it_came(q[at][v]);
+            E::widen(q[at][v], z);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float d = z[i] - mean;
+                if (v * by + lane * PER + (WHOLE ? 0 : i) < n) sum[0] += d * d;
+            }
+        }
+        team_sums<TEAM>(sum, lds[at][1]);
+        const float rstd = 1.0f / sqrtf(sum[0] / (float)n + A.eps);
+        if (A.stats && lane == 0) A.stats[2 * row] = mean, A.stats[2 * row + 1] = rstd;
+        typename E::T *y = static_cast<typename E::T *>(A.y) + row * A.y_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float g[PER], b[PER];
+            as_it_came(q[at][v]);
+#pragma unroll
+            for (int i = 0; i < gamma[v].N; ++i) as_it_came(gamma[v].q[i]), as_it_came(beta[v].q[i]);
+            E::widen(q[at][v], z);
+            gamma[v].get(g);
+            beta[v].get(b);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) z[i] = (z[i] - mean) * rstd * g[i] + b[i];
+            if (v * by + lane * PER < n) store_some<E, WHOLE>(y, v * by + lane * PER, n, z, A.through);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * TEAMS + team;
+    if (row < A.rows) fetch(row, 0);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        gamma[v].load(A.gamma, v * by + lane * PER, n, 1.0f);
+        beta[v].load(A.beta, v * by + lane * PER, n, 0.0f);
+    }
+    for (; row < A.rows; row += 2 * step) {
+        if (row + step < A.rows) fetch(row + step, 1);
+        work(row, 0);
+        if (row + step >= A.rows) break;
+        if (row + 2 * step < A.rows) fetch(row + 2 * step, 0);
+        work(row + step, 1);
     }
 }
 
@@ -237,54 +373,88 @@ struct NormGradArgs {
     const void *gamma;
     const float *stats;
     float *partials;          // [workgroup][2][cols], or null
+    bool through;
 };
-// Rows dealt in turn to the workgroups' teams, which add up dy xhat and dy of their own rows for each column; a workgroup's teams join theirs in LDS.
-template <typename E, typename W, int TEAM, int NV>
+// Rows dealt in turn to the workgroups' teams, which add up dy xhat and dy of their own rows for each column; a workgroup's teams join theirs in LDS.  The next
+// row is on its way while one is worked on, unless the registers of 1024 lanes have no room for it.
+template <typename E, typename W, int TEAM, int NV, bool WHOLE>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormGradArgs A)
 {
-    constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM, PER = E::PER, NW = TEAM / 64;
+    constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM, PER = E::PER, NW = TEAM / 64, BUFFERS = TEAM * NV > 1024 ? 1 : 2;
     __shared__ float lds[2][2 * NW];
     __shared__ float joint[TEAMS > 1 ? TEAMS * TEAM * NV * PER : 1];
     const int team = TEAMS > 1 ? threadIdx.x / TEAM : 0, lane = TEAMS > 1 ? threadIdx.x % TEAM : threadIdx.x;
-    const int64_t n = A.cols, by = (int64_t)TEAM * PER;
-    float gamma[NV][PER], dgamma[NV][PER], dbeta[NV][PER];
+    const int64_t n = A.cols, by = (int64_t)TEAM * PER, step = (int64_t)gridDim.x * TEAMS;
+    Weights<W, PER, WHOLE> gamma[NV];
+    float dgamma[NV][PER], dbeta[NV][PER];
+    u32x4 x[BUFFERS][NV], dy[BUFFERS][NV];
+    float2 stats[BUFFERS];
+    auto fetch = [&](int64_t row, int to) {
+        const typename E::T *xr = static_cast<const typename E::T *>(A.x) + row * A.stride, *dr = static_cast<const typename E::T *>(A.dy) + row * A.dy_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            x[to][v] = load_some<E, true, WHOLE>(xr, v * by + lane * PER, n);
+            dy[to][v] = load_some<E, true, WHOLE>(dr, v * by + lane * PER, n);
+        }
+        stats[to] = float2{A.stats[2 * row], A.stats[2 * row + 1]};
+    };
+    int turn = 0;
+    auto work = [&](int64_t row, int at) {
+        const float mean = stats[at].x, rstd = stats[at].y;
+        float z[PER], d[PER], g[PER], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            E::widen(x[at][v], z);
+            E::widen(dy[at][v], d);
+            gamma[v].get(g);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                z[i] = (z[i] - mean) * rstd;                 // behind the row d is 0
+                dgamma[v][i] += d[i] * z[i];
+                dbeta[v][i] += d[i];
+                d[i] *= g[i];
+                sum[0] += d[i];
+                sum[1] += d[i] * z[i];
+            }
+            if (BUFFERS == 1) __builtin_amdgcn_sched_barrier(0);       // one vector's widened values at a time
+        }
+        team_sums<TEAM>(sum, lds[turn]);
+        turn ^= 1;
+        const float a = sum[0] / (float)n, b = sum[1] / (float)n;
+        typename E::T *dx = static_cast<typename E::T *>(A.dx) + row * A.dx_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            as_it_came(x[at][v]);
+            as_it_came(dy[at][v]);
+#pragma unroll
+            for (int i = 0; i < gamma[v].N; ++i) as_it_came(gamma[v].q[i]);
+            E::widen(x[at][v], z);
+            E::widen(dy[at][v], d);
+            gamma[v].get(g);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) d[i] = rstd * (d[i] * g[i] - a - (z[i] - mean) * rstd * b);
+            if (v * by + lane * PER < n) store_some<E, WHOLE>(dx, v * by + lane * PER, n, d, A.through);
+            if (BUFFERS == 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * TEAMS + team;
+    if (row < A.rows) fetch(row, 0);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_weights<W, PER>(A.gamma, v * by + lane * PER, n, 1.0f, gamma[v]);
+        gamma[v].load(A.gamma, v * by + lane * PER, n, 1.0f);
 #pragma unroll
         for (int i = 0; i < PER; ++i) dgamma[v][i] = dbeta[v][i] = 0.0f;
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < A.rows; row += (int64_t)gridDim.x * TEAMS, turn ^= 1) {
-        const typename E::T *x = static_cast<const typename E::T *>(A.x) + row * A.stride;
-        const typename E::T *dy = static_cast<const typename E::T *>(A.dy) + row * A.dy_stride;
-        typename E::T *dx = static_cast<typename E::T *>(A.dx) + row * A.dx_stride;
-        const float mean = A.stats[2 * row], rstd = A.stats[2 * row + 1];
-        float z[NV][PER], d[NV][PER], sum[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            load_some<E>(x, v * by + lane * PER, n, z[v]);
-            load_some<E>(dy, v * by + lane * PER, n, d[v]);
-        }
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                z[v][i] = (z[v][i] - mean) * rstd;                 // behind the row d is 0
-                dgamma[v][i] += d[v][i] * z[v][i];
-                dbeta[v][i] += d[v][i];
-                d[v][i] *= gamma[v][i];
-                sum[0] += d[v][i];
-                sum[1] += d[v][i] * z[v][i];
-            }
-        team_sums<TEAM>(sum, lds[turn]);
-        const float a = sum[0] / (float)n, b = sum[1] / (float)n;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) d[v][i] = rstd * (d[v][i] - a - z[v][i] * b);
-            if (v * by + lane * PER < n) store_some<E>(dx, v * by + lane * PER, n, d[v]);
-        }
+    for (; BUFFERS == 1 && row < A.rows; row += step) {
+        work(row, 0);
+        if (row + step < A.rows) fetch(row + step, 0);
+    }
+    for (; row < A.rows; row += 2 * step) {
+        if (row + step < A.rows) fetch(row + step, BUFFERS - 1);
+        work(row, 0);
+        if (row + step >= A.rows) break;
+        if (row + 2 * step < A.rows) fetch(row + 2 * step, 0);
+        work(row + step, BUFFERS - 1);
     }
     if (!A.partials) return;
     float *out = A.partials + (int64_t)blockIdx.x * 2 * n;
@@ -294,8 +464,18 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormGradA
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (v * by + lane * PER + i < n) out[v * by + lane * PER + i] = q ? dbeta[v][i] : dgamma[v][i];
+                for (int h = 0; h < PER; h += 4) {
+                    const float *f = (q ? dbeta[v] : dgamma[v]) + h;
+                    const float four[4] = {f[0], f[1], f[2], f[3]};
+                    const int64_t c = v * by + lane * PER + h;
+                    if (WHOLE ? c < n : c + 4 <= n) {
+                        *reinterpret_cast<Loose<4>::T *>(out + c) = F32::narrow(four);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (c + i < n) out[c + i] = four[i];
+                    }
+                }
         } else {
             __syncthreads();
 #pragma unroll
@@ -323,10 +503,12 @@ __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs A)
     typename E::T *dx = static_cast<typename E::T *>(A.dx) + row * A.dx_stride;
     const float mean = A.stats[2 * row], rstd = A.stats[2 * row + 1];
     float z[PER], d[PER], g[PER], sum[2] = {0.0f, 0.0f};
+    Weights<W, PER> gamma;
     for (int64_t c = threadIdx.x * PER; c < n; c += 1024 * PER) {
-        load_some<E>(x, c, n, z);
-        load_some<E>(dy, c, n, d);
-        load_weights<W, PER>(A.gamma, c, n, 1.0f, g);
+        E::widen(load_some<E, false>(x, c, n), z);
+        E::widen(load_some<E, false>(dy, c, n), d);
+        gamma.load(A.gamma, c, n, 1.0f);
+        gamma.get(g);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             d[i] *= g[i];
@@ -337,12 +519,13 @@ __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs A)
     team_sums<1024>(sum, lds);
     const float a = sum[0] / (float)n, b = sum[1] / (float)n;
     for (int64_t c = threadIdx.x * PER; c < n; c += 1024 * PER) {
-        load_some<E>(x, c, n, z);
-        load_some<E>(dy, c, n, d);
-        load_weights<W, PER>(A.gamma, c, n, 1.0f, g);
+        E::widen(load_some<E, false>(x, c, n), z);
+        E::widen(load_some<E, false>(dy, c, n), d);
+        gamma.load(A.gamma, c, n, 1.0f);
+        gamma.get(g);
 #pragma unroll
         for (int i = 0; i < PER; ++i) d[i] = rstd * (d[i] * g[i] - a - (z[i] - mean) * rstd * b);
-        store_some<E>(dx, c, n, d);
+        store_some<E>(dx, c, n, d, A.through);
     }
 }
 // and the columns' sums by themselves (before, since dx may lie where dy does): a lane PER columns, a workgroup a share of the rows
@@ -356,8 +539,8 @@ __global__ __launch_bounds__(256) void k_norm_columns(NormGradArgs A, int64_t pe
     float dgamma[PER] = {}, dbeta[PER] = {};
     for (int64_t row = from; row < to; ++row) {
         float z[PER], d[PER];
-        load_some<E>(static_cast<const typename E::T *>(A.x) + row * A.stride, c, n, z);
-        load_some<E>(static_cast<const typename E::T *>(A.dy) + row * A.dy_stride, c, n, d);
+        E::widen(load_some<E, false>(static_cast<const typename E::T *>(A.x) + row * A.stride, c, n), z);
+        E::widen(load_some<E, false>(static_cast<const typename E::T *>(A.dy) + row * A.dy_stride, c, n), d);
         const float mean = A.stats[2 * row], rstd = A.stats[2 * row + 1];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -378,12 +561,15 @@ __global__ __launch_bounds__(1024) void k_norm_fold(const float *partials, int p
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
     double s = 0.0;
-    if (c < 2 * cols)
+    if (c < 2 * cols) {
+#pragma unroll 8
         for (int i = wave; i < parts; i += 16) s += (double)partials[(int64_t)i * 2 * cols + c];
+    }
     part[wave][lane] = s;
     __syncthreads();
     if (wave != 0 || c >= 2 * cols) return;
     s = 0.0;
+#pragma unroll
     for (int i = 0; i < 16; ++i) s += part[i][lane];
     W::store(static_cast<typename W::T *>(c < cols ? dgamma : dbeta) + (c < cols ? c : c - cols), (float)s);
 }
@@ -404,70 +590,68 @@ struct DropoutArgs {
     const void *x, *residual;
     void *out;
     int64_t n;
-    uint64_t offset, blocks;      // blocks of 8 elements by their numbers, the first and last perhaps in part
+    uint64_t offset, vectors;     // vectors by their first elements' numbers, the first and last perhaps in part
     uint32_t least;               // T
     float scale;                  // 1 / (1 - P)
     uint32_t k0, k1;
     const uint64_t *step;
+    bool through;
 };
 constexpr int DROP_BLOCK = 256;
-// Eight elements a lane: one block of the generator.
+// A vector a lane: a block of the generator for eight bf16, half of one for four fp32 (two lanes make the same block, which costs less than accesses of half
+// lines: 4095 x 5003 with a residual 40 us against 50).
 template <typename E, bool RESIDUAL>
 __global__ __launch_bounds__(DROP_BLOCK) void k_dropout(DropoutArgs A)
 {
-    constexpr int V = 8 / E::PER;
-    const uint64_t b = (uint64_t)blockIdx.x * DROP_BLOCK + threadIdx.x;
-    if (b >= A.blocks) return;
-    const uint64_t number = (A.offset >> 3) + b;
-    const int64_t at = (int64_t)(b * 8) - (int64_t)(A.offset & 7);       // of its first element, which may lie before the array
+    constexpr int PER = E::PER;
+    const uint64_t u = (uint64_t)blockIdx.x * DROP_BLOCK + threadIdx.x;
+    if (u >= A.vectors) return;
+    const uint64_t number = A.offset / PER + u;
+    const int64_t at = (int64_t)(u * PER) - (int64_t)(A.offset % PER);       // of its first element, which may lie before the array
     const typename E::T *x = static_cast<const typename E::T *>(A.x), *res = static_cast<const typename E::T *>(A.residual);
     typename E::T *out = static_cast<typename E::T *>(A.out);
-    const bool whole = at >= 0 && at + 8 <= A.n;
-    float z[V][E::PER], r[V][E::PER];
+    const bool whole = at >= 0 && at + PER <= A.n;
+    float z[PER], r[PER];
+    if (whole) {
+        E::widen(load_once<E>(x + at), z);
+        if (RESIDUAL) E::widen(load_once<E>(res + at), r);
+    } else {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        if (whole) {
-            E::widen(load_vector<E>(x + at + v * E::PER), z[v]);
-            if (RESIDUAL) E::widen(load_vector<E>(res + at + v * E::PER), r[v]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E::PER; ++i) {
-                const int64_t e = at + v * E::PER + i;
-                const bool there = e >= 0 && e < A.n;
-                z[v][i] = there ? E::load(x + e) : 0.0f;
-                r[v][i] = RESIDUAL && there ? E::load(res + e) : 0.0f;
-            }
+        for (int i = 0; i < PER; ++i) {
+            const int64_t e = at + i;
+            const bool there = e >= 0 && e < A.n;
+            z[i] = there ? E::load(x + e) : 0.0f;
+            r[i] = RESIDUAL && there ? E::load(res + e) : 0.0f;
         }
     }
-    const uint64_t step = A.step ? *A.step : 0;
-    uint32_t c[4] = {(uint32_t)number, (uint32_t)(number >> 32), (uint32_t)step, (uint32_t)(step >> 32)};
+    const uint64_t step = A.step ? *A.step : 0, block = number * PER / 8;
+    uint32_t c[4] = {(uint32_t)block, (uint32_t)(block >> 32), (uint32_t)step, (uint32_t)(step >> 32)};
     philox(c, A.k0, A.k1);
+    if (PER == 4 && (number & 1)) c[0] = c[2], c[1] = c[3];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t bits = i & 1 ? c[i >> 1] >> 16 : c[i >> 1] & 0xffffu;
+        z[i] = bits >= A.least ? z[i] * A.scale : 0.0f;
+        if (RESIDUAL) z[i] += r[i];
+    }
+    if (whole) {
+        store_vector<E>(out + at, E::narrow(z), A.through);
+    } else {
 #pragma unroll
-        for (int i = 0; i < E::PER; ++i) {
-            const int e = v * E::PER + i;
-            const uint32_t bits = e & 1 ? c[e >> 1] >> 16 : c[e >> 1] & 0xffffu;
-            z[v][i] = bits >= A.least ? z[v][i] * A.scale : 0.0f;
-            if (RESIDUAL) z[v][i] += r[v][i];
-        }
-        if (whole) {
-            *reinterpret_cast<typename Loose<sizeof(typename E::T)>::T *>(out + at + v * E::PER) = E::narrow(z[v]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E::PER; ++i) {
-                const int64_t e = at + v * E::PER + i;
-                if (e >= 0 && e < A.n) E::store(out + e, z[v][i]);
-            }
+        for (int i = 0; i < PER; ++i) {
+            const int64_t e = at + i;
+            if (e >= 0 && e < A.n) E::store(out + e, z[i]);
         }
     }
 }
 
 // ---- launches ------------------------------------------------------------------------------------
 constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
+constexpr int64_t NORM_FEW = 512;                // rows up to which a row's own time counts
+constexpr int64_t NORM_LANES = 256 * 1024;      // of workgroups that stay
 constexpr int NORM_PARTS = 512;                  // workgroups of a gradient, and partials of its columns
 
-template <typename E, typename W, int TEAM, int NV, bool HELD>
+template <typename E, typename W, int TEAM, int NV, bool HELD, bool EARLY>
 static hipError_t launch_norm_as(const NormArgs &A, hipStream_t stream)
 {
     constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM;
@@ -478,23 +662,36 @@ static hipError_t launch_norm_as(const NormArgs &A, hipStream_t stream)
         B.y = static_cast<typename E::T *>(A.y) + r * A.y_stride;
         B.stats = A.stats ? A.stats + 2 * r : nullptr;
         B.rows = std::min(most, A.rows - r);
-        k_norm<E, W, TEAM, NV, HELD><<<(uint32_t)((B.rows + TEAMS - 1) / TEAMS), BLOCK, 0, stream>>>(B);
+        k_norm<E, W, TEAM, NV, HELD, EARLY><<<(uint32_t)((B.rows + TEAMS - 1) / TEAMS), BLOCK, 0, stream>>>(B);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+template <typename E, typename W, int TEAM, int NV>
+static hipError_t launch_norm_many(const NormArgs &A, hipStream_t stream)
+{
+    constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM;
+    const uint32_t grid = (uint32_t)std::min<int64_t>(NORM_LANES / BLOCK, (A.rows + TEAMS - 1) / TEAMS);
+    if (A.cols % E::PER == 0) k_norm_many<E, W, TEAM, NV, true><<<grid, BLOCK, 0, stream>>>(A);
+    else k_norm_many<E, W, TEAM, NV, false><<<grid, BLOCK, 0, stream>>>(A);
+    return hipGetLastError();
 }
 template <typename E, typename W>
 static hipError_t launch_norm(const NormArgs &A, hipStream_t stream)
 {
     const int64_t v = (A.cols + E::PER - 1) / E::PER;
-    if (v <= 64) return launch_norm_as<E, W, 64, 1, true>(A, stream);
-    if (v <= 128) return launch_norm_as<E, W, 64, 2, true>(A, stream);
-    if (v <= 256) return launch_norm_as<E, W, 64, 4, true>(A, stream);
-    if (v <= 512) return launch_norm_as<E, W, 256, 2, true>(A, stream);
-    if (v <= 1024) return launch_norm_as<E, W, 256, 4, true>(A, stream);
-    if (v <= 2048) return launch_norm_as<E, W, 1024, 2, true>(A, stream);
-    if (v <= 4096) return launch_norm_as<E, W, 1024, 4, true>(A, stream);
-    return launch_norm_as<E, W, 1024, 1, false>(A, stream);
+    if (v <= 64) return launch_norm_as<E, W, 64, 1, true, true>(A, stream);
+    if (A.rows <= NORM_FEW && v <= 1024) {
+        if (v <= 256) return launch_norm_as<E, W, 256, 1, true, true>(A, stream);
+        return launch_norm_as<E, W, 1024, 1, true, true>(A, stream);
+    }
+    if (v <= 128) return launch_norm_many<E, W, 64, 2>(A, stream);
+    if (v <= 256) return launch_norm_many<E, W, 256, 1>(A, stream);
+    if (v <= 512) return launch_norm_many<E, W, 256, 2>(A, stream);
+    if (v <= 1024) return launch_norm_many<E, W, 512, 2>(A, stream);
+    if (v <= 2048) return launch_norm_as<E, W, 1024, 2, true, false>(A, stream);
+    if (v <= 4096) return launch_norm_as<E, W, 1024, 4, true, false>(A, stream);
+    return launch_norm_as<E, W, 1024, 1, false, false>(A, stream);
 }
 
 // Workgroups of a gradient over rows that are held: all that fit the chip at once, two a CU.
@@ -502,8 +699,10 @@ template <typename E, typename W, int TEAM, int NV>
 static hipError_t launch_norm_grad_as(const NormGradArgs &A, int &parts, hipStream_t stream)
 {
     constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM;
-    parts = (int)std::min<int64_t>(NORM_PARTS, (A.rows + TEAMS - 1) / TEAMS);
-    k_norm_grad<E, W, TEAM, NV><<<parts, BLOCK, 0, stream>>>(A);
+    parts = (int)std::min<int64_t>(BLOCK == 1024 ? NORM_PARTS / 2 : NORM_PARTS, (A.rows + TEAMS - 1) / TEAMS);
+    if constexpr (TEAM * NV > 1024) k_norm_grad<E, W, TEAM, NV, true><<<parts, BLOCK, 0, stream>>>(A);
+    else if (A.cols % E::PER == 0) k_norm_grad<E, W, TEAM, NV, true><<<parts, BLOCK, 0, stream>>>(A);
+    else k_norm_grad<E, W, TEAM, NV, false><<<parts, BLOCK, 0, stream>>>(A);
     return hipGetLastError();
 }
 template <typename E, typename W>
@@ -516,9 +715,9 @@ static hipError_t launch_norm_grad(const NormGradArgs &A, void *dgamma, void *db
     } else if (v <= 64) e = launch_norm_grad_as<E, W, 64, 1>(A, parts, stream);
     else if (v <= 128) e = launch_norm_grad_as<E, W, 64, 2>(A, parts, stream);
     else if (v <= 256) e = launch_norm_grad_as<E, W, 256, 1>(A, parts, stream);
-    else if (v <= 512) e = launch_norm_grad_as<E, W, 256, 2>(A, parts, stream);
-    else if (v <= 1024) e = launch_norm_grad_as<E, W, 256, 4>(A, parts, stream);
-    else if (v <= 2048) e = launch_norm_grad_as<E, W, 1024, 2>(A, parts, stream);
+    else if (v <= 512) e = launch_norm_grad_as<E, W, 512, 1>(A, parts, stream);
+    else if (v <= 1024) e = launch_norm_grad_as<E, W, 1024, 1>(A, parts, stream);
+    else if (v <= 2048 && A.cols % E::PER == 0) e = launch_norm_grad_as<E, W, 1024, 2>(A, parts, stream);      // 1024 lanes have no registers for cut vectors
     else {
         if (A.partials) {
             const int64_t blocks = (v + 255) / 256, wanted = std::min<int64_t>(NORM_PARTS, std::max<int64_t>(1, 2048 / blocks)), per = (A.rows + wanted - 1) / wanted;
@@ -543,23 +742,23 @@ static hipError_t launch_norm_grad(const NormGradArgs &A, void *dgamma, void *db
 }
 
 template <typename E>
-static hipError_t launch_dropout(const DropoutArgs &A, hipStream_t stream)
+static hipError_t launch_dropout(DropoutArgs A, hipStream_t stream)
 {
-    const int64_t most = kMaxItems / DROP_BLOCK * DROP_BLOCK;       // blocks of a launch
-    DropoutArgs B = A;
-    for (uint64_t done = 0; done < A.blocks; done += most) {
-        B.blocks = std::min<uint64_t>(most, A.blocks - done);
-        const uint32_t grid = (uint32_t)((B.blocks + DROP_BLOCK - 1) / DROP_BLOCK);
-        if (A.residual) k_dropout<E, true><<<grid, DROP_BLOCK, 0, stream>>>(B);
-        else k_dropout<E, false><<<grid, DROP_BLOCK, 0, stream>>>(B);
+    const int64_t most = kMaxItems / DROP_BLOCK * DROP_BLOCK, size = sizeof(typename E::T);       // vectors of a launch
+    A.through = whole_lines(static_cast<char *>(A.out) - A.offset % E::PER * size, 0);
+    for (uint64_t left = (A.offset % E::PER + (uint64_t)A.n + E::PER - 1) / E::PER; left; left -= A.vectors) {
+        A.vectors = std::min<uint64_t>(most, left);
+        const uint32_t grid = (uint32_t)((A.vectors + DROP_BLOCK - 1) / DROP_BLOCK);
+        if (A.residual) k_dropout<E, true><<<grid, DROP_BLOCK, 0, stream>>>(A);
+        else k_dropout<E, false><<<grid, DROP_BLOCK, 0, stream>>>(A);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        // the next launch's first block begins with the next element
-        const int64_t elements = most * 8 - (int64_t)(B.offset & 7);
-        B.x = static_cast<const typename E::T *>(B.x) + elements;
-        if (B.residual) B.residual = static_cast<const typename E::T *>(B.residual) + elements;
-        B.out = static_cast<typename E::T *>(B.out) + elements;
-        B.n -= elements;
-        B.offset += elements;
+        // the next launch's first vector begins with the next element
+        const int64_t elements = (int64_t)(A.vectors * E::PER - A.offset % E::PER);
+        A.x = static_cast<const typename E::T *>(A.x) + elements;
+        if (A.residual) A.residual = static_cast<const typename E::T *>(A.residual) + elements;
+        A.out = static_cast<typename E::T *>(A.out) + elements;
+        A.n -= elements;
+        A.offset += elements;
     }
     return hipSuccess;
 }
@@ -615,7 +814,8 @@ gs_status gs_layer_norm(const gs_matrix *x, const void *gamma, const void *beta,
     const Range s[] = {matrix_range(*x, x->data, x->row_stride, false), matrix_range(*x, y, y_stride, true), range_of(gamma, x->cols * wsize, false),
                        range_of(beta, x->cols * wsize, false), range_of(row_stats, x->rows * 8, true)};
     if (!apart(s, 5, same(*x, x->data, x->row_stride, y, y_stride), 0, 1)) return GS_ERR_INVALID_ARG;
-    const NormArgs A = {x->data, x->rows, x->cols, x->rows > 1 ? x->row_stride : x->cols, gamma, beta, eps, y, x->rows > 1 ? y_stride : x->cols, row_stats};
+    const NormArgs A = {x->data, x->rows, x->cols, x->rows > 1 ? x->row_stride : x->cols, gamma, beta, eps, y, x->rows > 1 ? y_stride : x->cols, row_stats,
+                        whole_lines(y, (x->rows > 1 ? y_stride : 0) * size_of(x->dtype))};
     hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = by_types(x->dtype, weight_dtype, [&](auto t, auto w) { return launch_norm<decltype(t), decltype(w)>(A, st); });
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_layer_norm launch");
@@ -643,7 +843,7 @@ gs_status gs_layer_norm_grad(const gs_matrix *x, const void *gamma, int32_t weig
     if (!apart(s, 8, x->rows && same(*x, dy, dy_stride, dx, dx_stride), 0, 1)) return GS_ERR_INVALID_ARG;
     const bool many = x->rows > 1;
     const NormGradArgs A = {x->data, dy, dx, x->rows, x->cols, many ? x->row_stride : x->cols, many ? dy_stride : x->cols, many ? dx_stride : x->cols,
-                            gamma, row_stats, dgamma ? static_cast<float *>(d_workspace) : nullptr};
+                            gamma, row_stats, dgamma ? static_cast<float *>(d_workspace) : nullptr, whole_lines(dx, (many ? dx_stride : 0) * size_of(x->dtype))};
     hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = by_types(x->dtype, weight_dtype, [&](auto t, auto w) { return launch_norm_grad<decltype(t), decltype(w)>(A, dgamma, dbeta, st); });
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_layer_norm_grad launch");
@@ -666,7 +866,6 @@ gs_status gs_dropout(const void *x, const void *residual, void *out, int64_t n, 
     A.out = out;
     A.n = n;
     A.offset = offset;
-    A.blocks = ((offset & 7) + (uint64_t)n + 7) / 8;
     A.least = (uint32_t)std::lround((double)p * 65536.0);
     A.scale = A.least < 65536 ? (float)(65536.0 / (65536.0 - A.least)) : 0.0f;
     A.k0 = (uint32_t)seed;

@@ -293,6 +293,10 @@ _call.setup_loss(*[ctypes.cast(getattr(_lib, name), _vp).value for name in (
     PolicyHParams, PreferenceHParams)
 
 
+_call.setup_layers(*[ctypes.cast(getattr(_lib, name), _vp).value for name in (
+    "gs_head_logp", "gs_head_logp_grad", "gs_head_cross_entropy", "gs_layer_norm", "gs_layer_norm_grad", "gs_dropout")])
+
+
 def _hp(hp):
     if hp is None:
         return None
@@ -689,6 +693,9 @@ def _head_grads(h: gs_head, dx, dw, dbias) -> gs_head_grads:
 def gs_head_logp(x, w, bias, targets, logp, row_stats=None, temperature: float = 1.0, d_workspace=None,
                  workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
     """x: hidden states (rows, hidden); w: (vocab, hidden); bias: (vocab,) or None."""
+    st = _call.head_logp(x, w, bias, targets, logp, row_stats, temperature, d_workspace, workspace_bytes, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_head_logp", check)
     h = _head(x, w, bias)
     _on_current(x, w, bias, targets, logp, row_stats, d_workspace)
     st = _lib.gs_head_logp(ctypes.byref(h), _gpu(targets, h.rows, torch.int64, "targets"), temperature, _gpu(logp, h.rows, torch.float32, "logp"),
@@ -699,6 +706,9 @@ def gs_head_logp(x, w, bias, targets, logp, row_stats=None, temperature: float =
 
 def gs_head_logp_grad(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace, temperature: float = 1.0,
                       workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
+    st = _call.head_logp_grad(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace, temperature, workspace_bytes, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_head_logp_grad", check)
     h = _head(x, w, bias)
     _on_current(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_workspace)
     g = _head_grads(h, dx, dw, dbias)
@@ -711,6 +721,9 @@ def gs_head_logp_grad(x, w, bias, targets, row_stats, dlogp, dx, dw, dbias, d_wo
 def gs_head_cross_entropy(x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace, temperature: float = 1.0,
                           accumulate: bool = False, workspace_bytes: int | None = None, stream=None, check: bool = True) -> int:
     """With dx, dw and dbias all None there is no gradient, and less workspace is needed."""
+    st = _call.head_cross_entropy(x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace, temperature, accumulate, workspace_bytes, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_head_cross_entropy", check)
     h = _head(x, w, bias)
     _on_current(x, w, bias, targets, weights, logp, dx, dw, dbias, d_loss, d_workspace)
     g = None if dx is None and dw is None and dbias is None else _head_grads(h, dx, dw, dbias)
@@ -733,6 +746,9 @@ def _norm_weights(cols: int, **weights):
 
 def gs_layer_norm(x, gamma, beta, y, row_stats=None, eps: float = 1e-5, stream=None, check: bool = True) -> int:
     """x, y: (rows, cols), bfloat16 or float32; gamma, beta: (cols,), of a type of their own, or None."""
+    st = _call.layer_norm(x, gamma, beta, y, row_stats, eps, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_layer_norm", check)
     xp, rows, cols, xs = _rows_of(x, "x", tuple(_DTYPES))
     yp, ys = _rows_like(y, "y", (rows, cols), x.dtype)
     (g, b), wt = _norm_weights(cols, gamma=gamma, beta=beta)
@@ -749,6 +765,9 @@ def gs_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
 def gs_layer_norm_grad(dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace=None, workspace_bytes: int | None = None, stream=None,
                        check: bool = True) -> int:
     """dgamma and dbeta may both be None; then no workspace is needed."""
+    st = _call.layer_norm_grad(dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace, workspace_bytes, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_layer_norm_grad", check)
     xp, rows, cols, xs = _rows_of(x, "x", tuple(_DTYPES))
     dyp, dys = _rows_like(dy, "dy", (rows, cols), x.dtype)
     dxp, dxs = _rows_like(dx, "dx", (rows, cols), x.dtype)
@@ -762,6 +781,9 @@ def gs_layer_norm_grad(dy, x, gamma, row_stats, dx, dgamma, dbeta, d_workspace=N
 
 def gs_dropout(x, residual, out, p: float, seed: int, offset: int = 0, d_step=None, stream=None, check: bool = True) -> int:
     """Contiguous tensors of one type and size; residual may be None.  d_step: an int64 GPU tensor, or None."""
+    st = _call.dropout(x, residual, out, p, seed, offset, d_step, stream)
+    if st is not None:
+        return st if st == GS_OK else _check(st, "gs_dropout", check)
     if not isinstance(x, torch.Tensor) or x.dtype not in _DTYPES:
         raise TypeError("x: a bfloat16 or float32 tensor is needed")
     n = x.numel()

@@ -314,6 +314,23 @@ def test_preference_loss_without_logits():
     check({"dx": c.dx, "dw": c.dw, "db": c.db}, out, bound, ["dx", "dw", "db"])
 
 
+def test_native_and_general_reading_agree():
+    """A raw stream and workspace bytes by name are read natively too, a NumPy-like temperature or a raw address is not: the same results."""
+    c = Case(70, 64, 300, bias=True, prompt=True)
+    want = {k: v.clone() for k, v in c.cross_entropy().items()}
+    ws = c.workspace()
+    for t in (c.logp, c.dx, c.dw, c.db):
+        t.fill_(8.0)
+    gs.gs_head_cross_entropy(c.x, c.w, c.bias, c.targets, c.weights, c.logp, c.dx, c.dw, c.db, c.loss, ws.data_ptr(), 1, workspace_bytes=ws.numel(),
+                             stream=torch.cuda.current_stream().cuda_stream)
+    for k, v in {"logp": c.logp, "dx": c.dx, "dw": c.dw, "db": c.db}.items():
+        assert torch.equal(v, want[k]), k
+    c.score(0.5)
+    one = c.logp.clone(), c.stats.clone()
+    gs.gs_head_logp(c.x, c.w, c.bias, c.targets, c.logp.fill_(0), c.stats, 0.5, ws.data_ptr(), workspace_bytes=ws.numel())
+    assert torch.equal(c.logp, one[0]) and torch.equal(c.stats, one[1])
+
+
 def test_binding_refuses():
     c = Case(10, 64, 100)
     ws = c.workspace()

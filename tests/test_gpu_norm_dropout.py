@@ -331,6 +331,25 @@ def test_dropout_beyond_32_bits_of_offsets():
     assert torch.equal(x[-1000:], tail)
 
 
+def test_native_and_general_reading_agree():
+    x, gamma, beta, y, stats, dy, dx, dgamma, dbeta, ws = run_norm(9, 300, F32, BF16)
+    want = [t.clone() for t in (y, stats, dx, dgamma, dbeta)]
+    for t in (y, stats, dx, dgamma, dbeta):
+        t.fill_(3.0)
+
+    class Stream:
+        cuda_stream = torch.cuda.current_stream().cuda_stream
+
+    gs.gs_layer_norm(torch.nn.Parameter(x, requires_grad=False), gamma, beta, y, stats, np.float64(1e-5), stream=Stream())
+    gs.gs_layer_norm_grad(dy, x, gamma, stats, dx, dgamma, dbeta, ws.data_ptr(), ws.numel())
+    for t, w in zip((y, stats, dx, dgamma, dbeta), want):
+        assert torch.equal(t, w)
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    gs.gs_dropout(x, None, a, 0.5, (1 << 64) - 5, 3)
+    gs.gs_dropout(x, None, b, np.float64(0.5), (1 << 64) - 5, 3)
+    assert torch.equal(a, b) and bool((a == 0).any())
+
+
 def test_binding_refuses():
     x = torch.zeros(4, 64, dtype=BF16, device=DEV)
     w = torch.zeros(64, device=DEV)
