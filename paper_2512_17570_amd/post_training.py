@@ -8,6 +8,8 @@ The model is a linear head: logits = x W^T + b over hidden states x that are giv
   * gs_grads_sqnorm takes the norm of all sums together, gs_grads_clip scales them, gs_adamw_from_acc steps each tensor.
 Nothing in a step waits for the GPU.  PyTorch supplies memory and the head's products.
 
+The same without logits, and with what lies in front of the head: fine_tuning.py.
+
     python -m paper_2512_17570_amd.post_training
 """
 from __future__ import annotations
@@ -43,6 +45,7 @@ class Head:
         self.sq = torch.zeros(1, dtype=torch.float64, device=DEV)
         self.norm = torch.zeros(1, device=DEV)
         self.workspace = torch.empty(gs.gs_sqnorm_workspace_bytes(), dtype=torch.uint8, device=DEV)
+        self.head_workspace = None
         self.step = 0
 
     def logits(self, x):
@@ -52,8 +55,18 @@ class Head:
         for par, g in ((self.weight, dlogits.t() @ x), (self.bias, dlogits.sum(0))):
             gs.gs_accum_add(par.acc, g.reshape(-1), first, 0, par.acc.numel())
 
+    def parameters(self):
+        return [self.weight, self.bias]
+
+    def room(self, rows: int):
+        """Workspace of the head's calls without logits, kept for the largest batch so far."""
+        need = gs.gs_head_workspace_bytes(rows, self.weight.w.size(1), self.weight.w.size(0))
+        if self.head_workspace is None or self.head_workspace.numel() < need:
+            self.head_workspace = torch.empty(need, dtype=torch.uint8, device=DEV)
+        return self.head_workspace
+
     def update(self, lr: float, max_norm: float):
-        pars = [self.weight, self.bias]
+        pars = self.parameters()
         self.step += 1
         hp = gs.HParams(lr=lr, weight_decay=0.0, max_grad_norm=0.0, step=self.step)      # clipped before
         gs.gs_grads_sqnorm([q.acc for q in pars], self.sq, self.workspace)
