@@ -315,14 +315,11 @@ __global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets
     if (threadIdx.x == 0) *L.count = before;
 }
 
-// Row j of `to` (stride `width`, a multiple of 8): row index[j] of `from` (row j without an index), zeros behind its `cols` elements and in rows from count on.
+// Elements of a row, and zeros up to `width` (a multiple of 8); `there`: whether there is such a row.
 template <bool WIDE>
-__global__ __launch_bounds__(256) void k_head_pack(const uint16_t *from, int64_t stride, int64_t cols, const Live L, int64_t rows, uint16_t *to, int64_t width)
+__device__ __forceinline__ void copy_row(const uint16_t *f, int64_t cols, bool there, uint16_t *to, int64_t width)
 {
-    const int64_t j = blockIdx.x;
-    const bool there = L.count ? j < *L.count : j < rows;
-    const uint16_t *f = from + (there ? (L.index ? (int64_t)L.index[j] : j) : 0) * stride;
-    u32x4 *t = reinterpret_cast<u32x4 *>(to + j * width);
+    u32x4 *t = reinterpret_cast<u32x4 *>(to);
     for (int64_t c = threadIdx.x; c < width / 8; c += 256) {
         u32x4 q = {};
         if (there) {
@@ -337,6 +334,63 @@ __global__ __launch_bounds__(256) void k_head_pack(const uint16_t *from, int64_t
         }
         t[c] = q;
     }
+}
+// Row j of `to` (stride `width`, a multiple of 8): row index[j] of `from` (row j without an index), zeros behind its `cols` elements and in rows from count on.
+template <bool WIDE>
+__global__ __launch_bounds__(256) void k_head_pack(const uint16_t *from, int64_t stride, int64_t cols, const Live L, int64_t rows, uint16_t *to, int64_t width)
+{
+    const int64_t j = blockIdx.x;
+    const bool there = L.count ? j < *L.count : j < rows;
+    copy_row<WIDE>(from + (there ? (L.index ? (int64_t)L.index[j] : j) : 0) * stride, cols, there, to + j * width, width);
+}
+// Both for up to GATHER_MAX rows, in one launch: every workgroup counts the rows that count by itself, which is less than another launch takes.
+constexpr int GATHER_MAX = 1024;
+template <bool WIDE>
+__global__ __launch_bounds__(256) void k_head_gather(const int64_t *targets, const float *factor, int rows, int vocab, Live L, float *logp, float *row_stats,
+                                                     const uint16_t *from, int64_t stride, int64_t cols, uint16_t *to, int64_t width)
+{
+    __shared__ int waves[4], found;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = blockIdx.x;
+    constexpr int EACH = GATHER_MAX / 256;
+    uint64_t masks[EACH];
+    int before = 0;
+    if (threadIdx.x == 0) found = -1;
+    // wave w has rows [256 w, 256 w + 256), 64 at a time
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+        const int r = wave * (64 * EACH) + q * 64 + lane;
+        bool live = false;
+        if (r < rows) {
+            const int64_t t = targets[r];
+            live = t >= 0 && t < vocab && (!factor || factor[r] != 0.0f);
+        }
+        masks[q] = __ballot(live);
+        before += __popcll(masks[q]);
+    }
+    if (lane == 0) waves[wave] = before;
+    __syncthreads();
+    int at = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) at += waves[w];
+        count += waves[w];
+    }
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+        const int r = wave * (64 * EACH) + q * 64 + lane, mine = at + __popcll(masks[q] & ((1ull << lane) - 1));
+        const bool live = masks[q] >> lane & 1;
+        if (live && mine == j) found = r;
+        if (j == 0 && r < rows) {
+            if (live) L.index[mine] = r;
+            L.place[r] = live ? mine : -1;
+            if (!live && logp) logp[r] = 0.0f;
+            if (!live && row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
+        }
+        at += __popcll(masks[q]);
+    }
+    if (j == 0 && threadIdx.x == 0) *L.count = count;
+    __syncthreads();
+    copy_row<WIDE>(from + (int64_t)max(found, 0) * stride, cols, found >= 0, to + j * width, width);
 }
 
 // What the tiles of z leave, or take.  Columns of a tile (n) are rows of the batch, its rows (m) are words.
@@ -490,10 +544,33 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, i
     uint16_t *out = G.dz + (tr * T::BN + wn * T::NI * 16) * G.stride + (w0 - G.word0);
     store_rows<T>(lds, wave, lane, [&](int i, int j, int r) { return acc[i][j][r]; }, out, G.stride, T::NI * 16, T::MI * 16);
 }
-// the same from z that was kept: a lane four words
-__global__ __launch_bounds__(256) void k_head_dz_kept(Logit G)
+// loss (+)= sum of weights times -logp over the rows that count, by one workgroup
+struct Loss {
+    const float *logp, *weights;
+    float *loss;              // null: none
+    int accumulate;
+};
+__device__ __forceinline__ void loss_of(const Live &live, const Loss &L)
+{
+    __shared__ double lds[4];
+    const int count = *live.count;
+    double s = 0.0;
+    for (int j = threadIdx.x; j < count; j += 256) {
+        const int r = live.index[j];
+        s -= (double)(L.weights ? L.weights[r] : 1.0f) * (double)L.logp[r];
+    }
+    s = block_sum<256>(s, lds);
+    if (threadIdx.x == 0) *L.loss = (float)(s + (L.accumulate ? (double)*L.loss : 0.0));
+}
+__global__ __launch_bounds__(256) void k_head_loss(Live live, Loss L) { loss_of(live, L); }
+// dz from z that was kept: a lane four words; the workgroup behind the rows' has the loss
+__global__ __launch_bounds__(256) void k_head_dz_kept(Logit G, Loss L)
 {
     const int64_t row = blockIdx.x, w = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
+    if (row >= G.rows) {
+        if (blockIdx.y == 0 && L.loss) loss_of(G.live, L);
+        return;
+    }
     const int count = *G.live.count;
     if (row >= (count + 255) / 256 * 256 || w >= (G.words + 255) / 256 * 256) return;
     float d[4] = {};
@@ -657,20 +734,6 @@ __global__ __launch_bounds__(256) void k_head_rows(Live live, const float *row_s
     const int64_t r = live.index[j];
     const float unit = unit_of(it * dlogp[live.index[0]]);
     row[j] = float4{row_stats[2 * r], 1.0f / row_stats[2 * r + 1], it * dlogp[r] / unit, unit};
-}
-
-// loss (+)= sum of weights times -logp over the rows that count
-__global__ __launch_bounds__(1024) void k_head_loss(Live live, const float *logp, const float *weights, float *loss, int accumulate)
-{
-    __shared__ double lds[16];
-    const int count = *live.count;
-    double s = 0.0;
-    for (int j = threadIdx.x; j < count; j += 1024) {
-        const int r = live.index[j];
-        s -= (double)(weights ? weights[r] : 1.0f) * (double)logp[r];
-    }
-    s = block_sum<1024>(s, lds);
-    if (threadIdx.x == 0) *loss = (float)(s + (accumulate ? (double)*loss : 0.0));
 }
 
 // dx of the rows that count from their sums, zeros in the others: a lane four elements
@@ -866,7 +929,8 @@ typedef Tile<128, 64, 4, 1, 3> Slim;          // up to 64: the weights' way from
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 256 << 20;          // of dz
-constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits
+constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits; with less of the hidden
+constexpr int64_t kKeptWidth = 512;                 // state than this z is made again as soon as it is written and read
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
 constexpr int64_t MID_TILES = 200;                  // large tiles of z below which there are too few for the chip
 
@@ -879,6 +943,7 @@ struct Plan {
     int64_t joined;          // maxima and sums of a row
     int splits;              // of the sums to the rows
     int words, side;         // of a tile: words (or hidden columns), rows
+    int dx, dw;              // rows of the tiles of the sums to the rows, words of those to the weights
     bool kept;
     size_t index, x, partials, target, row, z, dz, sum, w, all;      // places in the workspace, and its size
 };
@@ -894,11 +959,21 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     P.tiles = up(vocab, 256) / 256;
     P.joined = up(vocab, P.words) / P.words;
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * P.rows * 256));
-    P.kept = gradient && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
+    P.kept = gradient && P.width >= kKeptWidth && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
     P.piece = (P.kept ? P.tiles : std::min(P.tiles, most)) * 256;
     P.packed = std::min(P.piece, std::max<int64_t>(1, kPackedBytes / (2 * P.width * 256)) * 256);
-    const int64_t out = P.rows / P.side * (up(hidden, P.words) / P.words);      // tiles of the sums to the rows
-    P.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(P.piece / 1024, 32), 512 / out));
+    // Tiles of 256 columns of the hidden state, unless those would be a quarter wider than it.
+    const bool wide = up(hidden, 256) * 4 <= up(hidden, 128) * 5;
+    P.dx = P.side == Slim::BN ? Slim::BN : wide && P.side == Big::BN ? Big::BN : Mid::BN;
+    P.dw = wide ? Big::BN : Mid::BN;
+    // The sums to the rows in parts of k that fill the chip: the fewest of those whose tiles take least, a step each and 24 for what a tile has to do besides.
+    const int64_t out = P.rows / P.dx * (up(hidden, P.dx == Big::BN ? Big::BM : Slim::BM) / (P.dx == Big::BN ? Big::BM : Slim::BM)), at_once = P.dx == Big::BN ? 256 : 512;
+    const int64_t steps = up(std::min(P.piece, vocab), BK) / BK;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= 32 && s * 4 <= std::max<int64_t>(steps, 4); ++s) {
+        const int64_t time = up(out * s, at_once) / at_once * ((steps + s - 1) / s + 24);
+        if (time * 20 < least * 19 || s == 1) least = time, P.splits = s;
+    }
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
@@ -964,8 +1039,14 @@ static hipError_t pack(const Call &C, const uint16_t *from, int64_t stride, cons
 // the rows that count, packed
 static hipError_t pack_rows(const Call &C, const float *factor, float *logp, float *row_stats)
 {
-    k_head_live<<<1, LIVE_BLOCK, 0, C.stream>>>(C.targets, factor, (int)C.h.rows, (int)C.h.vocab, C.live, logp, row_stats);
-    return pack(C, C.h.x, C.h.x_stride, C.live, C.P.rows, C.P.rows, C.x());
+    const gs_head &h = C.h;
+    if (C.P.rows <= GATHER_MAX) {
+        auto *kernel = multiple16(h.x, h.x_stride) ? k_head_gather<true> : k_head_gather<false>;
+        kernel<<<(uint32_t)C.P.rows, 256, 0, C.stream>>>(C.targets, factor, (int)h.rows, (int)h.vocab, C.live, logp, row_stats, h.x, h.x_stride, h.hidden, C.x(), C.P.width);
+        return hipGetLastError();
+    }
+    k_head_live<<<1, LIVE_BLOCK, 0, C.stream>>>(C.targets, factor, (int)h.rows, (int)h.vocab, C.live, logp, row_stats);
+    return pack(C, h.x, h.x_stride, C.live, C.P.rows, C.P.rows, C.x());
 }
 static Logit logit_of(const Call &C, int64_t word0, int64_t words)
 {
@@ -990,15 +1071,16 @@ static Logit logit_of(const Call &C, int64_t word0, int64_t words)
 }
 static uint32_t grid_of(int64_t tiles) { return (uint32_t)(up(tiles, 8)); }
 
-// each(first word, words, their weights) of every piece
-template <typename F> static hipError_t pieces(const Call &C, F each)
+// each(first word, words, their weights) of every piece; have_w: weights packed as one piece are there already
+template <typename F> static hipError_t pieces(const Call &C, bool have_w, F each)
 {
     const int64_t piece = C.packed ? C.P.packed : C.P.piece;
     for (int64_t w = 0; w < C.h.vocab; w += piece) {
         const int64_t words = std::min(piece, C.h.vocab - w);
         Operand W = {C.h.w + w * C.h.w_stride, C.h.w_stride, words, C.h.hidden};
         if (C.packed) {
-            if (hipError_t e = pack(C, W.p, W.stride, Live{}, words, words, C.w()); e != hipSuccess) return e;
+            if (!(have_w && piece >= C.h.vocab))
+                if (hipError_t e = pack(C, W.p, W.stride, Live{}, words, words, C.w()); e != hipSuccess) return e;
             W = {C.w(), C.P.width, words, C.P.width};
         }
         if (hipError_t e = each(w, words, W); e != hipSuccess) return e;
@@ -1010,7 +1092,7 @@ template <typename T>
 static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
 {
     const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
-    hipError_t e = pieces(C, [&](int64_t w, int64_t words, const Operand &W) {
+    hipError_t e = pieces(C, false, [&](int64_t w, int64_t words, const Operand &W) {
         k_head_stats<T><<<grid_of(up(words, T::BM) / T::BM * (C.P.rows / T::BN)), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), logit_of(C, w, words));
         return hipGetLastError();
     });
@@ -1039,7 +1121,11 @@ static void launch_dot(const Few &G, uint32_t grid, hipStream_t stream)
 }
 // Rows that are scored without LDS: up to 4 in any case, up to 16 while the weights are few (us, against tiles, 16 rows: 2^25 values 21/24, 2^27 57/57, 2^28 123/129,
 // 2^29 267/187: half lines, but more workgroups).
-static bool few_rows(int64_t rows, int64_t hidden, int64_t vocab) { return rows <= DOT_ROWS || (rows <= FEW_ROWS && hidden * vocab <= (int64_t)1 << 28); }
+static bool few_rows(int64_t rows, int64_t hidden, int64_t vocab)
+{
+    if (vocab > (int64_t)1 << 28) return false;            // of whose workgroups a launch does not take as many
+    return rows <= DOT_ROWS || (rows <= FEW_ROWS && hidden * vocab <= (int64_t)1 << 28);
+}
 static hipError_t forward_few(const Call &C, float *logp, float *row_stats)
 {
     const gs_head &h = C.h;
@@ -1055,36 +1141,45 @@ static hipError_t forward_few(const Call &C, float *logp, float *row_stats)
     return hipGetLastError();
 }
 
-template <typename T>
-static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
+template <typename T> static void launch_dx(const Call &C, const Operand &W, const Operand &DZ, const ToRows &R)
 {
-    const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
-    const int64_t H = C.P.width, htiles = up(H, T::BM) / T::BM, rtiles = C.P.rows / T::BN;
-    hipError_t e = pieces(C, [&](int64_t w, int64_t words, const Operand &W) {
-        const int64_t wtiles = up(words, T::BM) / T::BM;
+    k_head_dx<T><<<dim3(grid_of(C.P.rows / T::BN * (up(C.P.width, T::BM) / T::BM)), (uint32_t)C.P.splits), T::BLOCK, 0, C.stream>>>(W, DZ, R);
+}
+template <typename T> static void launch_dw(const Call &C, const Operand &X, const Operand &DZ, const ToWeights &R)
+{
+    k_head_dw<T><<<grid_of(up(R.words, T::BN) / T::BN * (up(R.hidden, T::BM) / T::BM)), T::BLOCK, 0, C.stream>>>(X, DZ, R);
+}
+template <typename T> static void launch_dz(const Call &C, const Operand &W, const Operand &X, const Logit &G)
+{
+    k_head_dz<T><<<grid_of(up(G.words, T::BM) / T::BM * (C.P.rows / T::BN)), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
+}
+// after_forward: z, if it is kept, and weights packed as one piece are there from the forward pass, whose loss is still to be summed
+static hipError_t backward(const Call &C, const gs_head_grads &D, bool after_forward, const Loss &loss)
+{
+    const Plan &P = C.P;
+    const bool have_z = after_forward && P.kept;
+    if (loss.loss && !have_z) k_head_loss<<<1, 256, 0, C.stream>>>(C.live, loss);
+    const Operand X = {C.x(), P.width, P.rows, P.width};
+    hipError_t e = pieces(C, after_forward, [&](int64_t w, int64_t words, const Operand &W) {
         const Logit G = logit_of(C, w, words);
-        if (have_z) k_head_dz_kept<<<dim3((uint32_t)C.P.rows, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G);
-        else k_head_dz<T><<<grid_of(wtiles * rtiles), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
-        const Operand DZ = {C.dz(), C.P.piece, C.P.rows, C.P.piece};
+        if (have_z) k_head_dz_kept<<<dim3((uint32_t)P.rows + 1, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G, w == 0 ? loss : Loss{});
+        else (P.side == Slim::BN ? launch_dz<Slim> : P.side == Mid::BN ? launch_dz<Mid> : launch_dz<Big>)(C, W, X, G);
+        const Operand DZ = {C.dz(), P.piece, P.rows, P.piece};
         if (D.dx) {
-            const ToRows R = {C.live, C.P.rows, H, C.sum(), w == 0, C.P.splits, (int)(up(words, BK) / BK)};
-            k_head_dx<T><<<dim3(grid_of(rtiles * htiles), (uint32_t)C.P.splits), T::BLOCK, 0, C.stream>>>(W, DZ, R);
+            const ToRows R = {C.live, P.rows, P.width, C.sum(), w == 0, P.splits, (int)(up(words, BK) / BK)};
+            (P.dx == Slim::BN ? launch_dx<Slim> : P.dx == Mid::BN ? launch_dx<Mid> : launch_dx<Big>)(C, W, DZ, R);
         }
         if (D.dw) {
-            const ToWeights R = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : H, C.row()};
-            k_head_dw<Big><<<grid_of(up(words, 256) / 256 * (up(C.h.hidden, 256) / 256)), Big::BLOCK, 0, C.stream>>>(X, DZ, R);
+            const ToWeights R = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : C.h.hidden, C.row()};
+            (P.dw == Mid::BN ? launch_dw<Mid> : launch_dw<Big>)(C, X, DZ, R);
         }
-        if (D.dbias) k_head_db<<<(uint32_t)((words + 127) / 128), 1024, 0, C.stream>>>(C.dz(), C.P.piece, C.live, words, C.row(), D.dbias + w);
+        if (D.dbias) k_head_db<<<(uint32_t)((words + 127) / 128), 1024, 0, C.stream>>>(C.dz(), P.piece, C.live, words, C.row(), D.dbias + w);
         return hipGetLastError();
     });
     if (e != hipSuccess || !D.dx || !C.h.rows) return e;
-    k_head_rows_out<<<dim3((uint32_t)C.h.rows, (uint32_t)((C.h.hidden + 1023) / 1024)), 256, 0, C.stream>>>(C.live, C.sum(), C.P.splits, C.P.rows, H, C.h.hidden, C.row(),
-                                                                                                          D.dx, C.h.rows > 1 ? D.dx_stride : C.h.hidden);
+    k_head_rows_out<<<dim3((uint32_t)C.h.rows, (uint32_t)((C.h.hidden + 1023) / 1024)), 256, 0, C.stream>>>(C.live, C.sum(), P.splits, P.rows, P.width, C.h.hidden, C.row(), D.dx,
+                                                                                                          C.h.rows > 1 ? D.dx_stride : C.h.hidden);
     return hipGetLastError();
-}
-static hipError_t backward(const Call &C, const gs_head_grads &D, bool have_z)
-{
-    return (C.P.side == Slim::BN ? backward<Slim> : C.P.side == Mid::BN ? backward<Mid> : backward<Big>)(C, D, have_z);
 }
 
 // ---- checks -------------------------------------------------------------------------------------
@@ -1205,7 +1300,7 @@ gs_status gs_head_logp_grad(const gs_head *head, const int64_t *targets, float t
         k_head_rows<<<(uint32_t)((C.P.rows + 255) / 256), 256, 0, C.stream>>>(C.live, row_stats, dlogp, C.it, C.row());
         e = hipGetLastError();
     }
-    if (e == hipSuccess) e = backward(C, *grads, false);
+    if (e == hipSuccess) e = backward(C, *grads, false, Loss{});
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_head_logp_grad launch");
 }
 
@@ -1230,11 +1325,12 @@ gs_status gs_head_cross_entropy(const gs_head *head, const int64_t *targets, con
     const Call C = call_of(*head, targets, temperature, grads != nullptr, d_workspace, stream);
     hipError_t e = pack_rows(C, weights, logp, nullptr);
     if (e == hipSuccess) e = forward(C, logp, nullptr, weights, grads != nullptr);
-    if (e == hipSuccess) {
-        k_head_loss<<<1, 1024, 0, C.stream>>>(C.live, logp, weights, d_loss, accumulate);
+    const Loss loss = {logp, weights, d_loss, accumulate};
+    if (e == hipSuccess && grads) e = backward(C, *grads, true, loss);
+    if (e == hipSuccess && !grads) {
+        k_head_loss<<<1, 256, 0, C.stream>>>(C.live, loss);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && grads) e = backward(C, *grads, C.P.kept);
     return e == hipSuccess ? GS_OK : hip_fail(e, "gs_head_cross_entropy launch");
 }
 
