@@ -662,7 +662,8 @@ typedef struct {
 } gs_head_grads;
 
 /* Bytes of device workspace that the calls below need for such a head, with or without a gradient; 0 for sizes that they refuse.
- * The workspace is aligned to 256 bytes; nothing has to be in it before, and nothing is kept in it from call to call. */
+ * The workspace is aligned to 256 bytes; nothing has to be in it before, and nothing is kept in it from call to call.  Calls that may run at the same time
+ * (on two streams, or captured into graphs that do) need one each. */
 size_t gs_head_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab, int gradient);
 
 /* gs_token_logp of a head's rows: scoring of sequences, or of the token just drawn (rows == 1). */
@@ -729,7 +730,8 @@ size_t gs_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
  *   row_stats      (mean, rstd) as gs_layer_norm left them for the same x
  *   dy, dx         device, x's type, at strides of their own; dx may be dy itself (same address and stride)
  *   dgamma, dbeta  device, `cols` values of weight_dtype, written; both or neither (NULL)
- *   workspace      aligned to 256 bytes, of gs_layer_norm_workspace_bytes; not looked at without dgamma
+ *   workspace      aligned to 256 bytes, of gs_layer_norm_workspace_bytes, one for each of the calls that may run at the same time; not looked at
+ *                  without dgamma
  */
 gs_status gs_layer_norm_grad(const gs_matrix *x, const void *gamma, int32_t weight_dtype, const float *row_stats, const void *dy,
                              int64_t dy_stride, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, void *d_workspace,

@@ -45,7 +45,8 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 // What bounds it is power: the chip holds its clock (1.9 GHz here, of 2.4) to what the matrix cores, LDS and loads draw together, and each adds to
 // the time.  16 x 16 x 32 products draw least (alone, of random values, 2160 TFLOP/s; 32 x 32 x 16, whose sums go through the registers twice as
 // often, 1900); rows of 128 bytes are whole lines of the caches (64 bytes a row, four stages: 1190 TFLOP/s against 1300 for 8192 x 4096 x 16384, both steps
-// together).  Four waves of 128 x 128, which read a third less LDS: level, they wait where eight do not.
+// together).  Four waves of 128 x 128, which read a third less LDS: level, they wait where eight do not.  Of 8192 x 4096 x 16384 (0.82 ms, 1340 TFLOP/s;
+// the library's 8192 x 131072 x 4096 1490) the products alone take 0.53 ms, with the reads 0.65, with the loads but not the reads 0.65.
 constexpr int BK = 64, PART = 32, PARTS = BK / PART;
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, BLOCK = WAVES * 64, STAGES = STAGES_;
@@ -59,12 +60,12 @@ struct Operand {
     int64_t rows, cols;
 };
 
-// 16 bytes a lane from base + offset to LDS, one lane's behind another's.  By hand because the compiler holds every transposing read back until all loads on
+// 16 bytes a lane from base + offset to LDS (from `lds` + AT on), one lane's behind another's.  By hand because the compiler holds every transposing read back until all loads on
 // their way to LDS have come; nothing is returned in registers, and who reads waits for vmcnt and a barrier.
-__device__ __forceinline__ void load_to_lds(const char *base, uint32_t offset, char *lds)
+template <int AT>
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
-    const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base), "n"(AT) : "memory", "scc");
 }
 
 // ALONG: LDS has W rows of 128 bytes, whose eight 16-byte chunks are exchanged by the row's bits 1 to 3, so that 16 lanes that read a chunk
@@ -75,18 +76,18 @@ template <int W, int WAVES, int FRAGS, bool ALONG, bool ENDS> struct Side {
     static constexpr int LOADS = W / 8 / WAVES;
     static_assert(LOADS >= 1 && W * BK * 2 == LOADS * WAVES * 1024, "whole loads of each wave");
     static_assert((FRAGS & (FRAGS - 1)) == 0 && (ALONG || W >= 128), "blocks are told apart by bits of an address");
-    const char *base;                     // of the tile
+    const char *next;                     // of the tile, in the step that is loaded next
     int64_t step_by;                      // bytes from a step to the next
     uint32_t at[LOADS], beyond[LOADS];    // bytes from the base; of them, what the last step's rows of k lie behind the operand's last one
     uint32_t frag;                        // of the wave's first block in a stage
-    int place;                            // in the stage of this wave's first load
+    uint32_t place;                       // in the stage of this wave's first load
 
     static __device__ __forceinline__ int slot(int row) { return 2 * (row & 3) | ((row >> 3) & 1); }
     __device__ __forceinline__ void start(const Operand &X, int64_t first, int64_t k0, int steps, int wave, int lane, int sub)
     {
-        place = wave * LOADS * 1024;
+        place = (uint32_t)(wave * LOADS * 1024);
         step_by = 2 * (ALONG ? BK : BK * X.stride);
-        base = reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(X.p + (ALONG ? first * X.stride + k0 : k0 * X.stride + first))));
+        next = reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(X.p + (ALONG ? first * X.stride + k0 : k0 * X.stride + first))));
         const uint32_t stride = (uint32_t)X.stride * 2;
 #pragma unroll
         for (int q = 0; q < LOADS; ++q) {
@@ -108,11 +109,11 @@ template <int W, int WAVES, int FRAGS, bool ALONG, bool ENDS> struct Side {
             frag = (uint32_t)(row * (2 * W) + (((sub * FRAGS) ^ slot(row)) << 5) + (lane & 3) * 8);
         }
     }
-    __device__ __forceinline__ void load(char *stage, int q, int step, bool end) const
+    template <int Q> __device__ __forceinline__ void load(uint32_t stage, bool end) const
     {
-        uint32_t offset = at[q];
-        if constexpr (ENDS) offset -= end ? beyond[q] : 0;
-        load_to_lds(base + step * step_by, offset, stage + place + q * 1024);
+        uint32_t offset = at[Q];
+        if constexpr (ENDS) offset -= end ? beyond[Q] : 0;
+        load_to_lds<Q * 1024>(next, offset, stage + place);
     }
     // block f's operand of part s of a stage
     __device__ __forceinline__ bf16x8 read(uint32_t stage, int s, int f) const
@@ -142,6 +143,15 @@ template <int N> __device__ __forceinline__ void wait_loads()
 }
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
+// f(0) ... f(N - 1), each a constant of its own
+template <int N, typename F> __device__ __forceinline__ void each(F f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
 // acc = the tile's product over `steps` steps of BK from k0 on.  Every access lies in the operands, whatever `steps` is: loads ahead of the end
 // repeat the last step's.  At the end every wave has passed a barrier and no load is on its way, so the LDS can be used again.
 //
@@ -164,61 +174,64 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
         for (int j = 0; j < T::NI; ++j) acc[i][j] = f32x4{};
     if (steps <= 0) return;
     const int end = steps - 1;
-    auto load = [&](int t, int q) {
-        char *stage = lds + t % T::STAGES * T::STAGE;
-        const int s = t < end ? t : end;
-        if (q < A_LOADS) a.load(stage, q, s, s == end);
-        else b.load(stage + T::BM * BK * 2, q - A_LOADS, s, s == end);
+    // What the wave's loads and reads go by is kept from step to step in scalar registers, a few additions each: between two products there is room for
+    // three other instructions.
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds), lds_last = lds0 + (T::STAGES - 1) * T::STAGE;
+    auto behind = [&](uint32_t stage) { return stage == lds_last ? lds0 : stage + (uint32_t)T::STAGE; };
+    int loading = 0;                       // the step that is loaded, and the stage that it takes
+    uint32_t to = lds0;
+    auto load = [&](auto q) {
+        if constexpr (q < A_LOADS) a.template load<q>(to, loading >= end);
+        else b.template load<q - A_LOADS>(to + T::BM * BK * 2, loading >= end);
+        if constexpr (q == L - 1) {
+            if (loading < end) a.next += a.step_by, b.next += b.step_by;
+            ++loading;
+            to = behind(to);
+        }
     };
-    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds);
     bf16x8 fa[T::MI], fb[2][T::NI];
-    auto read_a = [&](int t, int s, int i) { fa[i] = a.read(lds0 + t % T::STAGES * T::STAGE, s, i); };
-    auto read_b = [&](int t, int s, int j) { fb[s & 1][j] = b.read(lds0 + t % T::STAGES * T::STAGE + T::BM * BK * 2, s, j); };
+    uint32_t from = lds0;                  // the stage that is read
+    auto read_a = [&](int s, int i) { fa[i] = a.read(from, s, i); };
+    auto read_b = [&](int s, int j) { fb[s & 1][j] = b.read(from + T::BM * BK * 2, s, j); };
     // A part's products, with a read or a load behind some, so that none of them keeps the matrix cores waiting: a row of blocks' operand is read again as
     // soon as its last product has begun.  Loads begin behind the barrier and end half a step later.  The order is held as it stands here.
     constexpr int BAR = T::NI;                              // products of the last part in front of the barrier
     constexpr int EACH = MN * PARTS / 2 / L, FIRST = (MN - BAR) / EACH < L ? (MN - BAR) / EACH : L;      // products to a load; loads in the last part
     static_assert(EACH >= 1 && BAR + T::NI <= MN, "a place for each load and read");
-    auto part = [&](int t, int s) {
-        const bool last = s == PARTS - 1;
-        const int tr = last ? t + 1 : t, sr = last ? 0 : s + 1;
-#pragma unroll
-        for (int p = 0; p < MN; ++p) {
-            if (last && p == BAR) {
+    auto part = [&](auto part_of) {
+        constexpr int s = part_of, next = s == PARTS - 1 ? 0 : s + 1;
+        constexpr bool last = s == PARTS - 1;
+        each<MN>([&](auto p) {
+            if constexpr (last && p == BAR) {
                 wait_loads<(T::STAGES - 2) * L>();
                 barrier();
+                from = behind(from);
             }
-            const int i = p / T::NI, j = p % T::NI;
+            constexpr int i = p / T::NI, j = p % T::NI;
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[s & 1][j], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
-            if (j == 0 && i > 0) read_a(tr, sr, i - 1);
-            if (p == MN - 1) read_a(tr, sr, i);
-            if (p >= BAR && p - BAR < T::NI) read_b(tr, sr, p - BAR);
-            if (last) {
-                if (p >= BAR && (p - BAR) % EACH == 0 && (p - BAR) / EACH < FIRST) load(t + T::STAGES, (p - BAR) / EACH);
+            if constexpr (j == 0 && i > 0) read_a(next, i - 1);
+            if constexpr (p == MN - 1) read_a(next, i);
+            if constexpr (p >= BAR && p - BAR < T::NI) read_b(next, p - BAR);
+            if constexpr (last) {
+                if constexpr (p >= BAR && (p - BAR) % EACH == 0 && (p - BAR) / EACH < FIRST) load(std::integral_constant<int, (p - BAR) / EACH>{});
             } else {
-                const int g = s * MN + p;
-                if (g % EACH == 0 && FIRST + g / EACH < L) load(t + T::STAGES - 1, FIRST + g / EACH);
+                constexpr int g = s * MN + p;
+                if constexpr (g % EACH == 0 && FIRST + g / EACH < L) load(std::integral_constant<int, FIRST + g / EACH>{});
             }
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
 #pragma unroll
-    for (int t = 0; t < T::STAGES - 1; ++t)
-#pragma unroll
-        for (int q = 0; q < L; ++q) load(t, q);
+    for (int t = 0; t < T::STAGES - 1; ++t) each<L>([&](auto q) { load(q); });
     wait_loads<(T::STAGES - 2) * L>();
     barrier();
+    each<FIRST>([&](auto q) { load(q); });
 #pragma unroll
-    for (int q = 0; q < FIRST; ++q) load(T::STAGES - 1, q);
+    for (int f = 0; f < T::NI; ++f) read_b(0, f);
 #pragma unroll
-    for (int f = 0; f < T::NI; ++f) read_b(0, 0, f);
-#pragma unroll
-    for (int f = 0; f < T::MI; ++f) read_a(0, 0, f);
-    for (int t = 0; t < steps; ++t) {
-#pragma unroll
-        for (int s = 0; s < PARTS; ++s) part(t, s);
-    }
+    for (int f = 0; f < T::MI; ++f) read_a(0, f);
+    for (int t = 0; t < steps; ++t) each<PARTS>([&](auto s) { part(s); });
     wait_loads<0>();
     barrier();
 }
@@ -226,15 +239,16 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int6
 __device__ __forceinline__ int row_of(int r, int lane) { return 4 * (lane >> 4) + r; }
 __device__ __forceinline__ int column_of(int lane) { return lane & 15; }
 
-// Tiles in groups of 8 along the first dimension, dealt so that each of the 8 dies has neighbours: its 32 CUs work on about 8 x 4 tiles at a
-// time, whose operands its L2 holds.  false: no tile.
+// Tiles in groups along the first dimension, dealt so that each of the 8 dies has neighbours: its 32 CUs work on about 4 x 8 tiles at a time, whose
+// operands its L2 holds.  (8 at a time 1 % behind; where all the work is to write rows of results, 4 are 4 % behind.)  false: no tile.
+template <int GROUP = 4>
 __device__ __forceinline__ bool my_tile(int64_t tiles1, int64_t tiles2, int64_t &t1, int64_t &t2)
 {
     // a launch has fewer than 2^32 work items, and so fewer than 2^24 tiles
     const uint32_t second = (uint32_t)tiles2, all = (uint32_t)tiles1 * second, per = (all + 7) / 8, id = blockIdx.x, t = (id & 7) * per + (id >> 3);
     if ((id >> 3) >= per || t >= all) return false;
-    const uint32_t group = t / (8 * second), in = t - group * 8 * second, left = (uint32_t)tiles1 - group * 8, width = left < 8 ? left : 8;
-    t1 = __builtin_amdgcn_readfirstlane((int)(group * 8 + in % width));
+    const uint32_t group = t / (GROUP * second), in = t - group * GROUP * second, left = (uint32_t)tiles1 - group * GROUP, width = left < GROUP ? left : GROUP;
+    t1 = __builtin_amdgcn_readfirstlane((int)(group * GROUP + in % width));
     t2 = __builtin_amdgcn_readfirstlane((int)(in / width));
     return true;
 }
@@ -281,6 +295,7 @@ struct Live {
     int32_t *count;
     int32_t *index;        // the batch's row that is the j-th to count
     int32_t *place;        // of a row of the batch among those; -1: it does not count
+    int32_t *token;        // of the j-th
 };
 constexpr int LIVE_BLOCK = 1024;
 // Rows that do not count get logp 0 and statistics (0, 1) here, where there are any to write.
@@ -292,8 +307,9 @@ __global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets
     for (int base = 0; base < rows; base += LIVE_BLOCK) {
         const int r = base + threadIdx.x;
         bool live = false;
+        int64_t t = -1;
         if (r < rows) {
-            const int64_t t = targets[r];
+            t = targets[r];
             live = t >= 0 && t < vocab && (!factor || factor[r] != 0.0f);
             if (!live && logp) logp[r] = 0.0f;
             if (!live && row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
@@ -307,7 +323,7 @@ __global__ __launch_bounds__(LIVE_BLOCK) void k_head_live(const int64_t *targets
             sum += waves[w];
         }
         at += __popcll(mask & ((1ull << lane) - 1));
-        if (live) L.index[at] = r;
+        if (live) L.index[at] = r, L.token[at] = (int32_t)t;
         if (r < rows) L.place[r] = live ? at : -1;
         before += sum;
         __syncthreads();
@@ -381,7 +397,7 @@ __global__ __launch_bounds__(256) void k_head_gather(const int64_t *targets, con
         const bool live = masks[q] >> lane & 1;
         if (live && mine == j) found = r;
         if (j == 0 && r < rows) {
-            if (live) L.index[mine] = r;
+            if (live) L.index[mine] = r, L.token[mine] = (int32_t)targets[r];
             L.place[r] = live ? mine : -1;
             if (!live && logp) logp[r] = 0.0f;
             if (!live && row_stats) row_stats[2 * r] = 0.0f, row_stats[2 * r + 1] = 1.0f;
@@ -396,7 +412,6 @@ __global__ __launch_bounds__(256) void k_head_gather(const int64_t *targets, con
 // What the tiles of z leave, or take.  Columns of a tile (n) are rows of the batch, its rows (m) are words.
 struct Logit {
     const uint16_t *bias;
-    const int64_t *targets;
     Live live;
     int64_t rows;             // of the packed batch
     int64_t word0, words;     // this piece of the vocabulary; tiles' words are counted from word0
@@ -464,10 +479,18 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
-    f32x4 acc[T::MI][T::NI];
-    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
     const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 16;
+    int target[T::NI];                     // on its way during the product
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j) target[j] = G.live.token[tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane)];
+    f32x4 acc[T::MI][T::NI];
+    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j) {
+        asm volatile("" : "+v"(target[j]));          // not looked at before
+        target[j] = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane) < count ? place_of(target[j], w0, lane) : -1;
+    }
     add_bias<T>(G, w0, lane, acc);
     const int left = words_left(G, w0, lane);
     float2 *joint = reinterpret_cast<float2 *>(lds);        // [WM][BN]
@@ -475,7 +498,6 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X
     for (int j = 0; j < T::NI; ++j) {
         const int n = (wn * T::NI + j) * 16 + column_of(lane);
         const int64_t row = tr * T::BN + n;
-        const int target = row < count ? place_of(G.targets[G.live.index[row]], w0, lane) : -1;
         float m = -INFINITY, z = 0.0f;
         bool here = false;
         if (G.z) {
@@ -488,7 +510,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (word_of(i, r) >= left) acc[i][j][r] = -INFINITY;
-                if (word_of(i, r) == target) z = acc[i][j][r], here = true;
+                if (word_of(i, r) == target[j]) z = acc[i][j][r], here = true;
                 m = fmaxf(m, acc[i][j][r]);
             }
         if (here) G.target_logit[row] = z;
@@ -524,18 +546,26 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, i
     if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
-    f32x4 acc[T::MI][T::NI];
-    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
     const int64_t w0 = G.word0 + tw * T::BM + wm * T::MI * 16;
+    int targets[T::NI];                    // on their way during the product
+    f32x4 rows[T::NI];
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j) {
+        const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
+        targets[j] = G.live.token[row];
+        rows[j] = *reinterpret_cast<const f32x4 *>(G.row + row);
+    }
+    f32x4 acc[T::MI][T::NI];
+    product<T, true, true, false>(W, X, tw * T::BM, tr * T::BN, 0, steps, lds, acc);
     add_bias<T>(G, w0, lane, acc);
     const int left = words_left(G, w0, lane);
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) {
         const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
-        const bool live = row < count;
-        const int target = live ? place_of(G.targets[G.live.index[row]], w0, lane) : -1, words = live ? left : 0;
-        const float4 R = live ? G.row[row] : float4{};
+        asm volatile("" : "+v"(targets[j]), "+v"(rows[j]));          // not looked at before
+        const int words = row < count ? left : 0, target = row < count ? place_of(targets[j], w0, lane) : -1;
+        const float4 R = {rows[j][0], rows[j][1], rows[j][2], rows[j][3]};
 #pragma unroll
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
@@ -577,7 +607,7 @@ __global__ __launch_bounds__(256) void k_head_dz_kept(Logit G, Loss L)
     if (row < count) {
         const float4 R = G.row[row];
         const f32x4 z = *reinterpret_cast<const f32x4 *>(G.z + row * G.z_stride + w);
-        const int64_t target = G.targets[G.live.index[row]] - G.word0;
+        const int64_t target = G.live.token[row] - G.word0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (w + i < G.words) d[i] = dz_of(G, R, z[i], w + i == target);
@@ -632,7 +662,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, 
 {
     __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, th;
-    if (!my_tile((G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
+    if (!my_tile<8>((G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
     f32x4 acc[T::MI][T::NI];
     const int count = *G.live.count;
     product<T, false, false, false>(X, DZ, th * T::BM, tw * T::BN, 0, (count + BK - 1) / BK, lds, acc);
@@ -928,7 +958,7 @@ typedef Tile<128, 128, 2, 2, 2> Mid;          // up to 128, or too few for the o
 typedef Tile<128, 64, 4, 1, 3> Slim;          // up to 64: the weights' way from memory is all the time there is
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
-constexpr int64_t kPieceBytes = 256 << 20;          // of dz
+constexpr int64_t kPieceBytes = 512 << 20;          // of dz: 8192 x 4096 x 131072 25.9 ms, with 256 MB 26.1, 128 MB 26.0, 64 MB 27.1; 4095 x 2048 x 50001 2.33, 2.43, 2.69, 2.82
 constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits; with less of the hidden
 constexpr int64_t kKeptWidth = 512;                 // state than this z is made again as soon as it is written and read
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
@@ -980,7 +1010,7 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
         at += (size_t)up(bytes, 256);
         return here;
     };
-    P.index = take((2 * P.rows + 64) * 4);
+    P.index = take((3 * P.rows + 64) * 4);
     P.x = take(P.rows * P.width * 2);
     P.partials = take(std::max(P.joined * P.rows, rows <= FEW_ROWS ? up(vocab, FEW_WORDS) / FEW_WORDS * FEW_ROWS : 0) * 8);
     P.target = take(P.rows * 4);
@@ -1024,7 +1054,7 @@ static Call call_of(const gs_head &h, const int64_t *targets, float temperature,
     C.targets = targets;
     C.it = 1.0f / temperature;
     int32_t *index = reinterpret_cast<int32_t *>(C.ws + C.P.index);
-    C.live = {index, index + 64, index + 64 + C.P.rows};
+    C.live = {index, index + 64, index + 64 + C.P.rows, index + 64 + 2 * C.P.rows};
     C.stream = static_cast<hipStream_t>(stream);
     C.packed = h.hidden % 64 != 0 || !multiple16(h.w, C.h.w_stride) || C.h.w_stride >= 1 << 23;
     return C;
@@ -1052,7 +1082,6 @@ static Logit logit_of(const Call &C, int64_t word0, int64_t words)
 {
     Logit G = {};
     G.bias = C.h.bias;
-    G.targets = C.targets;
     G.live = C.live;
     G.rows = C.P.rows;
     G.word0 = word0;

@@ -169,7 +169,7 @@ def test_nan_and_infinity_in_a_row_stay_there():
     assert not bool(c.dx[rest].isnan().any())
 
 
-@pytest.mark.parametrize("rows, hidden, vocab, bias", [(8192, 64, 40_000, True), (20_000, 72, 9_000, False), (3, 64, 300_000, True), (5, 8, 2_200_000, True),
+@pytest.mark.parametrize("rows, hidden, vocab, bias", [(8192, 64, 40_000, True), (20_000, 72, 9_000, False), (3, 64, 300_000, True), (5, 8, 4_400_000, True), (1100, 512, 20_000, True),
                                                        (20, 8200, 10_000, True), (300, 8200, 9_000, False)])
 def test_many_pieces_and_tiles(rows, hidden, vocab, bias):
     """More words than a piece has, with z kept and made again, weights packed in pieces of their own, more rows than a group of tiles."""
@@ -275,6 +275,39 @@ def test_same_bits_from_call_to_call_on_any_stream_and_from_a_graph(rows):
             graph.replay()
     torch.cuda.synchronize()
     check_all(c, 0), check_all(d, 1)
+
+
+@pytest.mark.parametrize("rows", [3, 50, 400])
+def test_on_some_of_the_cus(rows):
+    """A stream that has 16 of the CUs: the same bits."""
+    c = Case(rows, 512, 1500, bias=True, prompt=rows > 4)
+    want = {k: v.clone() for k, v in c.cross_entropy().items()}
+    ws = c.workspace()
+    stream = gs.gs_cu_stream_create(16)
+    try:
+        for t in (c.logp, c.dx, c.dw, c.db):
+            t.fill_(8.0)
+        torch.cuda.synchronize()
+        gs.gs_head_cross_entropy(c.x, c.w, c.bias, c.targets, c.weights, c.logp, c.dx, c.dw, c.db, c.loss, ws, stream=stream)
+        torch.cuda.synchronize()
+        for k, v in {"logp": c.logp, "dx": c.dx, "dw": c.dw, "db": c.db}.items():
+            assert torch.equal(v, want[k]), k
+    finally:
+        gs.gs_cu_stream_destroy(stream)
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own():
+    c, d = Case(300, 256, 2000), Case(90, 256, 2000, seed=3)
+    want = [{k: v.clone() for k, v in q.cross_entropy().items()} for q in (c, d)]
+    spaces, streams = [c.workspace(), d.workspace()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q, ws, s in zip((c, d), spaces, streams):
+            gs.gs_head_cross_entropy(q.x, q.w, q.bias, q.targets, q.weights, q.logp, q.dx, q.dw, q.db, q.loss, ws, stream=s)
+    torch.cuda.synchronize()
+    for q, w in zip((c, d), want):
+        for k, v in {"logp": q.logp, "dx": q.dx, "dw": q.dw, "db": q.db}.items():
+            assert torch.equal(v, w[k]), k
 
 
 def test_weights_beyond_32_bits_of_offsets():
