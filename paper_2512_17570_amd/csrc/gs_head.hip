@@ -3,7 +3,9 @@
 // vocabulary at a time, as dz in bf16, which two more products take to the hidden states and to the weights.
 //
 // All the work is in products of matrices: 2 N V H operations for the log-probabilities and 8 N V H with the gradient (2 of them to make
-// z again), on the matrix cores.
+// z again), on the matrix cores.  rows x hidden x vocabulary: 8192 x 2048 x 50304 scored in 1.34 ms (1262 TFLOP/s), 8192 x 4096 x 131072 with its gradients
+// 26.5 ms (1330 TFLOP/s), 4095 x 2048 x 50001 with a bias 2.33 ms; with few rows memory is the bound: one of 4096 x 131072 scored in 161 us (7.0 TB/s of weights),
+// 64 x 4096 x 32000 with gradients 222 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -359,7 +361,8 @@ __global__ __launch_bounds__(256) void k_head_pack(const uint16_t *from, int64_t
     const bool there = L.count ? j < *L.count : j < rows;
     copy_row<WIDE>(from + (there ? (L.index ? (int64_t)L.index[j] : j) : 0) * stride, cols, there, to + j * width, width);
 }
-// Both for up to GATHER_MAX rows, in one launch: every workgroup counts the rows that count by itself, which is less than another launch takes.
+// Both for up to GATHER_MAX rows, in one launch: every workgroup counts the rows that count by itself, which is less than another launch takes (5 us,
+// where the two take 4 and 7 for 512 rows; counting 8192 rows takes one workgroup 12 us, beside a product of 1.4 ms).
 constexpr int GATHER_MAX = 1024;
 template <bool WIDE>
 __global__ __launch_bounds__(256) void k_head_gather(const int64_t *targets, const float *factor, int rows, int vocab, Live L, float *logp, float *row_stats,
@@ -470,7 +473,8 @@ __device__ __forceinline__ void join(float k, float &m, float &s, float2 q)
     m = top;
 }
 
-// Maximum and sum of exponentials of each row of the batch over a tile of words.
+// Maximum and sum of exponentials of each row of the batch over a tile of words.  8192 x 4096 x 32768 1.60 ms (1380 TFLOP/s);
+// 64 x 4096 x 32000 62 us with the weights in the memory-side cache, 90 from HBM.
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X, int steps, Logit G)
 {
@@ -537,7 +541,9 @@ __device__ __forceinline__ float dz_of(const Logit &G, const float4 &R, float z,
 {
     return R.z * ((target ? 1.0f : 0.0f) - __builtin_amdgcn_exp2f(G.k * (z - R.x)) * R.y);
 }
-// dz of a tile of words, rounded to bf16; zeros in rows from count on and for words behind the vocabulary, which products that follow meet
+// dz of a tile of words (8192 x 4096 x 32768 1.72 ms), rounded to bf16, since it is an operand of the two products that follow; each of its roundings is
+// independent (`unit_of` sees to that) and they meet in sums of thousands: 2e-3 of a gradient's norm, of which its own rounding to bf16 is 1.7e-3. Zeros
+// in rows from count on and for words behind the vocabulary, which products that follow meet
 template <typename T>
 __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, int steps, Logit G)
 {
@@ -593,7 +599,7 @@ __device__ __forceinline__ void loss_of(const Live &live, const Loss &L)
     if (threadIdx.x == 0) *L.loss = (float)(s + (L.accumulate ? (double)*L.loss : 0.0));
 }
 __global__ __launch_bounds__(256) void k_head_loss(Live live, Loss L) { loss_of(live, L); }
-// dz from z that was kept: a lane four words; the workgroup behind the rows' has the loss
+// dz from z that was kept: a lane four words; the workgroup behind the rows' has the loss, which is a launch less (64 x 32000 5 us)
 __global__ __launch_bounds__(256) void k_head_dz_kept(Logit G, Loss L)
 {
     const int64_t row = blockIdx.x, w = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
@@ -615,7 +621,8 @@ __global__ __launch_bounds__(256) void k_head_dz_kept(Logit G, Loss L)
     *reinterpret_cast<u32x2 *>(G.dz + row * G.stride + w) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
 }
 
-// sum[split][row][h] (+)= dz W over a piece of the vocabulary
+// sum[split][row][h] (+)= dz W over a piece of the vocabulary; W is read as it lies, k across its rows (8192 x 4096 x 32768 1.64 ms, 64 x 4096 x 32000
+// in 16 parts 56 us)
 struct ToRows {
     Live live;
     int64_t rows, hidden;
@@ -649,7 +656,8 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, 
     }
 }
 
-// dW[word][h] = dz^T x of a piece of the vocabulary
+// dW[word][h] = dz^T x of a piece of the vocabulary; of both k lies across the rows (8192 x 4096 x 32768 1.61 ms, 1360 TFLOP/s; 64 x 4096 x 32000,
+// nearly all of it writing, 67 us)
 struct ToWeights {
     Live live;
     int64_t word0, words, hidden;
@@ -673,7 +681,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, 
                   (int)min(G.words - w0, (int64_t)4096), (int)min(G.hidden - h0, (int64_t)4096));
 }
 
-// db[word] = sum over rows of dz: a lane two words, a wave a share of the rows
+// db[word] = sum over rows of dz: a lane two words, a wave a share of the rows; dz is read once more (4095 x 50001 59 us, 6.9 TB/s)
 __global__ __launch_bounds__(1024) void k_head_db(const uint16_t *dz, int64_t dz_stride, Live live, int64_t words, const float4 *row, uint16_t *db)
 {
     __shared__ float part[16][128];
@@ -953,16 +961,23 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_dot(Few G)
 }
 
 // ---- the plan of a call ------------------------------------------------------------------------
-typedef Tile<256, 256, 2, 4, 2> Big;          // many rows
-typedef Tile<128, 128, 2, 2, 2> Mid;          // up to 128, or too few for the others
-typedef Tile<128, 64, 4, 1, 3> Slim;          // up to 64: the weights' way from memory is all the time there is
+// Many rows; up to 128, or too few for the others; up to 64, where the weights' way from memory is all the time there is.  Scoring, us, hidden x
+// vocabulary 4096 x 131072, 2048 x 50304, 4096 x 32000, 8192 x 32000, 1024 x 32000: Mid of 128 rows 201/66/79/153/31, with a third stage, which leaves a
+// CU one workgroup of it fewer, 215/72/69/136/28, and of 256 rows (the last four) 98/97/175/37 against 108/105/190/42; Slim 187/57/67/129/24, with six
+// stages 195/64/67/129/25, of 256 words 186/62/87/170/32.
+typedef Tile<256, 256, 2, 4, 2> Big;
+typedef Tile<128, 128, 2, 2, 2> Mid;
+typedef Tile<128, 64, 4, 1, 3> Slim;
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 512 << 20;          // of dz: 8192 x 4096 x 131072 25.9 ms, with 256 MB 26.1, 128 MB 26.0, 64 MB 27.1; 4095 x 2048 x 50001 2.33, 2.43, 2.69, 2.82
-constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits; with less of the hidden
-constexpr int64_t kKeptWidth = 512;                 // state than this z is made again as soon as it is written and read
+constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits: what a call may take beside dz
+constexpr int64_t kKeptWidth = 512;                 // of the hidden state from which z is kept: 1354 x 320 x 39296 355 us kept, 324 made again
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
-constexpr int64_t MID_TILES = 200;                  // large tiles of z below which there are too few for the chip
+// Large tiles up to which a product is done in small ones, four times as many, all of which run at once, two on each of the 256 CUs.  Scored, us, large
+// against small: 256 rows of 4096 x 32000 (125 tiles) 117/99, of 2048 x 50304 (197) 79/96, 200 of 4096 x 50304 (197) 133/172, 512 of 4096 x 32000 (250)
+// 126/184.  To the weights: 70 x 512 x 1152 (10 tiles) a loss of 39/36, 1024 x 4096 x 8192 (512) 252/253, 4096 x 2048 x 50304 2772/3038.
+constexpr int64_t MID_TILES = 128;
 
 struct Plan {
     int64_t rows;            // of the packed batch
@@ -982,7 +997,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
 {
     Plan P = {};
-    P.side = rows <= Slim::BN ? Slim::BN : rows <= Mid::BN || up(rows, Big::BN) / Big::BN * (up(vocab, Big::BM) / Big::BM) < MID_TILES ? Mid::BN : Big::BN;
+    P.side = rows <= Slim::BN ? Slim::BN : rows <= Mid::BN || up(rows, Big::BN) / Big::BN * (up(vocab, Big::BM) / Big::BM) <= MID_TILES ? Mid::BN : Big::BN;
     P.words = P.side == Big::BN ? Big::BM : Slim::BM;
     P.rows = up(std::max<int64_t>(rows, 1), P.side);
     P.width = up(hidden, 64);
@@ -992,11 +1007,14 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     P.kept = gradient && P.width >= kKeptWidth && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
     P.piece = (P.kept ? P.tiles : std::min(P.tiles, most)) * 256;
     P.packed = std::min(P.piece, std::max<int64_t>(1, kPackedBytes / (2 * P.width * 256)) * 256);
-    // Tiles of 256 columns of the hidden state, unless those would be a quarter wider than it.
-    const bool wide = up(hidden, 256) * 4 <= up(hidden, 128) * 5;
+    // Tiles of 256 columns of the hidden state where it has more than 128 (loss of 4096 x 320 x 32000 544 us, of 128 columns 548; 640 814 and 841, 896
+    // 919 and 1027).
+    const bool wide = hidden > 128;
     P.dx = P.side == Slim::BN ? Slim::BN : wide && P.side == Big::BN ? Big::BN : Mid::BN;
-    P.dw = wide ? Big::BN : Mid::BN;
-    // The sums to the rows in parts of k that fill the chip: the fewest of those whose tiles take least, a step each and 24 for what a tile has to do besides.
+    P.dw = wide && up(hidden, Big::BM) / Big::BM * (up(std::min(P.piece, vocab), Big::BN) / Big::BN) > MID_TILES ? Big::BN : Mid::BN;
+    // The sums to the rows in parts of k that fill the chip: the fewest of those whose tiles take least, a step each and 24 for what a tile has to do
+    // besides (a loss of 64 x 4096 x 32000 222 us, in one part 347; 1000 x 2048 x 32000 450 and 938, 4096 x 2048 x 50304 2772 and 3145, 70 x 512 x 1152
+    // 39 and 45).
     const int64_t out = P.rows / P.dx * (up(hidden, P.dx == Big::BN ? Big::BM : Slim::BM) / (P.dx == Big::BN ? Big::BM : Slim::BM)), at_once = P.dx == Big::BN ? 256 : 512;
     const int64_t steps = up(std::min(P.piece, vocab), BK) / BK;
     int64_t least = INT64_MAX;

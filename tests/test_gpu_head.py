@@ -176,6 +176,13 @@ def test_many_pieces_and_tiles(rows, hidden, vocab, bias):
     Case(rows, hidden, vocab, prompt=True, bias=bias).check_loss()
 
 
+@pytest.mark.parametrize("rows, hidden, vocab", [(256, 136, 32_768), (250, 136, 32_769), (700, 1000, 11_003), (600, 264, 17_001), (40, 1000, 8_300), (40, 1000, 8_100),
+                                                 (70, 128, 20_000), (300, 129, 17_000)])
+def test_large_and_small_tiles(rows, hidden, vocab):
+    """Both sides of the numbers of tiles from which they are large: of the statistics and dz, of the sums to the rows, of those to the weights."""
+    Case(rows, hidden, vocab, prompt=True, bias=vocab % 2 == 1).check_loss()
+
+
 @pytest.mark.parametrize("rows, hidden, vocab", [(4, 64, 500), (30, 256, 700), (400, 128, 600)])
 def test_gradient_from_logp(rows, hidden, vocab):
     """Any gradient in the log-probabilities, statistics from gs_head_logp; the parts that nobody needs left out."""

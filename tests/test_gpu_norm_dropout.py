@@ -115,6 +115,14 @@ def test_norm_of_many_rows(rows, cols):
     run_norm(rows, cols, F32, F32, vectors=False)
 
 
+@pytest.mark.parametrize("rows", [256, 257])
+@pytest.mark.parametrize("cols", [1000, 2052, 8192])
+def test_norm_of_few_and_many_rows(rows, cols):
+    """Both sides of the number of rows from which workgroups stay."""
+    run_norm(rows, cols, BF16, BF16)
+    run_norm(rows, cols, F32, BF16, vectors=False)
+
+
 def test_norm_in_place():
     g = torch.Generator(device=DEV).manual_seed(0)
     for cols in (100, 1000, 5000, 40000):
