@@ -5,7 +5,7 @@
 // All the work is in products of matrices: 2 N V H operations for the log-probabilities and 8 N V H with the gradient (2 of them to make
 // z again), on the matrix cores.  rows x hidden x vocabulary: 8192 x 2048 x 50304 scored in 1.34 ms (1262 TFLOP/s), 8192 x 4096 x 131072 with its gradients
 // 26.5 ms (1330 TFLOP/s), 4095 x 2048 x 50001 with a bias 2.33 ms; with few rows memory is the bound: one of 4096 x 131072 scored in 161 us (7.0 TB/s of weights),
-// 64 x 4096 x 32000 with gradients 222 us.
+// 64 x 4096 x 32000 with gradients 212 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -244,10 +244,10 @@ __device__ __forceinline__ int column_of(int lane) { return lane & 15; }
 // Tiles in groups along the first dimension, dealt so that each of the 8 dies has neighbours: its 32 CUs work on about 4 x 8 tiles at a time, whose
 // operands its L2 holds.  (8 at a time 1 % behind; where all the work is to write rows of results, 4 are 4 % behind.)  false: no tile.
 template <int GROUP = 4>
-__device__ __forceinline__ bool my_tile(int64_t tiles1, int64_t tiles2, int64_t &t1, int64_t &t2)
+__device__ __forceinline__ bool my_tile(uint32_t id, int64_t tiles1, int64_t tiles2, int64_t &t1, int64_t &t2)
 {
     // a launch has fewer than 2^32 work items, and so fewer than 2^24 tiles
-    const uint32_t second = (uint32_t)tiles2, all = (uint32_t)tiles1 * second, per = (all + 7) / 8, id = blockIdx.x, t = (id & 7) * per + (id >> 3);
+    const uint32_t second = (uint32_t)tiles2, all = (uint32_t)tiles1 * second, per = (all + 7) / 8, t = (id & 7) * per + (id >> 3);
     if ((id >> 3) >= per || t >= all) return false;
     const uint32_t group = t / (GROUP * second), in = t - group * GROUP * second, left = (uint32_t)tiles1 - group * GROUP, width = left < GROUP ? left : GROUP;
     t1 = __builtin_amdgcn_readfirstlane((int)(group * GROUP + in % width));
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_stats(Operand W, Operand X
 {
     __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, tr;
-    if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
+    if (!my_tile(blockIdx.x, (G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dz(Operand W, Operand X, i
 {
     __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, tr;
-    if (!my_tile((G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
+    if (!my_tile(blockIdx.x, (G.words + T::BM - 1) / T::BM, G.rows / T::BN, tw, tr)) return;
     const int count = *G.live.count;
     if (tr * T::BN >= count) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
@@ -621,8 +621,7 @@ __global__ __launch_bounds__(256) void k_head_dz_kept(Logit G, Loss L)
     *reinterpret_cast<u32x2 *>(G.dz + row * G.stride + w) = u32x2{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
 }
 
-// sum[split][row][h] (+)= dz W over a piece of the vocabulary; W is read as it lies, k across its rows (8192 x 4096 x 32768 1.64 ms, 64 x 4096 x 32000
-// in 16 parts 56 us)
+// sum[split][row][h] (+)= dz W over a piece of the vocabulary; W is read as it lies, k across its rows (8192 x 4096 x 32768 1.64 ms)
 struct ToRows {
     Live live;
     int64_t rows, hidden;
@@ -631,13 +630,12 @@ struct ToRows {
     int splits, steps;        // steps: of the piece
 };
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, ToRows G)
+__device__ __forceinline__ void dx_tile(const Operand &W, const Operand &DZ, const ToRows &G, uint32_t id, int split, char *lds)
 {
-    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tr, th;
-    if (!my_tile(G.rows / T::BN, (G.hidden + T::BM - 1) / T::BM, tr, th)) return;
+    if (!my_tile(id, G.rows / T::BN, (G.hidden + T::BM - 1) / T::BM, tr, th)) return;
     if (tr * T::BN >= *G.live.count) return;
-    const int per = (G.steps + G.splits - 1) / G.splits, from = blockIdx.y * per, mine = G.steps - from < per ? G.steps - from : per;
+    const int per = (G.steps + G.splits - 1) / G.splits, from = split * per, mine = G.steps - from < per ? G.steps - from : per;
     f32x4 acc[T::MI][T::NI];
     product<T, false, true, true>(W, DZ, th * T::BM, tr * T::BN, (int64_t)from * BK, mine, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / T::WN, wn = wave % T::WN;
@@ -645,7 +643,7 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, 
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) {
         const int64_t row = tr * T::BN + (wn * T::NI + j) * 16 + column_of(lane);
-        float *out = G.sum + ((int64_t)blockIdx.y * G.rows + row) * G.hidden;          // hidden: of the sums' rows, a multiple of 4
+        float *out = G.sum + ((int64_t)split * G.rows + row) * G.hidden;          // hidden: of the sums' rows, a multiple of 4
 #pragma unroll
         for (int i = 0; i < T::MI; ++i) {
             const int64_t h = h0 + i * 16;
@@ -655,9 +653,14 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, 
         }
     }
 }
+template <typename T>
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dx(Operand W, Operand DZ, ToRows G)
+{
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
+    dx_tile<T>(W, DZ, G, blockIdx.x, (int)blockIdx.y, lds);
+}
 
-// dW[word][h] = dz^T x of a piece of the vocabulary; of both k lies across the rows (8192 x 4096 x 32768 1.61 ms, 1360 TFLOP/s; 64 x 4096 x 32000,
-// nearly all of it writing, 67 us)
+// dW[word][h] = dz^T x of a piece of the vocabulary; of both k lies across the rows (8192 x 4096 x 32768 1.61 ms, 1360 TFLOP/s)
 struct ToWeights {
     Live live;
     int64_t word0, words, hidden;
@@ -666,11 +669,10 @@ struct ToWeights {
     const float4 *row;
 };
 template <typename T>
-__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, ToWeights G)
+__device__ __forceinline__ void dw_tile(const Operand &X, const Operand &DZ, const ToWeights &G, uint32_t id, char *lds)
 {
-    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     int64_t tw, th;
-    if (!my_tile<8>((G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
+    if (!my_tile<8>(id, (G.words + T::BN - 1) / T::BN, (G.hidden + T::BM - 1) / T::BM, tw, th)) return;
     f32x4 acc[T::MI][T::NI];
     const int count = *G.live.count;
     product<T, false, false, false>(X, DZ, th * T::BM, tw * T::BN, 0, (count + BK - 1) / BK, lds, acc);
@@ -679,6 +681,28 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, 
     const int64_t w0 = tw * T::BN + wn * T::NI * 16, h0 = th * T::BM + wm * T::MI * 16;
     store_rows<T>(lds, wave, lane, [&](int i, int j, int r) { return acc[i][j][r] * unit; }, G.dw + (G.word0 + w0) * G.stride + h0, G.stride,
                   (int)min(G.words - w0, (int64_t)4096), (int)min(G.hidden - h0, (int64_t)4096));
+}
+template <typename T>
+__global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, ToWeights G)
+{
+    __shared__ __attribute__((aligned(128))) char lds[T::LDS];
+    dw_tile<T>(X, DZ, G, blockIdx.x, lds);
+}
+// Both of few rows, in one launch: the sums to the rows read all weights and write little, those to the weights read little and write as much.  The first
+// `dx` workgroups (`dx` / splits of each part) have the rows, about one on each CU; the others come and go beside them.  Losses, us, against two launches: 64 x 4096 x 32000
+// 212/221, 128 x 4096 x 50304 361/384, 120 x 2048 x 8192 65/77, 70 x 512 x 1152 31/36, 1 x 4864 x 7680 93/102, 300 x 8192 x 10000 290/285.  Large tiles leave no room on a CU
+// for another workgroup.
+template <typename TX, typename TW>
+__global__ __launch_bounds__(TX::BLOCK, 2) void k_head_dx_dw(Operand W, Operand X, Operand DZ, ToRows R, ToWeights G, uint32_t dx)
+{
+    static_assert(TX::BLOCK == TW::BLOCK, "one launch");
+    __shared__ __attribute__((aligned(128))) char lds[TX::LDS > TW::LDS ? TX::LDS : TW::LDS];
+    if (blockIdx.x < dx) {
+        const uint32_t per = dx / (uint32_t)R.splits, split = blockIdx.x / per;
+        dx_tile<TX>(W, DZ, R, blockIdx.x - split * per, (int)split, lds);
+    } else {
+        dw_tile<TW>(X, DZ, G, blockIdx.x - dx, lds);
+    }
 }
 
 // db[word] = sum over rows of dz: a lane two words, a wave a share of the rows; dz is read once more (4095 x 50001 59 us, 6.9 TB/s)
@@ -976,7 +1000,7 @@ constexpr int64_t kKeptWidth = 512;                 // of the hidden state from 
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
 // Large tiles up to which a product is done in small ones, four times as many, all of which run at once, two on each of the 256 CUs.  Scored, us, large
 // against small: 256 rows of 4096 x 32000 (125 tiles) 117/99, of 2048 x 50304 (197) 79/96, 200 of 4096 x 50304 (197) 133/172, 512 of 4096 x 32000 (250)
-// 126/184.  To the weights: 70 x 512 x 1152 (10 tiles) a loss of 39/36, 1024 x 4096 x 8192 (512) 252/253, 4096 x 2048 x 50304 2772/3038.
+// 126/184.  To the weights, a loss: 1024 x 4096 x 8192 (512) 252/253, 4096 x 2048 x 50304 2772/3038.
 constexpr int64_t MID_TILES = 128;
 
 struct Plan {
@@ -1013,9 +1037,8 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     P.dx = P.side == Slim::BN ? Slim::BN : wide && P.side == Big::BN ? Big::BN : Mid::BN;
     P.dw = wide && up(hidden, Big::BM) / Big::BM * (up(std::min(P.piece, vocab), Big::BN) / Big::BN) > MID_TILES ? Big::BN : Mid::BN;
     // The sums to the rows in parts of k that fill the chip: the fewest of those whose tiles take least, a step each and 24 for what a tile has to do
-    // besides (a loss of 64 x 4096 x 32000 222 us, in one part 347; 1000 x 2048 x 32000 450 and 938, 4096 x 2048 x 50304 2772 and 3145, 70 x 512 x 1152
-    // 39 and 45).
-    const int64_t out = P.rows / P.dx * (up(hidden, P.dx == Big::BN ? Big::BM : Slim::BM) / (P.dx == Big::BN ? Big::BM : Slim::BM)), at_once = P.dx == Big::BN ? 256 : 512;
+    // besides (a loss of 1000 x 2048 x 32000 450 us, in one part 938; 4096 x 2048 x 50304 2772 and 3145).
+    const int64_t out = P.rows / P.dx * (up(hidden, P.dx == Big::BN ? Big::BM : Slim::BM) / (P.dx == Big::BN ? Big::BM : Slim::BM)), at_once = 256;
     const int64_t steps = up(std::min(P.piece, vocab), BK) / BK;
     int64_t least = INT64_MAX;
     for (int s = 1; s <= 32 && s * 4 <= std::max<int64_t>(steps, 4); ++s) {
@@ -1196,6 +1219,11 @@ template <typename T> static void launch_dw(const Call &C, const Operand &X, con
 {
     k_head_dw<T><<<grid_of(up(R.words, T::BN) / T::BN * (up(R.hidden, T::BM) / T::BM)), T::BLOCK, 0, C.stream>>>(X, DZ, R);
 }
+template <typename T> static void launch_dx_dw(const Call &C, const Operand &W, const Operand &X, const Operand &DZ, const ToRows &R, const ToWeights &G)
+{
+    const uint32_t dx = grid_of(C.P.rows / T::BN * (up(C.P.width, T::BM) / T::BM)) * (uint32_t)C.P.splits;
+    k_head_dx_dw<T, Mid><<<dx + grid_of(up(G.words, Mid::BN) / Mid::BN * (up(G.hidden, Mid::BM) / Mid::BM)), T::BLOCK, 0, C.stream>>>(W, X, DZ, R, G, dx);
+}
 template <typename T> static void launch_dz(const Call &C, const Operand &W, const Operand &X, const Logit &G)
 {
     k_head_dz<T><<<grid_of(up(G.words, T::BM) / T::BM * (C.P.rows / T::BN)), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), G);
@@ -1212,14 +1240,14 @@ static hipError_t backward(const Call &C, const gs_head_grads &D, bool after_for
         if (have_z) k_head_dz_kept<<<dim3((uint32_t)P.rows + 1, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G, w == 0 ? loss : Loss{});
         else (P.side == Slim::BN ? launch_dz<Slim> : P.side == Mid::BN ? launch_dz<Mid> : launch_dz<Big>)(C, W, X, G);
         const Operand DZ = {C.dz(), P.piece, P.rows, P.piece};
-        if (D.dx) {
-            const ToRows R = {C.live, P.rows, P.width, C.sum(), w == 0, P.splits, (int)(up(words, BK) / BK)};
+        const ToRows R = {C.live, P.rows, P.width, C.sum(), w == 0, P.splits, (int)(up(words, BK) / BK)};
+        const ToWeights E = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : C.h.hidden, C.row()};
+        if (D.dx && D.dw && P.side < Big::BN) {
+            (P.dx == Slim::BN ? launch_dx_dw<Slim> : launch_dx_dw<Mid>)(C, W, X, DZ, R, E);
+        } else if (D.dx) {
             (P.dx == Slim::BN ? launch_dx<Slim> : P.dx == Mid::BN ? launch_dx<Mid> : launch_dx<Big>)(C, W, DZ, R);
         }
-        if (D.dw) {
-            const ToWeights R = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : C.h.hidden, C.row()};
-            (P.dw == Mid::BN ? launch_dw<Mid> : launch_dw<Big>)(C, X, DZ, R);
-        }
+        if (D.dw && !(D.dx && P.side < Big::BN)) (P.dw == Mid::BN ? launch_dw<Mid> : launch_dw<Big>)(C, X, DZ, E);
         if (D.dbias) k_head_db<<<(uint32_t)((words + 127) / 128), 1024, 0, C.stream>>>(C.dz(), P.piece, C.live, words, C.row(), D.dbias + w);
         return hipGetLastError();
     });
