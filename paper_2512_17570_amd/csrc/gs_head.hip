@@ -992,6 +992,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_dot(Few G)
 typedef Tile<256, 256, 2, 4, 2> Big;
 typedef Tile<128, 128, 2, 2, 2> Mid;
 typedef Tile<128, 64, 4, 1, 3> Slim;
+typedef Tile<64, 64, 2, 2, 3> Tiny;           // up to 64 rows and so few words that those would leave CUs without work
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 512 << 20;          // of dz: 8192 x 4096 x 131072 25.9 ms, with 256 MB 26.1, 128 MB 26.0, 64 MB 27.1; 4095 x 2048 x 50001 2.33, 2.43, 2.69, 2.82
@@ -1002,6 +1003,9 @@ constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be
 // against small: 256 rows of 4096 x 32000 (125 tiles) 117/99, of 2048 x 50304 (197) 79/96, 200 of 4096 x 50304 (197) 133/172, 512 of 4096 x 32000 (250)
 // 126/184.  To the weights, a loss: 1024 x 4096 x 8192 (512) 252/253, 4096 x 2048 x 50304 2772/3038.
 constexpr int64_t MID_TILES = 128;
+// The same up to 64 rows: 64 x 4096 x 16000 (125 tiles of 128 words) scored in 48 us against 40, 64 x 4096 x 8000 29/25, 1 x 4864 x 7680 a loss of 93/83; 32 x 4096 x 24000 (188) 54/57,
+// 64 x 4096 x 32000 (250) level.
+constexpr int64_t TINY_WORDS = MID_TILES * Slim::BM;
 
 struct Plan {
     int64_t rows;            // of the packed batch
@@ -1022,7 +1026,7 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
 {
     Plan P = {};
     P.side = rows <= Slim::BN ? Slim::BN : rows <= Mid::BN || up(rows, Big::BN) / Big::BN * (up(vocab, Big::BM) / Big::BM) <= MID_TILES ? Mid::BN : Big::BN;
-    P.words = P.side == Big::BN ? Big::BM : Slim::BM;
+    P.words = P.side == Big::BN ? Big::BM : P.side == Slim::BN && vocab <= TINY_WORDS ? Tiny::BM : Slim::BM;
     P.rows = up(std::max<int64_t>(rows, 1), P.side);
     P.width = up(hidden, 64);
     P.tiles = up(vocab, 256) / 256;
@@ -1174,7 +1178,7 @@ static hipError_t forward(const Call &C, float *logp, float *row_stats, const fl
 }
 static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
 {
-    return (C.P.side == Slim::BN ? forward<Slim> : C.P.side == Mid::BN ? forward<Mid> : forward<Big>)(C, logp, row_stats, row_weights, gradient);
+    return (C.P.words == Tiny::BM ? forward<Tiny> : C.P.side == Slim::BN ? forward<Slim> : C.P.side == Mid::BN ? forward<Mid> : forward<Big>)(C, logp, row_stats, row_weights, gradient);
 }
 template <int R> static void launch_dot(const Few &G, uint32_t grid, hipStream_t stream)
 {
@@ -1238,7 +1242,7 @@ static hipError_t backward(const Call &C, const gs_head_grads &D, bool after_for
     hipError_t e = pieces(C, after_forward, [&](int64_t w, int64_t words, const Operand &W) {
         const Logit G = logit_of(C, w, words);
         if (have_z) k_head_dz_kept<<<dim3((uint32_t)P.rows + 1, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G, w == 0 ? loss : Loss{});
-        else (P.side == Slim::BN ? launch_dz<Slim> : P.side == Mid::BN ? launch_dz<Mid> : launch_dz<Big>)(C, W, X, G);
+        else (P.words == Tiny::BM ? launch_dz<Tiny> : P.side == Slim::BN ? launch_dz<Slim> : P.side == Mid::BN ? launch_dz<Mid> : launch_dz<Big>)(C, W, X, G);
         const Operand DZ = {C.dz(), P.piece, P.rows, P.piece};
         const ToRows R = {C.live, P.rows, P.width, C.sum(), w == 0, P.splits, (int)(up(words, BK) / BK)};
         const ToWeights E = {C.live, w, words, C.h.hidden, D.dw, C.h.vocab > 1 ? D.dw_stride : C.h.hidden, C.row()};

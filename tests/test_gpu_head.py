@@ -183,6 +183,16 @@ def test_large_and_small_tiles(rows, hidden, vocab):
     Case(rows, hidden, vocab, prompt=True, bias=vocab % 2 == 1).check_loss()
 
 
+@pytest.mark.parametrize("rows, hidden, vocab", [(40, 1000, 16_384), (40, 264, 16_385), (33, 100, 17_003), (64, 600, 20_001), (17, 64, 33_000)])
+def test_narrow_tiles(rows, hidden, vocab):
+    """Up to 64 rows, both sides of the number of words from which their tiles are of 128."""
+    c = Case(rows, hidden, vocab, prompt=True, bias=vocab % 2 == 1)
+    got = c.score(0.7)
+    out, bound = oracle(c.x, c.w, c.bias, c.targets, None, 0.7, gradient=False)
+    check(got, out, bound, ["logp", "M", "S"])
+    c.check_loss(0.7)
+
+
 @pytest.mark.parametrize("rows, hidden, vocab", [(4, 64, 500), (30, 256, 700), (400, 128, 600)])
 def test_gradient_from_logp(rows, hidden, vocab):
     """Any gradient in the log-probabilities, statistics from gs_head_logp; the parts that nobody needs left out."""
