@@ -688,10 +688,11 @@ __global__ __launch_bounds__(T::BLOCK, 2) void k_head_dw(Operand X, Operand DZ, 
     __shared__ __attribute__((aligned(128))) char lds[T::LDS];
     dw_tile<T>(X, DZ, G, blockIdx.x, lds);
 }
-// Both of few rows, in one launch: the sums to the rows read all weights and write little, those to the weights read little and write as much.  The first
-// `dx` workgroups (`dx` / splits of each part) have the rows, about one on each CU; the others come and go beside them.  Losses, us, against two launches: 64 x 4096 x 32000
-// 212/221, 128 x 4096 x 50304 361/384, 120 x 2048 x 8192 65/77, 70 x 512 x 1152 31/36, 1 x 4864 x 7680 93/102, 300 x 8192 x 10000 290/285.  Large tiles leave no room on a CU
-// for another workgroup.
+// Both of few rows, in one launch: the sums to the rows read all weights and write little, those to the weights read little and write as much.  The
+// first `dx` workgroups (`dx` / splits of each part) have the rows, about one on each CU; the others come and go beside them.  Losses, us, against
+// two launches: 64 x 4096 x 32000 212/221, 128 x 4096 x 50304 361/384, 120 x 2048 x 8192 65/77, 70 x 512 x 1152 31/36, 1 x 4864 x 7680 93/102, 300 x
+// 8192 x 10000 290/285.  With up to 512 workgroups for the rows the first two take 222 and 373, with the rows' dealt evenly between the others 233
+// and 429.  Large tiles leave no room on a CU for another workgroup.
 template <typename TX, typename TW>
 __global__ __launch_bounds__(TX::BLOCK, 2) void k_head_dx_dw(Operand W, Operand X, Operand DZ, ToRows R, ToWeights G, uint32_t dx)
 {
