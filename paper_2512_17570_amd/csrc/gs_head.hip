@@ -63,7 +63,8 @@ struct Operand {
 };
 
 // 16 bytes a lane from base + offset to LDS (from `lds` + AT on), one lane's behind another's.  By hand because the compiler holds every transposing read back until all loads on
-// their way to LDS have come; nothing is returned in registers, and who reads waits for vmcnt and a barrier.
+// their way to LDS have come; nothing is returned in registers, and who reads waits for vmcnt and a barrier.  m0 is none of the registers that the compiler has values in, and
+// it takes no note of it as written (it is reserved): it would have it for uses of its own, of which these kernels have none (a test looks).
 template <int AT>
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
