@@ -661,10 +661,12 @@ typedef struct {
     int64_t dx_stride, dw_stride;
 } gs_head_grads;
 
-/* Bytes of device workspace that the calls below need for such a head, with or without a gradient; 0 for sizes that they refuse.
+/* Bytes of device workspace that the calls below need for such a head, with or without a gradient; 0 for sizes that they refuse.  gs_head_logp_grad
+ * does with less than a loss with its gradient where that keeps z, and gs_head_logp always does with what gs_head_logp_grad needs.
  * The workspace is aligned to 256 bytes; nothing has to be in it before, and nothing is kept in it from call to call.  Calls that may run at the same time
  * (on two streams, or captured into graphs that do) need one each. */
 size_t gs_head_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab, int gradient);
+size_t gs_head_logp_grad_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab);
 
 /* gs_token_logp of a head's rows: scoring of sequences, or of the token just drawn (rows == 1). */
 gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temperature, float *logp, float *row_stats, void *d_workspace,

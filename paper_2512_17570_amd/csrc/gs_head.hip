@@ -1015,6 +1015,7 @@ typedef Tile<64, 64, 2, 2, 3> Tiny;           // up to 64 rows and so few words 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 512 << 20;          // of dz: 8192 x 4096 x 131072 25.9 ms, with 256 MB 26.1, 128 MB 26.0, 64 MB 27.1; 4095 x 2048 x 50001 2.33, 2.43, 2.69, 2.82
 constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits: what a call may take beside dz
+static_assert(kKeptBytes <= 2 * kPieceBytes, "of a batch whose z is kept, dz is one piece");
 constexpr int64_t kKeptWidth = 512;                 // of the hidden state from which z is kept: 1354 x 320 x 39296 355 us kept, 324 made again
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
 // Large tiles up to which a product is done in small ones, four times as many, all of which run at once, two on each of the 256 CUs.  Scored, us, large
@@ -1039,9 +1040,12 @@ struct Plan {
     size_t index, x, partials, target, row, z, dz, sum, w, all;      // places in the workspace, and its size
 };
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+// A call without a gradient; with one, from the caller's statistics; with one behind a forward pass of its own, which is what can keep z.
+enum Work { SCORES, GRADIENT, LOSS };
 // Packed weights are reckoned with in any case: their alignment is not known when the size is asked for.
-static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
+static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, Work work)
 {
+    const bool gradient = work != SCORES;
     Plan P = {};
     P.side = rows <= Slim::BN ? Slim::BN : rows <= Mid::BN || up(rows, Big::BN) / Big::BN * (up(vocab, Big::BM) / Big::BM) <= MID_TILES ? Mid::BN : Big::BN;
     P.words = P.side == Big::BN ? Big::BM : P.side == Slim::BN && vocab <= TINY_WORDS ? Tiny::BM : Slim::BM;
@@ -1050,8 +1054,8 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     P.tiles = up(vocab, 256) / 256;
     P.joined = up(vocab, P.words) / P.words;
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * P.rows * 256));
-    P.kept = gradient && P.width >= kKeptWidth && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
-    P.piece = (P.kept ? P.tiles : std::min(P.tiles, most)) * 256;
+    P.kept = work == LOSS && P.width >= kKeptWidth && P.rows * P.tiles * 256 * 4 <= kKeptBytes;
+    P.piece = std::min(P.tiles, most) * 256;              // all of them where z is kept
     P.packed = std::min(P.piece, std::max<int64_t>(1, kPackedBytes / (2 * P.width * 256)) * 256);
     // Tiles of 256 columns of the hidden state where it has more than 128 (loss of 4096 x 320 x 32000 544 us, of 128 columns 548; 640 814 and 841, 896
     // 919 and 1027).
@@ -1078,10 +1082,10 @@ static Plan plan_of(int64_t rows, int64_t hidden, int64_t vocab, bool gradient)
     P.partials = take(std::max(P.joined * P.rows, rows <= FEW_ROWS ? up(vocab, FEW_WORDS) / FEW_WORDS * FEW_ROWS : 0) * 8);
     P.target = take(P.rows * 4);
     P.row = take(P.rows * 16);
-    P.z = P.kept ? take(P.rows * P.tiles * 256 * 4) : at;
     P.dz = gradient ? take(P.rows * P.piece * 2) : at;
     P.sum = gradient ? take(P.splits * P.rows * P.width * 4) : at;
     P.w = take(P.packed * P.width * 2);
+    P.z = P.kept ? take(P.rows * P.tiles * 256 * 4) : at;
     P.all = at;
     return P;
 }
@@ -1106,13 +1110,13 @@ struct Call {
 
 static bool multiple16(const void *p, int64_t stride) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(stride * 2)) & 15) == 0; }
 
-static Call call_of(const gs_head &h, const int64_t *targets, float temperature, bool gradient, void *ws, void *stream)
+static Call call_of(const gs_head &h, const int64_t *targets, float temperature, Work work, void *ws, void *stream)
 {
     Call C = {};
     C.h = h;
     if (h.rows <= 1) C.h.x_stride = h.hidden;
     if (h.vocab <= 1) C.h.w_stride = h.hidden;
-    C.P = plan_of(h.rows, h.hidden, h.vocab, gradient);
+    C.P = plan_of(h.rows, h.hidden, h.vocab, work);
     C.ws = static_cast<char *>(ws);
     C.targets = targets;
     C.it = 1.0f / temperature;
@@ -1347,7 +1351,13 @@ extern "C" {
 size_t gs_head_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab, int gradient)
 {
     if (!good_sizes(rows, hidden, vocab)) return 0;
-    return plan_of(rows, hidden, vocab, gradient != 0).all;
+    return plan_of(rows, hidden, vocab, gradient ? LOSS : SCORES).all;
+}
+
+size_t gs_head_logp_grad_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab)
+{
+    if (!good_sizes(rows, hidden, vocab)) return 0;
+    return plan_of(rows, hidden, vocab, GRADIENT).all;
 }
 
 gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temperature, float *logp, float *row_stats, void *d_workspace,
@@ -1365,7 +1375,7 @@ gs_status gs_head_logp(const gs_head *head, const int64_t *targets, float temper
     R.add(row_stats, rows * 8, true);
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
-    const Call C = call_of(*head, targets, temperature, false, d_workspace, stream);
+    const Call C = call_of(*head, targets, temperature, SCORES, d_workspace, stream);
     hipError_t e;
     if (few_rows(rows, head->hidden, head->vocab)) {
         e = forward_few(C, logp, row_stats);
@@ -1382,7 +1392,7 @@ gs_status gs_head_logp_grad(const gs_head *head, const int64_t *targets, float t
     if (!good_head(head) || !good_temperature(temperature) || !good_grads(*head, grads)) return GS_ERR_INVALID_ARG;
     const int64_t rows = head->rows;
     if (rows && (!good(targets, 8) || !good(row_stats, 4) || !good(dlogp, 4))) return GS_ERR_INVALID_ARG;
-    if (!good(d_workspace, 256) || workspace_bytes < gs_head_workspace_bytes(rows, head->hidden, head->vocab, 1)) return GS_ERR_WORKSPACE;
+    if (!good(d_workspace, 256) || workspace_bytes < gs_head_logp_grad_workspace_bytes(rows, head->hidden, head->vocab)) return GS_ERR_WORKSPACE;
     Ranges R;
     R.add(*head);
     R.add(*head, *grads);
@@ -1391,7 +1401,7 @@ gs_status gs_head_logp_grad(const gs_head *head, const int64_t *targets, float t
     R.add(dlogp, rows * 4, false);
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
-    const Call C = call_of(*head, targets, temperature, true, d_workspace, stream);
+    const Call C = call_of(*head, targets, temperature, GRADIENT, d_workspace, stream);
     hipError_t e = pack_rows(C, dlogp, nullptr, nullptr);
     if (e == hipSuccess) {
         k_head_rows<<<(uint32_t)((C.P.rows + 255) / 256), 256, 0, C.stream>>>(C.live, row_stats, dlogp, C.it, C.row());
@@ -1419,7 +1429,7 @@ gs_status gs_head_cross_entropy(const gs_head *head, const int64_t *targets, con
     R.add(d_loss, 4, true);
     R.add(d_workspace, (int64_t)workspace_bytes, true);
     if (!R.apart()) return GS_ERR_INVALID_ARG;
-    const Call C = call_of(*head, targets, temperature, grads != nullptr, d_workspace, stream);
+    const Call C = call_of(*head, targets, temperature, grads ? LOSS : SCORES, d_workspace, stream);
     hipError_t e = pack_rows(C, weights, logp, nullptr);
     if (e == hipSuccess) e = forward(C, logp, nullptr, weights, grads != nullptr);
     const Loss loss = {logp, weights, d_loss, accumulate};

@@ -27,7 +27,7 @@ def preference_step_without_logits(head: Head, micro_batches: list[Pairs], beta:
     dw, db = torch.empty_like(w), torch.empty_like(bias)
     loss, margins = torch.empty(1, device=DEV), []
     for j, b in enumerate(micro_batches):
-        rows, ws = len(b.targets), head.room(len(b.targets))
+        rows, ws = len(b.targets), head.room(len(b.targets), loss=False)
         logp, dlogp, row_stats = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, 2, device=DEV)
         margins.append(torch.empty((len(b.offsets) - 1) // 2, device=DEV))
         gs.gs_head_logp(b.x, w, bias, b.targets, logp, row_stats, d_workspace=ws)

@@ -627,6 +627,8 @@ _u64 = ctypes.c_uint64
 _sz = ctypes.c_size_t
 _lib.gs_head_workspace_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
 _lib.gs_head_workspace_bytes.restype = _sz
+_lib.gs_head_logp_grad_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.gs_head_logp_grad_workspace_bytes.restype = _sz
 _lib.gs_head_logp.argtypes = [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]
 _lib.gs_head_logp.restype = ctypes.c_int
 _lib.gs_head_logp_grad.argtypes = [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _sz, _vp]
@@ -673,6 +675,11 @@ def _rows_like(x, name: str, shape: tuple, dtype) -> tuple:
 
 def gs_head_workspace_bytes(rows: int, hidden: int, vocab: int, gradient: bool = True) -> int:
     return int(_lib.gs_head_workspace_bytes(rows, hidden, vocab, int(bool(gradient))))
+
+
+def gs_head_logp_grad_workspace_bytes(rows: int, hidden: int, vocab: int) -> int:
+    """Enough for gs_head_logp of the same sizes too."""
+    return int(_lib.gs_head_logp_grad_workspace_bytes(rows, hidden, vocab))
 
 
 def _head(x, w, bias) -> gs_head:

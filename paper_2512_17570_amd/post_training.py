@@ -58,9 +58,10 @@ class Head:
     def parameters(self):
         return [self.weight, self.bias]
 
-    def room(self, rows: int):
-        """Workspace of the head's calls without logits, kept for the largest batch so far."""
-        need = gs.gs_head_workspace_bytes(rows, self.weight.w.size(1), self.weight.w.size(0))
+    def room(self, rows: int, loss: bool = True):
+        """Workspace of the head's calls without logits, kept for the largest batch so far; loss: gs_head_cross_entropy is one of them."""
+        vocab, hidden = self.weight.w.shape
+        need = gs.gs_head_workspace_bytes(rows, hidden, vocab) if loss else gs.gs_head_logp_grad_workspace_bytes(rows, hidden, vocab)
         if self.head_workspace is None or self.head_workspace.numel() < need:
             self.head_workspace = torch.empty(need, dtype=torch.uint8, device=DEV)
         return self.head_workspace

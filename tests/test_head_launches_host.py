@@ -67,6 +67,7 @@ def lib(tmp_path_factory):
     subprocess.run(["g++", "-shared", "-Wl,-Bsymbolic", "-Wl,-z,defs", "-Wl,-z,muldefs", o, "-o", so], check=True, capture_output=True, text=True)
     lib = ctypes.CDLL(so)
     lib.gs_head_workspace_bytes.argtypes, lib.gs_head_workspace_bytes.restype = [i64, i64, i64, ctypes.c_int], sz
+    lib.gs_head_logp_grad_workspace_bytes.argtypes, lib.gs_head_logp_grad_workspace_bytes.restype = [i64, i64, i64], sz
     lib.gs_head_logp.argtypes = [vp, vp, f32, vp, vp, vp, sz, vp]
     lib.gs_head_logp_grad.argtypes = [vp, vp, f32, vp, vp, vp, vp, sz, vp]
     lib.gs_head_cross_entropy.argtypes = [vp, vp, vp, f32, vp, vp, vp, ctypes.c_int, vp, sz, vp]
@@ -85,7 +86,10 @@ class Call:
         g = Grads(*[a if n in parts.split() else None for n, a in (("dx", DX), ("dw", DW), ("db", DB))], hidden, hidden)
         h, g, t = ctypes.byref(h), ctypes.byref(g), f32(1.0)
         self.w = W + w_shift, W + w_shift + 2 * ((vocab - 1) * (hidden + w_pad) + hidden)
-        self.bytes = lib.gs_head_workspace_bytes(rows, hidden, vocab, what not in ("logp", "evaluation"))
+        if what == "logp_grad":
+            self.bytes = lib.gs_head_logp_grad_workspace_bytes(rows, hidden, vocab)
+        else:
+            self.bytes = lib.gs_head_workspace_bytes(rows, hidden, vocab, what == "loss")
         call = {"logp": lambda: lib.gs_head_logp(h, TARGETS, t, LOGP, STATS, WS, self.bytes, None),
                 "logp_grad": lambda: lib.gs_head_logp_grad(h, TARGETS, t, STATS, LOGP, g, WS, self.bytes, None),
                 "evaluation": lambda: lib.gs_head_cross_entropy(h, TARGETS, WEIGHTS, t, LOGP, None, LOSS, 0, WS, self.bytes, None),
@@ -172,6 +176,22 @@ def test_every_kernel_is_reached(lib):
     buffer = ctypes.create_string_buffer(1 << 16)
     lib.rec_kernels(buffer, len(buffer))
     assert {n for n in buffer.value.decode().split("\n") if n.startswith("k_")} - REACHED <= {n for n in buffer.value.decode().split("\n") if "<false>" in n and ("gather" in n or "pack" in n)}
+
+
+@pytest.mark.parametrize("rows, hidden, vocab", SIZES + [(1024, 4096, 131_072), (1024, 512, 131_072), (1024, 448, 131_072), (1025, 512, 131_072), (2, 512, 1 << 21)])
+def test_a_gradient_asks_for_no_memory_that_only_a_loss_uses(lib, rows, hidden, vocab):
+    """A loss keeps z, in 32 bits, of up to 2^27 values and of states that are wide enough; gs_head_logp_grad never does, and all that it asks for is
+    read or written where weights have to be packed, but for alignment and for the rest of a tile of 256 packed words."""
+    padded, words = max(64, -(-rows // 64) * 64), -(-vocab // 256) * 256
+    more = lib.gs_head_workspace_bytes(rows, hidden, vocab, 1) - lib.gs_head_logp_grad_workspace_bytes(rows, hidden, vocab)
+    kept = any(s.role == "z" for s in Call(lib, "loss", rows, hidden, vocab).spans)
+    assert kept == (more > 0) and more <= 1 << 29
+    if kept:
+        assert padded * words * 4 <= more and hidden > 448
+    assert lib.gs_head_workspace_bytes(rows, hidden, vocab, 0) <= lib.gs_head_logp_grad_workspace_bytes(rows, hidden, vocab)
+    c = Call(lib, "logp_grad", rows, hidden, vocab, w_shift=2)
+    used = max(s.hi for s in c.spans if WS <= s.lo < WS + (1 << 50)) - WS
+    assert c.bytes - used < 256 + 255 * 2 * -(-hidden // 64) * 64 and not any(s.role == "z" for s in c.spans)
 
 
 # ---- tiles and dies -------------------------------------------------------------------------------------------------------
