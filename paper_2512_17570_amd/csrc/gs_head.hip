@@ -1167,14 +1167,15 @@ static Logit logit_of(const Call &C, int64_t word0, int64_t words)
 }
 static uint32_t grid_of(int64_t tiles) { return (uint32_t)(up(tiles, 8)); }
 
-// each(first word, words, their weights) of every piece; have_w: weights packed as one piece are there already
-template <typename F> static hipError_t pieces(const Call &C, bool have_w, F each)
+// each(first word, words, their weights) of every piece; have_w: weights packed as one piece are there already; reads_w: whether weights are read at all
+template <typename F> static hipError_t pieces(const Call &C, bool have_w, bool reads_w, F each)
 {
-    const int64_t piece = C.packed ? C.P.packed : C.P.piece;
+    const bool packed = C.packed && reads_w;
+    const int64_t piece = packed ? C.P.packed : C.P.piece;
     for (int64_t w = 0; w < C.h.vocab; w += piece) {
         const int64_t words = std::min(piece, C.h.vocab - w);
         Operand W = {C.h.w + w * C.h.w_stride, C.h.w_stride, words, C.h.hidden};
-        if (C.packed) {
+        if (packed) {
             if (!(have_w && piece >= C.h.vocab))
                 if (hipError_t e = pack(C, W.p, W.stride, Live{}, words, words, C.w()); e != hipSuccess) return e;
             W = {C.w(), C.P.width, words, C.P.width};
@@ -1188,7 +1189,7 @@ template <typename T>
 static hipError_t forward(const Call &C, float *logp, float *row_stats, const float *row_weights, bool gradient)
 {
     const Operand X = {C.x(), C.P.width, C.P.rows, C.P.width};
-    hipError_t e = pieces(C, false, [&](int64_t w, int64_t words, const Operand &W) {
+    hipError_t e = pieces(C, false, true, [&](int64_t w, int64_t words, const Operand &W) {
         k_head_stats<T><<<grid_of(up(words, T::BM) / T::BM * (C.P.rows / T::BN)), T::BLOCK, 0, C.stream>>>(W, X, (int)(C.P.width / BK), logit_of(C, w, words));
         return hipGetLastError();
     });
@@ -1261,7 +1262,7 @@ static hipError_t backward(const Call &C, const gs_head_grads &D, bool after_for
     const bool have_z = after_forward && P.kept;
     if (loss.loss && !have_z) k_head_loss<<<1, 256, 0, C.stream>>>(C.live, loss);
     const Operand X = {C.x(), P.width, P.rows, P.width};
-    hipError_t e = pieces(C, after_forward, [&](int64_t w, int64_t words, const Operand &W) {
+    hipError_t e = pieces(C, after_forward, !have_z || D.dx, [&](int64_t w, int64_t words, const Operand &W) {
         const Logit G = logit_of(C, w, words);
         if (have_z) k_head_dz_kept<<<dim3((uint32_t)P.rows + 1, (uint32_t)((words + 1023) / 1024)), 256, 0, C.stream>>>(G, w == 0 ? loss : Loss{});
         else (P.words == Tiny::BM ? launch_dz<Tiny> : P.side == Slim::BN ? launch_dz<Slim> : P.side == Mid::BN ? launch_dz<Mid> : launch_dz<Big>)(C, W, X, G);

@@ -47,3 +47,17 @@ def test_losses_and_scores_stay_in_their_workspace(rows, hidden, vocab, pad):
     gs.gs_head_cross_entropy(c.x, c.w, c.bias, c.targets, c.weights, c.logp, None, None, None, c.loss, ws)
     gs.gs_head_logp(c.x, c.w, c.bias, c.targets, c.logp, c.stats, d_workspace=ws)
     assert bool((behind == 0xA5).all())
+
+
+@pytest.mark.parametrize("rows, hidden, vocab", [(40, 1000, 200_000), (300, 5000, 30_000), (40, 1000, 8300)])
+def test_a_loss_with_some_of_its_gradients(rows, hidden, vocab):
+    """z is kept and the weights are packed: the gradients that are asked for are those of a call that is asked for all."""
+    c = Case(rows, hidden, vocab, bias=True, prompt=True, w_stride=hidden + 3)
+    want = {k: v.clone() for k, v in c.cross_entropy().items()} | {"loss": c.loss.clone()}
+    for parts in ("dw db", "dw", "db", "dx"):
+        for t in (c.logp, c.dx, c.dw, c.db, c.loss):
+            t.fill_(7.0)
+        gs.gs_head_cross_entropy(c.x, c.w, c.bias, c.targets, c.weights, c.logp, *[t if n in parts.split() else None for n, t in (("dx", c.dx), ("dw", c.dw), ("db", c.db))],
+                                 c.loss, c.workspace())
+        for n, t in {"logp": c.logp, "dx": c.dx, "dw": c.dw, "db": c.db, "loss": c.loss}.items():
+            assert torch.equal(t, want[n]) if n in ("logp", "loss") or n in parts.split() else bool((t == 7.0).all()), (parts, n)

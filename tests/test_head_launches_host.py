@@ -194,6 +194,20 @@ def test_a_gradient_asks_for_no_memory_that_only_a_loss_uses(lib, rows, hidden, 
     assert c.bytes - used < 256 + 255 * 2 * -(-hidden // 64) * 64 and not any(s.role == "z" for s in c.spans)
 
 
+@pytest.mark.parametrize("rows, hidden, vocab, pieces", [(40, 1000, 16_384, 1), (40, 1000, 200_000, 4), (300, 5000, 30_000, 3), (3000, 520, 40_000, 1)])
+def test_weights_are_packed_where_they_are_read(lib, rows, hidden, vocab, pieces):
+    """A loss that kept z reads the weights for the hidden states' gradient only; packed as one piece they are there from the forward pass."""
+    def packed(what, parts):
+        c = Call(lib, what, rows, hidden, vocab, parts, w_pad=3).check()
+        return sum(s.role == "w packed" and s.write for s in c.spans), sum(l.is_a("k_head_dw") for l in c.launches)
+
+    assert packed("evaluation", "")[0] == pieces
+    for parts in ("dw", "db", "dw db", ""):
+        assert packed("loss", parts) == (pieces, "dw" in parts)
+    assert packed("loss", "dx dw db")[0] == packed("loss", "dx")[0] == (1 if pieces == 1 else 2 * pieces)
+    assert packed("logp_grad", "dw")[0] == pieces
+
+
 # ---- tiles and dies -------------------------------------------------------------------------------------------------------
 
 def dies_work(lib, tile, of_rows, workgroups, across, rows, count):
