@@ -436,7 +436,6 @@ struct Logit {
     int64_t word0, words;     // this piece of the vocabulary; tiles' words are counted from word0
     int64_t vocab;
     float k;                  // log2(e) / temperature
-    float it;                 // 1 / temperature
     float2 *partials;         // [tile of words][rows]: maximum, sum
     float *target_logit;      // [rows]
     float *z;                 // null, or [rows][z_stride], this piece's: z is kept, in 32 bits
@@ -1155,7 +1154,6 @@ static Logit logit_of(const Call &C, int64_t word0, int64_t words)
     G.words = words;
     G.vocab = C.h.vocab;
     G.k = kLog2e * C.it;
-    G.it = C.it;
     G.partials = C.partials();
     G.target_logit = C.target();
     G.z = C.P.kept ? reinterpret_cast<float *>(C.ws + C.P.z) + word0 : nullptr;
