@@ -633,10 +633,11 @@ gs_status gs_grads_clip(const gs_tensor *tensors, int64_t count, const double *d
  * A linear head without its logits.  With x a hidden state (a row of `hidden` bf16 values) and W, b the head's working
  * weights,
  *     z_i = sum_h x_h W_ih + b_i                 (products of bf16 values, sums and z in 32 bits, never rounded)
- * takes the place of a row of logits above: M, S, logp, targets, temperature and rows without a token are as there.  z is
- * never in memory: the forward pass leaves a maximum and a sum for each tile of words, the gradient makes z again,
- * a piece of the vocabulary at a time.  Rows without a token, or without a factor, cost no product, and what they hold
- * counts nowhere.
+ * takes the place of a row of logits above: M, S, logp, targets, temperature and rows without a token are as there.  The
+ * forward pass leaves a maximum and a sum for each tile of words, and z is gone; the gradient makes it again and has dz in the workspace, in bf16, a piece of
+ * the vocabulary at a time (at most 512 MiB).  One exception: gs_head_cross_entropy with a gradient keeps z, in 32 bits in the workspace, where it is at most
+ * 512 MiB (rows x vocab rounded up to tiles) and hidden is more than 448, which is a product less; there all of dz lies beside it.  Rows without a
+ * token, or without a factor, cost no product, and what they hold counts nowhere.
  * ------------------------------------------------------------------------------------------ */
 
 /* x: `rows` (0 .. 2^20) hidden states of `hidden` (1 .. 2^17) bf16 values, row r at element r * x_stride; w: `vocab` (1 .. 2^30) rows of
@@ -662,7 +663,10 @@ typedef struct {
 } gs_head_grads;
 
 /* Bytes of device workspace that the calls below need for such a head, with or without a gradient; 0 for sizes that they refuse.  gs_head_logp_grad
- * does with less than a loss with its gradient where that keeps z, and gs_head_logp always does with what gs_head_logp_grad needs.
+ * does with less than a loss with its gradient where that keeps z, and gs_head_logp always does with what gs_head_logp_grad needs.  MiB of scores, of
+ * gs_head_logp_grad and of a loss with its gradient: 64 x 4096 x 32000 129, 141, 148; 1024 x 4096 x 131072 140, 460, 972; 8192 x 4096 x 131072 224, 864, 864.  Up to 128 of
+ * each are for a copy of weights, since their alignment is not known here; the rest grows with rows x hidden, and with the vocabulary by a maximum and a sum of each
+ * row and tile of words.
  * The workspace is aligned to 256 bytes; nothing has to be in it before, and nothing is kept in it from call to call.  Calls that may run at the same time
  * (on two streams, or captured into graphs that do) need one each. */
 size_t gs_head_workspace_bytes(int64_t rows, int64_t hidden, int64_t vocab, int gradient);

@@ -1,11 +1,12 @@
 // gs_head.hip -- a linear head's token log-probabilities and cross entropy without its logits: z = x W^T + b is made a tile at a
 // time in registers, leaves a maximum and a sum of exponentials, and is gone.  The gradient makes it again, a piece of the
-// vocabulary at a time, as dz in bf16, which two more products take to the hidden states and to the weights.
+// vocabulary at a time, as dz in bf16, which two more products take to the hidden states and to the weights; where z is small (kKeptBytes) a loss leaves it
+// in memory instead.
 //
 // All the work is in products of matrices: 2 N V H operations for the log-probabilities and 8 N V H with the gradient (2 of them to make
-// z again), on the matrix cores.  rows x hidden x vocabulary: 8192 x 2048 x 50304 scored in 1.34 ms (1262 TFLOP/s), 8192 x 4096 x 131072 with its gradients
-// 26.5 ms (1330 TFLOP/s), 4095 x 2048 x 50001 with a bias 2.33 ms; with few rows memory is the bound: one of 4096 x 131072 scored in 161 us (7.0 TB/s of weights),
-// 64 x 4096 x 32000 with gradients 212 us.
+// z again), on the matrix cores.  rows x hidden x vocabulary: 8192 x 2048 x 50304 scored in 1.28 to 1.34 ms (1260 to 1315 TFLOP/s), 8192 x 4096 x 131072 with its
+// gradients 26.0 to 26.5 ms (1330 to 1350 TFLOP/s), 4095 x 2048 x 50001 with a bias, of whose rows 3075 count, 2.28 to 2.34 ms; with few rows memory is the bound: one of
+// 4096 x 131072 scored in 161 us (7.0 TB/s of weights), 64 x 4096 x 32000 with gradients 212 to 222 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -722,7 +723,8 @@ __global__ __launch_bounds__(TX::BLOCK, 2) void k_head_dx_dw(Operand W, Operand 
     }
 }
 
-// db[word] = sum over rows of dz: a lane two words, a wave a share of the rows; dz is read once more (4095 x 50001 59 us, 6.9 TB/s)
+// db[word] = sum over rows of dz, of the same one in bf16 that dW takes (db is dW of a state that is 1 in every row): a lane two words, a wave a share of the rows; dz is read
+// once more (3075 rows that count x 50001 59 us, 5.2 TB/s)
 __global__ __launch_bounds__(1024) void k_head_db(const uint16_t *dz, int64_t dz_stride, Live live, int64_t words, const float4 *row, uint16_t *db)
 {
     __shared__ float part[16][128];
@@ -1013,9 +1015,13 @@ typedef Tile<64, 64, 2, 2, 3> Tiny;           // up to 64 rows and so few words 
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxHidden = 1 << 17, kMaxVocab = 1 << 30;
 constexpr int64_t kPieceBytes = 512 << 20;          // of dz: 8192 x 4096 x 131072 25.9 ms, with 256 MB 26.1, 128 MB 26.0, 64 MB 27.1; 4095 x 2048 x 50001 2.33, 2.43, 2.69, 2.82
-constexpr int64_t kKeptBytes = 512 << 20;           // of z, in 32 bits: what a call may take beside dz
+// Of z, in 32 bits: what a call may take beside dz.  A bound on memory, not where time turns; a loss in us, kept and made again: 64 x 4096 x 32000 222/243, 1000 x 2048 x 32000
+// 446/500, 1024 x 4096 x 131072 3013/3641, and of more, with a limit of 1 GiB, 2600 x 2048 x 50304 1742/1990, 4095 x 2048 x 50001 2430/2777, 8192 x 512 x 32000 1255/1198.
+constexpr int64_t kKeptBytes = 512 << 20;
 static_assert(kKeptBytes <= 2 * kPieceBytes, "of a batch whose z is kept, dz is one piece");
-constexpr int64_t kKeptWidth = 512;                 // of the hidden state from which z is kept: 1354 x 320 x 39296 355 us kept, 324 made again
+// Of the hidden state from which z is kept, us kept and made again: 1354 x 320 x 39296 355/324; of 512 few rows gain, 500 x 50304 195/206, 128 rows of 1024 x 50304
+// 107/119, and many lose, 4000 x 512 x 32000 673/635.
+constexpr int64_t kKeptWidth = 512;
 constexpr int64_t kPackedBytes = 128 << 20;         // of weights that cannot be read where they lie
 // Large tiles up to which a product is done in small ones, four times as many, all of which run at once, two on each of the 256 CUs.  Scored, us, large
 // against small: 256 rows of 4096 x 32000 (125 tiles) 117/99, of 2048 x 50304 (197) 79/96, 200 of 4096 x 50304 (197) 133/172, 512 of 4096 x 32000 (250)

@@ -6,8 +6,8 @@
 //     are read again
 //   * vectors of 16 bytes at any address the element type allows: the hardware takes them from wherever they lie
 //
-// 16384 x 8192 bf16: norm 94 us (5.7 TB/s), gradient 148 (5.4), dropout onto a residual 122 (6.6; a copy on this card 6.7).  One row of 8192 4.2 us,
-// dropout of 257 x 1024 4.0, where a launch takes 3.7.
+// 16384 x 8192 bf16: norm 94 us (5.7 TB/s), gradient 148 (5.4), dropout onto a residual 122 to 124 (6.6; a copy on this card 6.7).  One row of 8192 4.2 us,
+// dropout of 257 x 1024 4.0, where a launch takes 3.7.  Pass after pass; in the first milliseconds of a load the clock moves, and the gradient takes up to 190.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -380,7 +380,8 @@ struct NormGradArgs {
     bool through;
 };
 // Rows dealt in turn to the workgroups' teams, which add up dy xhat and dy of their own rows for each column; a workgroup's teams join theirs in LDS.  The next
-// row is on its way while one is worked on, unless the registers of 1024 lanes have no room for it.  16384 x 8192 bf16 143 us (5.6 TB/s), 1023 x 1001 fp32 7.
+// row is on its way while one is worked on, unless the registers of 1024 lanes have no room for it.  16384 x 8192 bf16 143 us (5.6 TB/s) of the gradient's 148, 1023 x 1001
+// fp32 7 of 12; 8192 x 16384 bf16 152 with the fold, 8192 x 8192 fp32 141.
 template <typename E, typename W, int TEAM, int NV, bool WHOLE>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormGradArgs A)
 {
@@ -495,7 +496,8 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormGradA
         }
     }
 }
-// Rows that no team holds: dx from two readings, a row a workgroup;
+// Rows that no team holds: dx from two readings, a row a workgroup (8192 x 16384 fp32, with the columns' sums and the fold, 571 us, 2.8 TB/s of what has to move; 8191 x 16383 bf16 484,
+// 8191 x 8191 fp32 319);
 template <typename E, typename W>
 __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs A)
 {
@@ -558,7 +560,7 @@ __global__ __launch_bounds__(256) void k_norm_columns(NormGradArgs A, int64_t pe
         if (c + i < n) out[c + i] = dgamma[i], out[n + c + i] = dbeta[i];
 }
 // Sums over the workgroups: a lane a column of one of the two, 16 waves that each take a share; joined in 64 bits.  A launch of its own
-// (3.5 to 5 us): the workspace comes uncleared, so nothing in it can tell the last workgroup of the gradient that it is.
+// (3.5 to 5 us), since it takes many workgroups: one alone reads 512 partials of 1024 columns in 30 us, 256 of 8192 in 148 (110 to 140 GB/s).
 template <typename W>
 __global__ __launch_bounds__(1024) void k_norm_fold(const float *partials, int parts, int64_t cols, void *dgamma, void *dbeta)
 {
@@ -652,6 +654,8 @@ __global__ __launch_bounds__(DROP_BLOCK) void k_dropout(DropoutArgs A)
 
 // ---- launches ------------------------------------------------------------------------------------
 constexpr int64_t kMaxItems = 0xffffffffLL;      // HIP launches fewer than 2^32 work items at a time
+// Rows of more than 1024 vectors are a workgroup's in any case (8192 x 8192 fp32 97 us, 5.5 TB/s, 8192 x 16384 bf16 105, of odd width 166); of more than 4096 they are read three
+// times (8192 x 32768 bf16, the last that are held, 272).
 // Rows up to which a row's own time counts: a workgroup a row (with more of them, the ones that stay: 512 x 4096 bf16 3.8 us, a workgroup a row 4.6; 768
 // x 4096 4.1 and 6.3, 256 x 8192 3.9 and 3.8).
 constexpr int64_t NORM_FEW = 256;
@@ -703,7 +707,7 @@ static hipError_t launch_norm(const NormArgs &A, hipStream_t stream)
     return launch_norm_as<E, W, 1024, 1, false, false>(A, stream);
 }
 
-// Workgroups of a gradient over rows that are held: all that fit the chip at once, two a CU.
+// Workgroups of a gradient over rows that are held: all that fit the chip at once, two a CU, or one of 1024 lanes.
 template <typename E, typename W, int TEAM, int NV>
 static hipError_t launch_norm_grad_as(const NormGradArgs &A, int &parts, hipStream_t stream)
 {
