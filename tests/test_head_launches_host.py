@@ -194,6 +194,18 @@ def test_a_gradient_asks_for_no_memory_that_only_a_loss_uses(lib, rows, hidden, 
     assert c.bytes - used < 256 + 255 * 2 * -(-hidden // 64) * 64 and not any(s.role == "z" for s in c.spans)
 
 
+def test_sizes_and_workspaces_that_are_refused(lib):
+    size = lib.gs_head_logp_grad_workspace_bytes
+    assert size(-1, 64, 64) == size((1 << 20) + 1, 64, 64) == size(1, 0, 64) == size(1, (1 << 17) + 1, 64) == size(1, 64, 0) == size(1, 64, (1 << 30) + 1) == 0
+    rows, hidden, vocab = 1000, 2048, 32_000                # a loss would keep z
+    h, g = Head(X, W, BIAS, rows, hidden, vocab, hidden, hidden), Grads(DX, DW, DB, hidden, hidden)
+    lib.rec_reset()
+    for ws, n in ((WS, size(rows, hidden, vocab) - 1), (WS + 8, 1 << 40), (None, 1 << 40)):
+        assert lib.gs_head_logp_grad(ctypes.byref(h), TARGETS, 1.0, STATS, LOGP, ctypes.byref(g), ws, n, None) == -2
+    assert lib.gs_head_cross_entropy(ctypes.byref(h), TARGETS, WEIGHTS, 1.0, LOGP, ctypes.byref(g), LOSS, 0, WS, size(rows, hidden, vocab), None) == -2
+    assert lib.rec_count() == 0
+
+
 @pytest.mark.parametrize("rows, hidden, vocab, pieces", [(40, 1000, 16_384, 1), (40, 1000, 200_000, 4), (300, 5000, 30_000, 3), (3000, 520, 40_000, 1)])
 def test_weights_are_packed_where_they_are_read(lib, rows, hidden, vocab, pieces):
     """A loss that kept z reads the weights for the hidden states' gradient only; packed as one piece they are there from the forward pass."""
